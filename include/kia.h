@@ -93,6 +93,9 @@ extern "C" {
 #define KIA_ERR_ALIGN (-7)   /* tensor not 16-byte or stats not 256-byte aligned */
 #define KIA_ERR_HIP (-8)     /* HIP launch/runtime error */
 #define KIA_ERR_SCRATCH (-9) /* statistics larger than KIA_STATIC_BYTES */
+#define KIA_ERR_HEADS (-10)  /* H is no multiple of Hkv */
+#define KIA_ERR_VIEW (-11)   /* a view's strides (see kia_view) */
+#define KIA_ERR_CACHE (-12)  /* a page that is not 16, 32, 64, 128 or 256 tokens */
 
 #define KIA_CALIB_MINMAX 0
 #define KIA_CALIB_FWM 1
@@ -494,6 +497,156 @@ int kia_set_grid_policy(int policy);
  * for another value.
  */
 int kia_set_deterministic(int on);
+
+/*
+ * ---- Operators around the attention ---------------------------------------
+ *
+ * What a model trained with the operator needs beside it: positions, local
+ * layers, and the form for serving new tokens from a key/value cache. The
+ * conventions above hold (streams, checks before any launch, no allocation
+ * and no synchronization, return codes), with these differences:
+ *   - tensors are views [B, heads, T, d] with contiguous rows and any other
+ *     strides, so that a projection's [B, T, heads, d] needs no copy;
+ *   - query heads may share key heads: head h reads key head h / (H / Hkv)
+ *     (else KIA_ERR_HEADS);
+ *   - `dtype` (KIA_F32 or KIA_BF16) is the type of every tensor of a call,
+ *     outputs among them; sums, statistics and angles are fp32 or wider, and
+ *     an output is rounded once, to nearest even;
+ *   - arrays of int32 (positions, lengths, starts, counts, tables) are on the
+ *     device and read when the kernels run: values that the caller may not
+ *     pass (a page that the cache does not have, a position past the table)
+ *     are skipped as each call says and never followed;
+ *   - B*H*T*d may pass 2^31; T is at most 2^24;
+ *   - every call is bitwise repeatable, and keeps no state.
+ * The kernels are timed as "kia_rotary", "kia_window_fwd", "kia_window_dq",
+ * "kia_window_dkv", "kia_window_sum", "kia_cache4_write", "kia_cache4_read",
+ * "kia_cache4_extrema", "kia_cache4_attn" and "kia_cache4_join".
+ */
+#define KIA_F32 0
+#define KIA_BF16 1
+
+/*
+ * Element (b, h, t, c) of a view is data[b*sb + h*sh + t*st + c]. data is
+ * 16-byte aligned; each stride is a multiple of 16 bytes, sb and sh at least
+ * 0 (0: one slice for all, inputs only), st at least d and at most 2^22 (else
+ * KIA_ERR_VIEW; a stride of a dimension of size 1 is not looked at). Rows of
+ * an output may not overlap another's nor an input's, except that kia_rotary
+ * may write over its input.
+ */
+typedef struct kia_view {
+  void *data;
+  int64_t sb, sh, st;
+} kia_view;
+
+/*
+ * Rotary positions. Pair n of the first `rot` channels (even, 2 .. d), channels
+ * n and n + rot/2 (KIA_ROTARY_HALF) or 2n and 2n + 1 (KIA_ROTARY_NEIGHBOURS),
+ * turns by the angle a = p * freq[n] (radians; freq: rot/2 doubles on the
+ * device): (x, y) -> factor * (x cos a - y sin a, y cos a + x sin a). The
+ * other channels are copied. p is positions[b*positions_sb + t] (int32, any
+ * sign) or, with positions NULL, first + t. back = 1 takes -a: the gradient.
+ * Angles are taken in fp64. k and k_out may both be NULL (Hkv is then not
+ * looked at). q_out and k_out may be q and k.
+ */
+#define KIA_ROTARY_HALF 0
+#define KIA_ROTARY_NEIGHBOURS 1
+int kia_rotary(const kia_view *q, const kia_view *q_out, const kia_view *k,
+               const kia_view *k_out, const int32_t *positions,
+               int64_t positions_sb, int first, const double *freq,
+               float factor, int layout, int back, int B, int H, int Hkv,
+               int T, int d, int rot, int dtype, void *stream);
+
+/*
+ * Softmax attention with a sliding window and visible first tokens, causal:
+ * query i sees key j iff j <= i and (i - j < window or j < sinks), and, with
+ * `lengths` (int32 [B], or NULL), i < lengths[b]. window >= 1 (T or more:
+ * every earlier key), sinks >= 0. s = q.k / sqrt(d).
+ *   o = sum_j e^{s_j - lse} v_j, lse = ln sum_j e^{s_j} ([B,H,T] fp32,
+ *   contiguous); a query past its sequence has o = 0 and lse = -infinity.
+ * Rows at or past lengths[b] (clamped to [0, T]) of q, k, v and dO are never
+ * read as values, and what a query does not see has no influence on it,
+ * infinities and NaNs included.
+ * Backward: dq, dk, dv of a loss with gradient dO at o, from the forward's o
+ * and lse (dk and dv summed over the query heads of a key head); 0 in rows
+ * past their sequence. `ws`: kia_window_ws_bytes bytes, 256-byte aligned,
+ * uninitialized.
+ * bf16: the weights and the score gradients enter their products rounded to
+ * bf16 (2^-8 of each). fp32: every product is an fp32 product.
+ */
+int kia_window_fwd(const kia_view *q, const kia_view *k, const kia_view *v,
+                   const kia_view *o, float *lse, const int32_t *lengths,
+                   int B, int H, int Hkv, int T, int d, int window, int sinks,
+                   int dtype, void *stream);
+int kia_window_ws_bytes(int B, int H, int Hkv, int T, int d, int window,
+                        int sinks, size_t *bytes);
+int kia_window_bwd(const kia_view *q, const kia_view *k, const kia_view *v,
+                   const kia_view *o, const kia_view *dO, const float *lse,
+                   const int32_t *lengths, void *ws, const kia_view *dq,
+                   const kia_view *dk, const kia_view *dv, int B, int H,
+                   int Hkv, int T, int d, int window, int sinks, int dtype,
+                   void *stream);
+
+/*
+ * A key/value cache in 4 bits, in pages. d in {32, 64, 128}; `page` tokens
+ * (16, 32, 64, 128 or 256). Groups of 32 neighbouring channels of a token share
+ * a scale 2^(s - 127) with s a byte, the least of 2^-126 .. 2^125 under which
+ * no value passes 6 (above 6 2^125: 6); a value is held as the nearest of 0,
+ * 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives times the scale, an even level
+ * (of 0 .. 7 in that order) between two. A group with an infinity or NaN has s
+ * = 255 and stands for 32 NaNs.
+ * Layout, bytes: cache[pages][2][Hkv][page * (d/2 + d/32)]: a head's keys
+ * (0) and values (1), in each block the codes and then the scales. A code is
+ * the level plus 8 for a minus; a byte holds two, the even channel low.
+ *   keys:   codes [page][d/2], scales [page][d/32];
+ *   values: codes [page/4][16][4][d/32]: of four tokens side by side the
+ *           channels r*d/16 .. (r+1)*d/16 - 1, then the next r; scales
+ *           [page/4][d/32][4].
+ * Position p of sequence b is token p % page of page table[b*width +
+ * p / page] (int32 [B, width]). Entries outside [0, pages) are no page:
+ * writes to them are dropped, reads give 0, attention does not see them.
+ * width * page < 2^31. Pages may be shared by sequences that only read them.
+ */
+int kia_cache4_bytes(int pages, int page, int Hkv, int d, size_t *bytes);
+/* Writes token t of k, v [B, Hkv, T, d], t < counts[b] (NULL: every t), to
+ * position starts[b] + t; positions below 0 or past the table are dropped.
+ * Nothing else in the cache changes. */
+int kia_cache4_write(const kia_view *k, const kia_view *v, void *cache,
+                     int pages, int page, const int32_t *table, int width,
+                     const int32_t *starts, const int32_t *counts, int B,
+                     int Hkv, int T, int d, int dtype, void *stream);
+/* The values of positions starts[b] + t; 0 where kia_cache4_write would have
+ * dropped the token. (bf16 holds every value exactly.) */
+int kia_cache4_read(const void *cache, int pages, int page,
+                    const int32_t *table, int width, const int32_t *starts,
+                    const int32_t *counts, const kia_view *k,
+                    const kia_view *v, int B, int Hkv, int T, int d,
+                    int dtype, void *stream);
+
+/*
+ * Attention of new tokens over the cache, forward only. lengths[b] (int32,
+ * clamped to [0, width*page]): keys of sequence b, the new tokens' own among
+ * them; query t of T is at position i = lengths[b] - T + t and sees key
+ * j <= i, with window > 0 only if i - j < window or j < sinks (window 0: all).
+ * A query that sees nothing (i < 0, no pages) has o = 0.
+ * Weights by recon: KIA_RECON_SOFTMAX, or LERP / Nearest over the grid of
+ * calib, K and tau as in kia_attn_fwd (softmax looks at none of them), with
+ * the row's extrema over the keys that it sees. s = q.k / sqrt(d) from the
+ * values that the cache stands for, in an order of its own (a Nearest weight
+ * within rounding of a midpoint can fall on the other side than in
+ * kia_attn_fwd). A row that sees an infinite or NaN score under LERP or
+ * Nearest, or a NaN key or value, is NaN there.
+ * For few tokens: keys are read once for every 16 rows of (T x H / Hkv).
+ * bf16: weights are rounded to bf16 (2^-8 of each). fp32: queries and weights
+ * keep all bits (from 2^-100 to 2^126; an infinite query element gives NaN).
+ * `ws`: kia_cache4_ws_bytes bytes, 256-byte aligned, uninitialized.
+ */
+int kia_cache4_ws_bytes(int page, int width, int B, int H, int Hkv, int T,
+                        int d, int window, int sinks, size_t *bytes);
+int kia_cache4_attn(const kia_view *q, const kia_view *o, const void *cache,
+                    int pages, int page, const int32_t *table, int width,
+                    const int32_t *lengths, void *ws, int B, int H, int Hkv,
+                    int T, int d, int K, int calib, float tau, int recon,
+                    int window, int sinks, int dtype, void *stream);
 
 /* Human-readable text for a return code (static storage). */
 const char *kia_strerror(int code);

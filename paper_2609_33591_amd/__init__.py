@@ -91,6 +91,7 @@ def load():
                    "kia_timing_enable",
                    "kia_timing_read"):
             getattr(lib, fn).restype = I
+        around.declare(lib)
         _lib = lib
     return _lib
 
@@ -604,7 +605,7 @@ def _attention_function():
 
 
 def k_interval_attention(q, k, v, K=4, calib="fwm", tau=8.0, recon="nearest", ste="prob",
-                         detach=False, causal=True):
+                         detach=False, causal=True, rotary=None, positions=None):
     """Differentiable K-interval attention: o = attention of q, k, v [B,H,T,d]
     (float32, or bfloat16 with bfloat16 output), with the gradients of
     loss(o) with respect to q, k and v from the library's backward. The
@@ -612,8 +613,12 @@ def k_interval_attention(q, k, v, K=4, calib="fwm", tau=8.0, recon="nearest", st
     (False/True, or a KIA_GRAD_* name such as "max_only"). Where no
     gradient can be taken (grad mode off, or no input requiring grad) the
     forward runs forward-only (gradient mode "none") and o is returned as
-    is."""
+    is. rotary: a RotaryPlan that turns q and k by `positions` first."""
     import torch
+    if rotary is not None:
+        q, k = around.rotary(q, k, rotary, positions)
+    elif positions is not None:
+        raise KiaError("positions without a rotary plan")
     out_dtype = _attention_out_dtype(q, k, v)
     if not (torch.is_grad_enabled() and any(x.requires_grad for x in (q, k, v))):
         q, k, v = (x.contiguous() for x in (q, k, v))
@@ -633,3 +638,12 @@ def _attention_out_dtype(q, k, v):
         raise KiaError("q, k, v must be all float32 or all bfloat16, got "
                        f"{q.dtype}, {k.dtype}, {v.dtype}")
     return torch.bfloat16 if q.dtype == torch.bfloat16 else None
+
+
+# ------------------------------------------------- operators around the attention
+from . import around  # noqa: E402
+from .around import (  # noqa: E402,F401
+    Cache4, RotaryPlan, cache4_attention, cache4_read, cache4_write, kia_cache4_attn,
+    kia_cache4_bytes, kia_cache4_read, kia_cache4_write, kia_cache4_ws_bytes, kia_rotary,
+    kia_window_bwd, kia_window_fwd, kia_window_ws_bytes, new_cache4, rotary, rotary_plan,
+    window_attention, window_backward, window_forward)

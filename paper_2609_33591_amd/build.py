@@ -27,6 +27,9 @@ OBJECTS = {
     "kia_fwd.o": [("kia_fwd.hip", [f"-DKIA_HEAD={d}"]) for d in HEADS] + [("kia_debug.hip", [])],
     "kia_bwd.o": [("kia_bwd.hip", [f"-DKIA_HEAD={d}"]) for d in HEADS],
     "kia_bf16.o": [("kia_bf16.hip", [])],
+    "kia_around.o": [("kia_around_abi.hip", []), ("kia_rotary.hip", []), ("kia_cache.hip", [])],
+    "kia_window.o": [("kia_window.hip", [f"-DKIA_HEAD={d}"]) for d in HEADS],
+    "kia_cached.o": [("kia_cached.hip", [f"-DKIA_HEAD={d}"]) for d in HEADS[1:]],
 }
 # (source, flags, object file) of every compilation
 UNITS = [(src, flags, obj if len(parts) == 1 else f"{obj[:-2]}_{i}.o")

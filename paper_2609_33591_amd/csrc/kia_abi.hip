@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "kia.h"
+#include "kia_host.hpp"
 #include "kia_kernels.hpp"
 
 namespace {
@@ -170,6 +171,18 @@ void timed(const char *name, hipStream_t s, F launch) {
   hipEventRecord(t.stop, s);
   g_launches.push_back(t);
 }
+
+}  // namespace
+
+// the same for the entry points of the other files (kia_host.hpp)
+namespace kia {
+int host_cus() { return device_cus(); }
+void timed_launch(const char *name, hipStream_t s, void (*launch)(void *), void *ctx) {
+  timed(name, s, [&] { launch(ctx); });
+}
+}  // namespace kia
+
+namespace {
 
 int launched() {
   return hipGetLastError() == hipSuccess ? KIA_OK : KIA_ERR_HIP;
@@ -928,6 +941,10 @@ extern "C" const char *kia_strerror(int code) {
     case KIA_ERR_SCRATCH:
       return "the problem's statistics exceed the static scratch of kia_attn_fwd_bwd_static "
              "(KIA_STATIC_BYTES)";
+    case KIA_ERR_HEADS: return "the query heads must be a multiple of the key heads";
+    case KIA_ERR_VIEW:
+      return "a view's rows need a 16-byte stride of at least d elements and at most 2^22";
+    case KIA_ERR_CACHE: return "the cache's page must be 16, 32, 64, 128 or 256 tokens";
     default: return "unknown error code";
   }
 }

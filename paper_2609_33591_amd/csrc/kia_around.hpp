@@ -1,0 +1,93 @@
+// kia_around.hpp -- arguments and launchers of the operators around K-interval
+// attention: rotary positions, attention with a sliding window, the 4-bit cache.
+#pragma once
+
+#include "kia.h"
+#include "kia_device.hpp"
+
+namespace kia {
+
+// A [B, heads, T, d] tensor whose rows are contiguous (strides in elements).
+struct View {
+  void *p = nullptr;
+  int64_t sb = 0, sh = 0, st = 0;
+};
+template <typename TI> __device__ __forceinline__ TI *slice_of(const View &v, int b, int h) {
+  return static_cast<TI *>(v.p) + b * v.sb + h * v.sh;
+}
+
+// ---- rotary positions (kia_rotary.hip) ----------------------------------------
+struct RotSide {
+  const void *x;
+  void *y;
+  int64_t xb, xh, xt, yb, yh, yt;
+};
+struct RotArgs {
+  RotSide q, k;  // Hkv = 0: no keys
+  const int *pos;  // or nullptr: first + t
+  int64_t pos_sb;
+  const double *freq;
+  float factor;
+  int first, layout, back, B, H, Hkv, T, d, rot;
+  int tokens, per;  // tokens of a workgroup, rounds of heads of a share (the launcher's)
+};
+void launch_rotary(RotArgs a, int dtype, int cus, hipStream_t s);
+
+// ---- attention with a sliding window (kia_window.hip) ---------------------------
+struct WinArgs {
+  View q, k, v, o, dO, dq, dk, dv;
+  float *lse, *delta, *part;
+  const int *lengths;
+  int B, H, Hkv, T, window, sinks;
+  float scale;
+  // the key blocks' query ranges: blocks that hold first tokens, and the parts that
+  // each block of either kind is cut into
+  int sink_blocks, parts_a, parts_b;
+};
+constexpr int WIN_KB = 128;  // keys of a block of the key gradients
+constexpr int WIN_QT = 32;   // queries of one step there
+
+// Partial sums that the key blocks of one key head leave (blocks of one part leave none).
+__host__ __device__ inline int win_slots(int nkb, int sb, int pa, int pb) {
+  return (pa > 1 ? sb * pa : 0) + (pb > 1 ? (nkb - sb) * pb : 0);
+}
+template <int D> void launch_win_fwd(const WinArgs &a, int dtype, int cus, hipStream_t s);
+template <int D> void launch_win_bwd(const WinArgs &a, int dtype, int cus, hipStream_t s);
+
+// ---- the 4-bit cache (kia_cache.hip) --------------------------------------------
+struct CacheArgs {
+  uint8_t *cache;
+  const int *table, *starts, *counts;  // counts: new tokens of each sequence, or nullptr
+  View k, v;                           // the tokens to hold, or where to read them to
+  int pages, lpage, width, B, Hkv, T;  // lpage: log2 of the tokens of a page
+};
+void launch_cache_write(const CacheArgs &a, int d, int dtype, hipStream_t s);
+void launch_cache_read(const CacheArgs &a, int d, int dtype, hipStream_t s);
+
+struct CachedArgs {
+  const uint8_t *cache;
+  const int *table, *lengths;
+  View q, o;
+  float *ext, *stat, *part;  // workspace (cached_layout)
+  int pages, lpage, width, B, H, Hkv, T;
+  int window, sinks;  // window: INT_MAX where there is none
+  int K, calib, recon;
+  float tau, scale;
+  int tiles, splits;  // 16-row tiles of a key head's rows, workgroups that share a tile's keys
+};
+// Floats of the workspace: the parts' extrema, their maxima and sums, their rows.
+struct CachedLayout {
+  size_t ext, stat, part, total;
+};
+inline CachedLayout cached_layout(const CachedArgs &a, int d) {
+  const size_t n = (size_t)a.B * a.Hkv * a.tiles * a.splits * 16;
+  CachedLayout l;
+  l.ext = 0;
+  l.stat = 2 * n;
+  l.part = 4 * n;
+  l.total = 4 * n + n * d;
+  return l;
+}
+template <int D> void launch_cached(const CachedArgs &a, int dtype, hipStream_t s);
+
+}  // namespace kia

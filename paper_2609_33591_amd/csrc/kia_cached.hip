@@ -1,0 +1,520 @@
+// kia_cached.hip -- attention of a few new tokens over the 4-bit cache on gfx950, for
+// one head dimension (KIA_HEAD): softmax, or the interval weights (LERP, Nearest; MinMax,
+// FWM, resolved) of a model that was trained with them.
+//
+// Bound by memory: every visible key and value is read once, 17/32 byte a channel,
+// and everything else hides under that. Rows (token, head of the key head's group)
+// fill the 16 columns of v_mfma_f32_16x16x32_bf16, the keys its 16 rows: scores come
+// as S^T, lane l holding of row l % 16 the keys 4 (l / 16) + i of each 16-key tile, and
+// so its weights are the B operand of O^T = V^T P^T as they stand, with the key order
+// 16 (e / 4) + 4 (l / 16) + e % 4 in the slots of 32 keys. The cache is laid out for
+// that: a lane's share of a tile, of the keys by token and of the values by column
+// with four tokens side by side, is one access of D / 8 bytes, and a wave's is
+// contiguous. No LDS in the loop; codes become bf16 operands by one instruction a pair
+// (values by another, which puts neighbouring tokens together).
+//
+// A wave takes 64 keys at a time, the four waves of a workgroup and the workgroups
+// that share a row tile each take a part of the keys; parts are joined in order.
+// Softmax runs in one pass with a running maximum. The interval weights' grid
+// depends on the row's extrema, so a first pass over the keys alone (a third of the
+// bytes) finds them; the weights are absolute then and the parts' sums just add.
+//
+// bf16 queries: scores are sums of exact products, weights are rounded to bf16 (2^-8
+// of each) for the product with V. fp32 queries and weights go as three bf16 pieces
+// (exact for 2^-100 to 2^126; smaller ones lose less than 2^-133), which the idle matrix
+// unit takes for free. Sums, extrema and statistics are fp32.
+#include <limits.h>
+
+#include "kia_cache.hpp"
+#include "kia_host.hpp"
+
+namespace kia {
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int CHUNK = 64, NWAVE = 4;
+enum { PASS_SOFTMAX, PASS_EXTREMA, PASS_GRID };
+
+__device__ __forceinline__ f32x4 mma16(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// byte `s` of a word of codes as two bf16
+template <int S> __device__ __forceinline__ uint32_t pair(uint32_t w, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, S));
+}
+__device__ __forceinline__ uint32_t pair_at(int s, uint32_t w, float scale) {
+  return s == 0 ? pair<0>(w, scale) : s == 1 ? pair<1>(w, scale) : s == 2 ? pair<2>(w, scale)
+                                                                     : pair<3>(w, scale);
+}
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// One lane's share of a 64-key chunk: codes and scales of its keys and values.
+template <int D, bool VALUES> struct Stage4 {
+  static constexpr int N = D / 32;  // words of codes of a 16-key tile
+  uint32_t k[4][N], v[VALUES ? 4 : 1][N], vs[VALUES ? 4 : 1];
+  uint8_t ks[4];
+  int ok;  // bit t: the tile's page is one of the cache's
+  // the values of token e (of the lane's four) of tile i as zeros
+  __device__ __forceinline__ void clear(int i, int e) {
+    vs[i] &= ~(0xffu << (8 * e));
+    if constexpr (D == 128) v[i][e] = 0;
+    else if constexpr (D == 64) v[i][e / 2] &= ~(0xffffu << (16 * (e % 2)));
+    else v[i][0] &= ~(0xffu << (8 * e));
+  }
+};
+template <int N> __device__ __forceinline__ void load_words(const uint8_t *p, uint32_t (&w)[N]) {
+  if constexpr (N == 4) {
+    const u32x4 x = *reinterpret_cast<const u32x4 *>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = x[i];
+  } else if constexpr (N == 2) {
+    const u32x2 x = *reinterpret_cast<const u32x2 *>(p);
+    w[0] = x[0], w[1] = x[1];
+  } else {
+    w[0] = *reinterpret_cast<const uint32_t *>(p);
+  }
+}
+
+// The 64-key chunks that rows at positions lo .. hi see: the first tokens', then the
+// window's.
+struct Chunks {
+  int sink, low, count;
+  __device__ __forceinline__ Chunks(const CachedArgs &a, int lo, int hi) {
+    const int from = max(0, lo - a.window + 1);  // (window INT_MAX: 0)
+    low = from / CHUNK;
+    sink = min((min(a.sinks, from) + CHUNK - 1) / CHUNK, low);
+    count = hi < 0 ? 0 : sink + hi / CHUNK + 1 - low;
+  }
+  __device__ __forceinline__ int at(int n) const { return (n < sink ? n : low + n - sink) * CHUNK; }
+};
+
+template <typename TI, int D, int PASS, int CALIB, int RECON>
+__global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
+  constexpr int NP = Pieces<TI>::N, N = D / 32, NT = D / 16;
+  constexpr bool VALUES = PASS != PASS_EXTREMA;
+  __shared__ float red[NWAVE][16][2];
+  __shared__ __attribute__((aligned(16))) float rows[VALUES ? NWAVE * 16 * (D + 4) : 4];
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, kb = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // (slices fastest: the workgroups of one key head's rows share an XCD's L2 where
+  // their number is a multiple of 8)
+  const int kvs = a.B * a.Hkv, s = blockIdx.x % kvs, b = s / a.Hkv, hk = s % a.Hkv;
+  const int tile = (int)(blockIdx.x / kvs) % a.tiles, split = blockIdx.x / (kvs * a.tiles);
+  const int G = a.H / a.Hkv, total = a.T * G;
+  const int n = (int)min((int64_t)max(a.lengths[b], 0), (int64_t)a.width << a.lpage);
+  // this lane's row, and its position (-1 or less: before the text, sees nothing)
+  const int r = min(tile * 16 + col, total - 1), t = r / G, h = hk * G + r % G;
+  const int pos = n - a.T + t;
+  const int lo = n - a.T + tile * 16 / G, hi = n - a.T + min(tile * 16 + 15, total - 1) / G;
+  const Chunks chunks(a, max(lo, 0), hi);
+  const int c0 = (int)((int64_t)chunks.count * split / a.splits);
+  const int c1 = (int)((int64_t)chunks.count * (split + 1) / a.splits);
+
+  bf16x8 q[NP][N];
+  {
+    const TI *p = slice_of<TI>(a.q, b, h) + t * a.q.st + kb * (D / 4);
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+      if constexpr (NP == 1) {
+        q[0][c] = as_op(*reinterpret_cast<const u32x4 *>(p + 8 * c));
+      } else {
+        float x[8];
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const f32x4 v = load4(p + 8 * c + 4 * g);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[4 * g + e] = v[e];
+        }
+        bf16x8 y[3];
+        to_pieces<3>(x, y);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) q[i][c] = y[i];
+      }
+    }
+  }
+
+  const int codes = D / 2 << a.lpage;
+  const int64_t block = (int64_t)codes + (D / 32 << a.lpage);  // bytes of a head's block
+  auto load = [&](int j, Stage4<D, VALUES> &x) {
+    x.ok = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int key = j + 16 * i, at = key >> a.lpage;
+      int page = at < a.width ? a.table[(int64_t)b * a.width + at] : -1;
+      page = __builtin_amdgcn_readfirstlane(page);
+      const bool ok = page >= 0 && page < a.pages;
+      x.ok |= ok << i;
+      const uint8_t *kp = a.cache + cache_block<D>(ok ? page : 0, 0, hk, a.Hkv, a.lpage);
+      const int tok = key & ((1 << a.lpage) - 1);
+      load_words<N>(kp + (tok + col) * (D / 2) + kb * (D / 8), x.k[i]);
+      x.ks[i] = kp[codes + (tok + col) * (D / 32) + kb * (D / 4) / 32];
+      if constexpr (VALUES) {
+        const uint8_t *vp = kp + a.Hkv * block;
+        load_words<N>(vp + tok * (D / 2) + lane * (D / 8), x.v[i]);
+        x.vs[i] = *reinterpret_cast<const uint32_t *>(vp + codes + tok * (D / 32) + kb * (D / 8) +
+                                                      col * (D / 16) / 32 * 4);
+      }
+    }
+  };
+
+  // the row's grid, from the extrema that the first pass left
+  RowConst rc{};
+  float Mx = -INFINITY, Mn = INFINITY;
+  if constexpr (PASS == PASS_GRID) {
+    const float *e = a.ext + ((int64_t)(s * a.tiles + tile) * a.splits * 16 + col) * 2;
+    for (int i = 0; i < a.splits; ++i) {
+      Mx = fmaxf(Mx, e[32 * i]);
+      Mn = fminf(Mn, e[32 * i + 1]);
+    }
+    Mx *= a.scale, Mn *= a.scale;
+    rc = row_const(Mx, Mn, a.K, CALIB, a.tau, a.scale);
+  }
+  const float Kf = (float)a.K, edge = 2.f * Kf - 1.f, span = 1.f - rc.emh;
+  const float c2 = a.scale * 1.44269504f;
+
+  f32x4 o[VALUES ? NT : 1] = {};
+  float m = -INFINITY, l = 0.f, low = INFINITY;  // (extrema: m and low)
+  Stage4<D, VALUES> cur, nxt;
+  int c = c0 + wave;
+  if (c < c1) load(chunks.at(c), cur);
+  for (; c < c1; c += NWAVE) {
+    const int j = chunks.at(c);
+    if (c + NWAVE < c1) load(chunks.at(c + NWAVE), nxt);
+    // every row of the tile sees every key of the chunk
+    const bool all = j + CHUNK - 1 <= lo && cur.ok == 15 &&
+                     ((int64_t)hi - j < a.window || j + CHUNK - 1 < a.sinks);
+    auto sees = [&](int key, int i) {
+      return key <= pos && ((int64_t)pos - key < a.window || key < a.sinks) && (cur.ok >> i & 1);
+    };
+    // groups that hold an infinity or NaN
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      bad |= cur.ks[i] == 255;
+      if constexpr (VALUES) {
+        const uint32_t y = ~cur.vs[i];
+        bad |= ((y - 0x01010101u) & ~y & 0x80808080u) != 0;
+      }
+    }
+    bad = __any(bad);
+    float S[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float f = scale_of(cur.ks[i]);
+      f32x4 acc = {};
+      u32x4 w[N];
+#pragma unroll
+      for (int x = 0; x < N; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[x][e] = pair_at(e, cur.k[i][x], f);
+#pragma unroll
+      for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+        for (int x = 0; x < N; ++x) acc = mma16(as_op(w[x]), q[p][x], acc);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) S[i][e] = acc[e];
+    }
+    if (__builtin_expect(bad, 0)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint64_t y = __ballot(cur.ks[i] == 255);
+        y |= y >> 32;
+        y |= y >> 16;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[i][e] = y >> (4 * kb + e) & 1 ? NAN : S[i][e];
+      }
+    }
+    if (!all) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          S[i][e] = sees(j + 16 * i + 4 * kb + e, i) ? S[i][e] : -INFINITY;
+    }
+    if constexpr (PASS == PASS_EXTREMA) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          m = fmaxf(m, S[i][e]);
+          const bool in = all || sees(j + 16 * i + 4 * kb + e, i);
+          if constexpr (CALIB != CAL_FWM) low = in ? fminf(low, S[i][e]) : low;
+        }
+    } else {
+      float w[4][4];
+      if constexpr (PASS == PASS_SOFTMAX) {
+        float top = S[0][0];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top = fmaxf(top, S[i][e]);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        // (moved, and the sums scaled, only when passed by 2^8, row by row: no row's bits
+        // depend on another's)
+        const bool up = (top - m) * c2 > 8.f;
+        if (__any(up)) {
+          const float f = up ? __builtin_amdgcn_exp2f((m - top) * c2) : 1.f;
+          m = up ? top : m;
+          l *= f;
+#pragma unroll
+          for (int x = 0; x < NT; ++x) o[x] *= f;
+        }
+        const float mm = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[i][e] = __builtin_amdgcn_exp2f((S[i][e] - mm) * c2);
+      } else {
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            w[i][e] = fmaf(S[i][e], rc.alpha, rc.beta);
+            any |= is_ambiguous<CALIB>(w[i][e], rc.margin2, edge);
+          }
+        if (__any(any)) {
+          // keys within rounding of a boundary: decided in 64 bits
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const bool amb = is_ambiguous<CALIB>(w[i][e], rc.margin2, edge);
+              if (!__any(amb)) continue;
+              const float x = 0.5f * exact_v2<CALIB>(S[i][e] * a.scale, 2.f * w[i][e], Mx, Mn, a.K, a.tau);
+              w[i][e] = amb ? x : w[i][e];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const KeyDec k = key_of<CALIB>(w[i][e], Kf);
+            const float up = grid_upper(k.rf, rc);
+            float x;
+            if constexpr (RECON == REC_NEAREST) x = k.up ? up : up * rc.emh;
+            else x = up * fmaf(k.t, span, rc.emh);
+            x = k.tail ? 0.f : x;
+            // an infinite or NaN score makes its row NaN
+            x = fabsf(S[i][e]) < INFINITY ? x : NAN;
+            w[i][e] = x;
+          }
+        if (!all) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              w[i][e] = sees(j + 16 * i + 4 * kb + e, i) ? w[i][e] : 0.f;
+        }
+      }
+      if (!all) {
+        // values of tokens that no row sees (past the end, on no page) as zeros
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (j + 16 * i + 4 * kb + e > hi || !(cur.ok >> i & 1)) cur.clear(i, e);
+      }
+      if (__builtin_expect(bad, 0)) {
+        // groups of NaN: their values as zeros here, and NaN for the rows that see them
+        bf16x8 is[2], one[2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const bool nan = (cur.vs[i] >> (8 * e) & 255) == 255;
+            if (nan) cur.clear(i, e);
+            is[i / 2][i % 2 * 4 + e] = (__bf16)(nan ? 1.f : 0.f);
+            one[i / 2][i % 2 * 4 + e] = (__bf16)(sees(j + 16 * i + 4 * kb + e, i) ? 1.f : 0.f);
+          }
+        // (column `col` of the values here is row 4 kb + e of the sums)
+        const f32x4 k = mma16(is[1], one[1], mma16(is[0], one[0], f32x4{}));
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int x = 0; x < NT; ++x) o[x][e] = k[e] > 0.f ? NAN : o[x][e];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) l += (w[i][0] + w[i][1]) + (w[i][2] + w[i][3]);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        // the weights of the lane's eight keys of 32, and those keys' values
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = w[2 * u + e / 4][e % 4];
+        bf16x8 p[NP];
+        to_pieces<NP>(x, p);
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = scale_of(cur.vs[2 * u + e / 4] >> (8 * (e % 4)) & 255);
+#pragma unroll
+        for (int y = 0; y < NT / 2; ++y) {
+          uint32_t z[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int i = 2 * u + e / 4, k = e % 4;
+            z[e] = pair_at(D == 128 ? y : D == 64 ? 2 * (k % 2) + y : k,
+                           cur.v[i][D == 128 ? k : D == 64 ? k / 2 : 0], f[e]);
+          }
+          u32x4 even, odd;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            even[e] = __builtin_amdgcn_perm(z[2 * e + 1], z[2 * e], 0x05040100u);
+            odd[e] = __builtin_amdgcn_perm(z[2 * e + 1], z[2 * e], 0x07060302u);
+          }
+#pragma unroll
+          for (int i = NP - 1; i >= 0; --i) {
+            o[2 * y] = mma16(as_op(even), p[i], o[2 * y]);
+            o[2 * y + 1] = mma16(as_op(odd), p[i], o[2 * y + 1]);
+          }
+        }
+      }
+    }
+    cur = nxt;
+  }
+
+  const int64_t out = ((int64_t)(s * a.tiles + tile) * a.splits + split) * 16;
+  if constexpr (PASS == PASS_EXTREMA) {
+    m = fmaxf(m, __shfl_xor(m, 16));
+    m = fmaxf(m, __shfl_xor(m, 32));
+    low = fminf(low, __shfl_xor(low, 16));
+    low = fminf(low, __shfl_xor(low, 32));
+    if (kb == 0) red[wave][col][0] = m, red[wave][col][1] = low;
+    __syncthreads();
+    if (tid < 16) {
+#pragma unroll
+      for (int i = 1; i < NWAVE; ++i) {
+        m = fmaxf(m, red[i][col][0]);
+        low = fminf(low, red[i][col][1]);
+      }
+      a.ext[(out + col) * 2] = m;
+      a.ext[(out + col) * 2 + 1] = low;
+    }
+  } else {
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (kb == 0) red[wave][col][0] = m, red[wave][col][1] = l;
+    // channel (4 kb + e) NT + x of row `col`
+    float *mine = rows + (wave * 16 + col) * (D + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int x = 0; x < NT; ++x) mine[(4 * kb + e) * NT + x] = o[x][e];
+    __syncthreads();
+    // joined in wave order: 256 threads, 16 rows, D / 16 channels each
+    const int row = tid / 16, part = tid % 16;
+    float top = 0.f;
+    if constexpr (PASS == PASS_SOFTMAX) {
+      top = red[0][row][0];
+#pragma unroll
+      for (int i = 1; i < NWAVE; ++i) top = fmaxf(top, red[i][row][0]);
+      if (top == -INFINITY) top = 0.f;
+    }
+    float sum = 0.f, x[NT] = {};
+#pragma unroll
+    for (int i = 0; i < NWAVE; ++i) {
+      const float f = PASS == PASS_SOFTMAX ? __builtin_amdgcn_exp2f((red[i][row][0] - top) * c2) : 1.f;
+      sum = fmaf(red[i][row][1], f, sum);
+#pragma unroll
+      for (int e = 0; e < NT; ++e)
+        x[e] = fmaf(rows[(i * 16 + row) * (D + 4) + part * NT + e], f, x[e]);
+    }
+    if (a.splits == 1) {
+      const int rr = tile * 16 + row;
+      if (rr < total) {
+        const float f = sum == 0.f ? 0.f : 1.f / sum;
+        TI *y = slice_of<TI>(a.o, b, hk * G + rr % G) + rr / G * a.o.st + part * NT;
+#pragma unroll
+        for (int e = 0; e < NT; ++e) {
+          if constexpr (sizeof(TI) == 4) y[e] = x[e] * f;
+          else y[e] = (uint16_t)cvt_bf16x2(x[e] * f, 0.f);
+        }
+      }
+    } else {
+      float *y = a.part + (out + row) * D + part * NT;
+#pragma unroll
+      for (int e = 0; e < NT; ++e) y[e] = x[e];
+      if (part == 0) {
+        a.stat[(out + row) * 2] = PASS == PASS_SOFTMAX ? top : 0.f;
+        a.stat[(out + row) * 2 + 1] = sum;
+      }
+    }
+  }
+}
+
+// The parts of a row tile, joined in order of their keys.
+template <typename TI, int D> __global__ __launch_bounds__(256) void join_kernel(CachedArgs a) {
+  constexpr int NT = D / 16;
+  const int kvs = a.B * a.Hkv, s = blockIdx.x % kvs, b = s / a.Hkv, hk = s % a.Hkv;
+  const int tile = blockIdx.x / kvs, row = threadIdx.x / 16, part = threadIdx.x % 16;
+  const int G = a.H / a.Hkv, r = tile * 16 + row;
+  if (r >= a.T * G) return;
+  const int64_t first = (int64_t)(s * a.tiles + tile) * a.splits * 16 + row;
+  const float *st = a.stat + first * 2, *p = a.part + first * D + part * NT;
+  float top = -INFINITY;
+  for (int i = 0; i < a.splits; ++i)
+    if (st[32 * i + 1] != 0.f) top = fmaxf(top, st[32 * i]);  // (parts that saw a key)
+  const float c2 = a.scale * 1.44269504f;
+  float sum = 0.f, x[NT] = {};
+  for (int i = 0; i < a.splits; ++i) {
+    if (st[32 * i + 1] == 0.f) continue;
+    const float f = __builtin_amdgcn_exp2f((st[32 * i] - top) * c2);
+    sum = fmaf(st[32 * i + 1], f, sum);
+#pragma unroll
+    for (int e = 0; e < NT; ++e) x[e] = fmaf(p[(int64_t)i * 16 * D + e], f, x[e]);
+  }
+  const float f = sum == 0.f ? 0.f : 1.f / sum;
+  TI *y = slice_of<TI>(a.o, b, hk * G + r % G) + r / G * a.o.st + part * NT;
+#pragma unroll
+  for (int e = 0; e < NT; ++e) {
+    if constexpr (sizeof(TI) == 4) y[e] = x[e] * f;
+    else y[e] = (uint16_t)cvt_bf16x2(x[e] * f, 0.f);
+  }
+}
+
+template <typename TI, int D, int CALIB> void grid_passes(const CachedArgs &a, dim3 g, hipStream_t s) {
+  const dim3 t(64 * NWAVE);
+  timed_call("kia_cache4_extrema", s, [&] {
+    hipLaunchKernelGGL((cached_kernel<TI, D, PASS_EXTREMA, CALIB, REC_LERP>), g, t, 0, s, a);
+  });
+  timed_call("kia_cache4_attn", s, [&] {
+    if (a.recon == REC_LERP)
+      hipLaunchKernelGGL((cached_kernel<TI, D, PASS_GRID, CALIB, REC_LERP>), g, t, 0, s, a);
+    else
+      hipLaunchKernelGGL((cached_kernel<TI, D, PASS_GRID, CALIB, REC_NEAREST>), g, t, 0, s, a);
+  });
+}
+
+template <typename TI, int D> void run(const CachedArgs &a, hipStream_t s) {
+  const dim3 g((unsigned)(a.B * a.Hkv) * a.tiles * a.splits);
+  if (a.recon == REC_SOFTMAX) {
+    timed_call("kia_cache4_attn", s, [&] {
+      hipLaunchKernelGGL((cached_kernel<TI, D, PASS_SOFTMAX, CAL_FWM, REC_SOFTMAX>), g,
+                         dim3(64 * NWAVE), 0, s, a);
+    });
+  } else if (a.calib == CAL_MINMAX) {
+    grid_passes<TI, D, CAL_MINMAX>(a, g, s);
+  } else if (a.calib == CAL_FWM) {
+    grid_passes<TI, D, CAL_FWM>(a, g, s);
+  } else {
+    grid_passes<TI, D, CAL_RESOLVED>(a, g, s);
+  }
+  if (a.splits > 1) {
+    timed_call("kia_cache4_join", s, [&] {
+      hipLaunchKernelGGL((join_kernel<TI, D>), dim3((unsigned)(a.B * a.Hkv) * a.tiles), dim3(256), 0,
+                         s, a);
+    });
+  }
+}
+
+}  // namespace
+
+template <> void launch_cached<KIA_HEAD>(const CachedArgs &a, int dtype, hipStream_t s) {
+  if (dtype == KIA_F32) run<float, KIA_HEAD>(a, s);
+  else run<uint16_t, KIA_HEAD>(a, s);
+}
+
+}  // namespace kia

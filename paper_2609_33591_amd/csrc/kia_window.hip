@@ -1,0 +1,679 @@
+// kia_window.hip -- softmax attention with a sliding window and visible first
+// tokens on gfx950, forward and backward, for one head dimension (KIA_HEAD).
+//
+// Query i sees key j iff j <= i and (i - j < window or j < sinks). With
+// s = q.k / sqrt(d):
+//   O_i = sum_j p_ij v_j, p_ij = e^{s_ij - lse_i}, lse_i = ln sum_j e^{s_ij};
+//   D_i = dO_i . O_i, dS_ij = p_ij (dO_i . v_j - D_i);
+//   dQ = dS K / sqrt(d), dK = dS^T Q / sqrt(d), dV = P^T dO.
+// Query heads h share the key head h / (H / Hkv).
+//
+// Every kernel has the same shape: a wave keeps 32 rows of one side in registers
+// (queries; for dK and dV keys) as the B operand, rows of the other side stream
+// through LDS, and a 32x32 block of scores is formed with the streamed rows along
+// the registers, so that its weights are the B operand of the next product as they
+// stand (krel()) and the streamed rows are its A operand, by columns. Row sums and
+// maxima of a query are then one lane's (and its partner's, 32 lanes on).
+//
+// bf16 runs on v_mfma_f32_32x32x16_bf16; the weights p and dS, the products'
+// computed operands, are rounded to bf16 (2^-8 of each), all sums and statistics are
+// fp32. fp32 runs on v_mfma_f32_32x32x2_f32 throughout and rounds nothing.
+//
+// A key that a query does not see has no influence on it, whatever it holds: its
+// score is replaced before it is used, and in blocks where some pair is masked, rows
+// that hold infinities or NaNs take part with those values as zeros, and add them
+// only to the rows that see them (mul_rows, `bad`).
+#include <type_traits>
+
+#include "kia_around.hpp"
+#include "kia_host.hpp"
+
+namespace kia {
+namespace {
+
+constexpr float LOG2E_F = 1.44269504f, LN2_F = 0.69314718f;
+
+template <typename TI> constexpr bool is_f32 = sizeof(TI) == 4;
+
+// ---- rows in LDS ---------------------------------------------------------------
+// A [ROWS, D] block of rows of any stride, rows at or past `end` as zeros. The row
+// stride in LDS is D plus 16 bytes: 16-byte reads of eight rows fall in distinct banks.
+template <typename TI, int D, int ROWS, int NT> struct Rows {
+  static constexpr int V = 16 / sizeof(TI), RS = D + V, SIZE = ROWS * RS;
+  static constexpr int PER = ROWS * D / V, PF = (PER + NT - 1) / NT, RPP = NT * V / D;
+  static_assert(PER % NT == 0 || PF == 1, "whole passes");
+  u32x4 x[PF];
+  __device__ __forceinline__ void fetch(const TI *slice, int64_t st, int r0, int end, int tid) {
+    const int rows = min(ROWS, end - r0);
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<TI *>(slice) + (rows > 0 ? r0 : 0) * st, (short)0,
+        rows > 0 ? ((rows - 1) * (int)st + D) * (int)sizeof(TI) : 0, 0x00020000);
+    const uint32_t row = tid / (D / V) * (uint32_t)st;
+    const uint32_t off = PER % NT == 0 || tid < PER
+                             ? (row + tid % (D / V) * V) * (uint32_t)sizeof(TI)
+                             : 0x80000000u;
+    const uint32_t step = RPP * (uint32_t)st * (uint32_t)sizeof(TI);
+#pragma unroll
+    for (int e = 0; e < PF; ++e)
+      x[e] = __builtin_bit_cast(u32x4,
+                                __builtin_amdgcn_raw_buffer_load_b128(rs, off + e * step, 0, 0));
+  }
+  __device__ __forceinline__ void stash(TI *dst, int tid) const {
+    if (PER % NT != 0 && tid >= PER) return;
+#pragma unroll
+    for (int e = 0; e < PF; ++e) {
+      const int i = tid + NT * e;
+      *reinterpret_cast<u32x4 *>(dst + i / (D / V) * RS + i % (D / V) * V) = x[e];
+    }
+  }
+  // whether any of the thread's values is infinite or NaN
+  __device__ __forceinline__ bool bad() const {
+    bool b = false;
+#pragma unroll
+    for (int e = 0; e < PF; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (is_f32<TI>) {
+          b |= (x[e][i] & 0x7f800000u) == 0x7f800000u;
+        } else {
+          b |= (x[e][i] & 0x7f800000u) == 0x7f800000u;
+          b |= (x[e][i] & 0x00007f80u) == 0x00007f80u;
+        }
+      }
+    return b;
+  }
+};
+
+// ---- 32 rows in registers -------------------------------------------------------
+// Lane l holds of row l % 32 what its half of the matrix instructions takes: bf16,
+// channels 16 s + 8 (l / 32) + e; fp32, channels 8 c + 4 (l / 32) + e.
+template <typename TI, int D> struct RowReg {
+  bf16x8 v[D / 16];
+  __device__ __forceinline__ void load(const uint16_t *row, int half, bool ok) {
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      u32x4 x = *reinterpret_cast<const u32x4 *>(row + 16 * s + 8 * half);
+      if (!ok) x = u32x4{0, 0, 0, 0};
+      v[s] = as_op(x);
+    }
+  }
+  __device__ __forceinline__ float dot(const RowReg &o) const {
+    float sum = 0.f;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fmaf((float)v[s][e], (float)o.v[s][e], sum);
+    return sum;
+  }
+};
+template <int D> struct RowReg<float, D> {
+  float v[D / 2];
+  __device__ __forceinline__ void load(const float *row, int half, bool ok) {
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c) {
+      const f32x4 x = *reinterpret_cast<const f32x4 *>(row + 8 * c + 4 * half);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * c + e] = ok ? x[e] : 0.f;
+    }
+  }
+  __device__ __forceinline__ float dot(const RowReg &o) const {
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < D / 2; ++e) sum = fmaf(v[e], o.v[e], sum);
+    return sum;
+  }
+};
+
+// Products of 32 streamed rows (at `t`, row stride RS) with the 32 rows of b:
+// register r of lane l is the pair (streamed row krel(r, l / 32), row l % 32 of b).
+template <int D, int RS>
+__device__ __forceinline__ f32x16 dots(const uint16_t *t, const RowReg<uint16_t, D> &b, int lane) {
+  f32x16 c = {};
+  const uint16_t *p = t + (lane & 31) * RS + 8 * (lane >> 5);
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) c = mfma16(row_op(p + 16 * s), b.v[s], c);
+  return c;
+}
+template <int D, int RS>
+__device__ __forceinline__ f32x16 dots(const float *t, const RowReg<float, D> &b, int lane) {
+  f32x16 c = {};
+  const float *p = t + (lane & 31) * RS + 4 * (lane >> 5);
+#pragma unroll
+  for (int s = 0; s < D / 8; ++s) {
+    const f32x4 x = *reinterpret_cast<const f32x4 *>(p + 8 * s);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = mfma32(x[e], b.v[4 * s + e], c);
+  }
+  return c;
+}
+
+// A value with what is infinite or NaN in it as 0, and a count of the latter: 1 for
+// +inf, 2^7 for -inf, 2^14 for NaN (sums over 32 rows stay apart, and exact in bf16
+// products with fp32 sums).
+__device__ __forceinline__ float count_of(float x) {
+  return fabsf(x) < INFINITY ? 0.f : x == INFINITY ? 1.f : x == -INFINITY ? 128.f : 16384.f;
+}
+// what such a count adds to a sum
+__device__ __forceinline__ float sum_of(float n) {
+  const int k = (int)n;
+  const bool nan = k >= 16384 || ((k & 127) && k >= 128);
+  return nan ? NAN : k >= 128 ? -INFINITY : k ? INFINITY : 0.f;
+}
+
+// acc[c][channel][row of b's side] += sum over the 32 streamed rows of their
+// channels 32 c .. times the weights w (register r: streamed row krel(r, half)).
+// `bad`: the rows hold infinities or NaNs; see(r) tells whether the pair of register
+// r is one that counts.
+template <int D, int RS, int NC, class See>
+__device__ __forceinline__ void mul_rows(f32x16 (&acc)[NC], const uint16_t *t, const float (&w)[16],
+                                         int lane, bool bad, See see) {
+  const uint16_t *p = t + tr_base<D, RS>(lane);
+  if (!__builtin_expect(bad, 0)) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      u32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = cvt_bf16x2(w[8 * s + 2 * e], w[8 * s + 2 * e + 1]);
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        acc[c] = mfma16(tr_op<RS>(p + 16 * s * RS + 32 * c), as_op(x), acc[c]);
+    }
+    return;
+  }
+  bf16x8 x[2], one[2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x[s][e] = (__bf16)w[8 * s + e];
+      one[s][e] = (__bf16)(see(8 * s + e) ? 1.f : 0.f);
+    }
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    f32x16 n = {};
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const bf16x8 y = tr_op<RS>(p + 16 * s * RS + 32 * c);
+      bf16x8 f, k;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float v = (float)y[e];
+        f[e] = fabsf(v) < INFINITY ? y[e] : (__bf16)0.f;
+        k[e] = (__bf16)count_of(v);
+      }
+      acc[c] = mfma16(f, x[s], acc[c]);
+      n = mfma16(k, one[s], n);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[c][r] += sum_of(n[r]);
+  }
+}
+template <int D, int RS, int NC, class See>
+__device__ __forceinline__ void mul_rows(f32x16 (&acc)[NC], const float *t, const float (&w)[16],
+                                         int lane, bool bad, See see) {
+  const float *p = t + 4 * (lane >> 5) * RS + (lane & 31) % D;
+  if (!__builtin_expect(bad, 0)) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) acc[c] = mfma32(p[krel0(r) * RS + 32 * c], w[r], acc[c]);
+    return;
+  }
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    f32x16 n = {};
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float v = p[krel0(r) * RS + 32 * c];
+      acc[c] = mfma32(fabsf(v) < INFINITY ? v : 0.f, w[r], acc[c]);
+      n = mfma32(count_of(v), see(r) ? 1.f : 0.f, n);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[c][r] += sum_of(n[r]);
+  }
+}
+
+// One lane's row from accumulators (register r of block c: channel
+// 32 c + 8 (r / 4) + 4 half + r % 4), times f.
+template <int D, int NC>
+__device__ __forceinline__ void store_row(float *row, const f32x16 (&acc)[NC], int half, float f) {
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int g = 0; g < (D < 32 ? D / 8 : 4); ++g) {
+      const f32x4 x = {acc[c][4 * g] * f, acc[c][4 * g + 1] * f, acc[c][4 * g + 2] * f,
+                       acc[c][4 * g + 3] * f};
+      *reinterpret_cast<f32x4 *>(row + 32 * c + 8 * g + 4 * half) = x;
+    }
+}
+template <int D, int NC>
+__device__ __forceinline__ void store_row(uint16_t *row, const f32x16 (&acc)[NC], int half,
+                                          float f) {
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int g = 0; g < (D < 32 ? D / 8 : 4); ++g) {
+      const u32x2 x = {cvt_bf16x2(acc[c][4 * g] * f, acc[c][4 * g + 1] * f),
+                       cvt_bf16x2(acc[c][4 * g + 2] * f, acc[c][4 * g + 3] * f)};
+      *reinterpret_cast<u32x2 *>(row + 32 * c + 8 * g + 4 * half) = x;
+    }
+}
+
+template <int NC> __device__ __forceinline__ void clear(f32x16 (&acc)[NC]) {
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[c][r] = 0.f;
+}
+
+__device__ __forceinline__ int length_of(const WinArgs &a, int b) {
+  return a.lengths ? max(0, min(a.lengths[b], a.T)) : a.T;
+}
+__device__ __forceinline__ bool sees(const WinArgs &a, int i, int j) {
+  return j <= i && (i - j < a.window || j < a.sinks);
+}
+// whether some pair, every pair, of queries i .. i + ni - 1 and keys j .. j + nj - 1 counts
+__device__ __forceinline__ bool sees_some(const WinArgs &a, int i, int ni, int j, int nj) {
+  return j <= i + ni - 1 && (i - (j + nj - 1) < a.window || j < a.sinks);
+}
+__device__ __forceinline__ bool sees_all(const WinArgs &a, int i, int ni, int j, int nj) {
+  return j + nj - 1 <= i && (i + ni - 1 - j < a.window || j + nj - 1 < a.sinks);
+}
+
+// The key tiles of KT keys that queries i0 .. i1 - 1 see: the first tokens', then the
+// window's.
+template <int KT> struct KeyTiles {
+  int sink, low, count;
+  __device__ __forceinline__ KeyTiles(const WinArgs &a, int i0, int i1) {
+    const int lo = max(0, i0 - a.window + 1);
+    low = lo / KT;
+    sink = min((min(a.sinks, lo) + KT - 1) / KT, low);
+    count = sink + (i1 - 1) / KT + 1 - low;
+  }
+  __device__ __forceinline__ int at(int n) const { return (n < sink ? n : low + n - sink) * KT; }
+};
+
+template <typename TI, int D, int NW> struct FwdCfg {
+  static constexpr int KT = is_f32<TI> ? 32 : 64, NT = 64 * NW;
+  using R = Rows<TI, D, KT, NT>;
+};
+
+// One workgroup: NW groups of 32 queries of one head, over the key tiles that any of
+// them sees. Keys and values of the next tile are fetched into registers while a tile
+// is worked on, and stored to the other of two buffers: one barrier a tile.
+// The running maximum of a row moves (and its sums are scaled) only when a score
+// passes it by 2^8: sums of weights up to 2^8 lose nothing in fp32.
+template <typename TI, int D, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void win_fwd_kernel(WinArgs a) {
+  using C = FwdCfg<TI, D, NW>;
+  using R = typename C::R;
+  constexpr int KT = C::KT, NT = C::NT, SUB = KT / 32, NC = D >= 32 ? D / 32 : 1, RS = R::RS;
+  __shared__ __attribute__((aligned(16))) TI smem[4 * R::SIZE + 32];
+  __shared__ int flag[2][NW];
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = a.H / a.Hkv, kvs = a.B * a.Hkv;
+  const int s = blockIdx.x % kvs, b = s / a.Hkv, hk = s % a.Hkv;
+  const int h = hk * G + (int)(blockIdx.x / kvs) % G;
+  const int nqb = (a.T + 32 * NW - 1) / (32 * NW);
+  const int i0 = (nqb - 1 - (int)(blockIdx.x / (kvs * G))) * 32 * NW;
+  const int n = length_of(a, b);
+  const int iw = i0 + 32 * wave, row = iw + l32;
+  TI *orow = slice_of<TI>(a.o, b, h) + row * a.o.st;
+  float *lse = a.lse + ((int64_t)b * a.H + h) * a.T;
+  f32x16 acc[NC];
+  clear(acc);
+  float m = -INFINITY, l = 0.f;
+  const float c2 = a.scale * LOG2E_F;
+  if (i0 < n) {
+    RowReg<TI, D> q;
+    q.load(slice_of<TI>(a.q, b, h) + min(row, n - 1) * a.q.st, half, row < n);
+    const KeyTiles<KT> tiles(a, i0, min(i0 + 32 * NW, n));
+    const TI *ks = slice_of<TI>(a.k, b, hk), *vs = slice_of<TI>(a.v, b, hk);
+    R fk, fv;
+    fk.fetch(ks, a.k.st, tiles.at(0), n, tid);
+    fv.fetch(vs, a.v.st, tiles.at(0), n, tid);
+    for (int p = 0; p < tiles.count; ++p) {
+      const int j = tiles.at(p);
+      TI *kb = smem + (p & 1) * 2 * R::SIZE, *vb = kb + R::SIZE;
+      fk.stash(kb, tid);
+      fv.stash(vb, tid);
+      const bool part = !sees_all(a, i0, 32 * NW, j, KT);
+      if (part) {
+        const bool bad = __any(fv.bad());
+        if (lane == 0) flag[p & 1][wave] = bad;
+      }
+      if (p + 1 < tiles.count) {
+        fk.fetch(ks, a.k.st, tiles.at(p + 1), n, tid);
+        fv.fetch(vs, a.v.st, tiles.at(p + 1), n, tid);
+      }
+      lds_barrier();
+      if (iw >= n || !sees_some(a, iw, 32, j, KT)) continue;
+      const bool bad = part && any_flag<NW>(flag[p & 1]);
+      f32x16 S[SUB];
+#pragma unroll
+      for (int u = 0; u < SUB; ++u) S[u] = dots<D, RS>(kb + 32 * u * RS, q, lane);
+      if (!sees_all(a, iw, 32, j, KT)) {
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            S[u][r] = sees(a, row, j + 32 * u + krel(r, half)) ? S[u][r] : -INFINITY;
+      }
+      float top = S[0][0];
+#pragma unroll
+      for (int u = 0; u < SUB; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, S[u][r]);
+      top = fmaxf(top, __shfl_xor(top, 32));
+      // (row by row: no row's bits depend on another's)
+      const bool up = (top - m) * c2 > 8.f;
+      if (__any(up)) {
+        const float f = up ? __builtin_amdgcn_exp2f((m - top) * c2) : 1.f;
+        m = up ? top : m;
+        l *= f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[c][r] *= f;
+      }
+      const float mm = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int u = 0; u < SUB; ++u) {
+        float w[16], sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          // (fp32: the difference first, so that the error is its own and not the score's)
+          if constexpr (is_f32<TI>) w[r] = __builtin_amdgcn_exp2f((S[u][r] - mm) * c2);
+          else w[r] = __builtin_amdgcn_exp2f(fmaf(S[u][r], c2, -mm * c2));
+          sum += w[r];
+        }
+        l += sum;
+        mul_rows<D, RS, NC>(acc, vb + 32 * u * RS, w, lane, bad, [&](int r) {
+          return sees(a, row, j + 32 * u + krel(r, half));
+        });
+      }
+    }
+  }
+  if (row >= a.T) return;
+  l += __shfl_xor(l, 32);
+  const bool none = l == 0.f || row >= n;
+  store_row<D, NC>(orow, acc, half, none ? 0.f : 1.f / l);
+  if (half == 0) lse[row] = none ? -INFINITY : fmaf(m, a.scale, logf(l));
+}
+
+// dQ, and D for the key gradients. The same walk as the forward's, with the scores
+// formed again and p from lse.
+template <typename TI, int D, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void win_dq_kernel(WinArgs a) {
+  using C = FwdCfg<TI, D, NW>;
+  using R = typename C::R;
+  constexpr int KT = C::KT, SUB = KT / 32, NC = D >= 32 ? D / 32 : 1, RS = R::RS;
+  __shared__ __attribute__((aligned(16))) TI smem[4 * R::SIZE + 32];
+  __shared__ int flag[2][NW];
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = a.H / a.Hkv, kvs = a.B * a.Hkv;
+  const int s = blockIdx.x % kvs, b = s / a.Hkv, hk = s % a.Hkv;
+  const int h = hk * G + (int)(blockIdx.x / kvs) % G;
+  const int nqb = (a.T + 32 * NW - 1) / (32 * NW);
+  const int i0 = (nqb - 1 - (int)(blockIdx.x / (kvs * G))) * 32 * NW;
+  const int n = length_of(a, b);
+  const int iw = i0 + 32 * wave, row = iw + l32;
+  TI *dqrow = slice_of<TI>(a.dq, b, h) + row * a.dq.st;
+  f32x16 acc[NC];
+  clear(acc);
+  if (i0 < n) {
+    RowReg<TI, D> q, g;
+    const int at = min(row, n - 1);
+    q.load(slice_of<TI>(a.q, b, h) + at * a.q.st, half, row < n);
+    g.load(slice_of<TI>(a.dO, b, h) + at * a.dO.st, half, row < n);
+    float lse, delta;
+    {
+      RowReg<TI, D> o;
+      o.load(slice_of<TI>(a.o, b, h) + at * a.o.st, half, row < n);
+      delta = g.dot(o);
+      delta += __shfl_xor(delta, 32);
+      const int64_t r = ((int64_t)b * a.H + h) * a.T;
+      lse = row < n ? a.lse[r + row] : INFINITY;
+      if (lse == -INFINITY) lse = INFINITY;  // a row of nothing: no weight anywhere
+      if (half == 0 && row < n) a.delta[r + row] = delta;
+    }
+    const float c2 = a.scale * LOG2E_F, lse2 = lse * LOG2E_F;
+    const KeyTiles<KT> tiles(a, i0, min(i0 + 32 * NW, n));
+    const TI *ks = slice_of<TI>(a.k, b, hk), *vs = slice_of<TI>(a.v, b, hk);
+    R fk, fv;
+    fk.fetch(ks, a.k.st, tiles.at(0), n, tid);
+    fv.fetch(vs, a.v.st, tiles.at(0), n, tid);
+    for (int p = 0; p < tiles.count; ++p) {
+      const int j = tiles.at(p);
+      TI *kb = smem + (p & 1) * 2 * R::SIZE, *vb = kb + R::SIZE;
+      fk.stash(kb, tid);
+      fv.stash(vb, tid);
+      const bool part = !sees_all(a, i0, 32 * NW, j, KT);
+      if (part) {
+        const bool bad = __any(fk.bad());
+        if (lane == 0) flag[p & 1][wave] = bad;
+      }
+      if (p + 1 < tiles.count) {
+        fk.fetch(ks, a.k.st, tiles.at(p + 1), n, tid);
+        fv.fetch(vs, a.v.st, tiles.at(p + 1), n, tid);
+      }
+      lds_barrier();
+      if (iw >= n || !sees_some(a, iw, 32, j, KT)) continue;
+      const bool bad = part && any_flag<NW>(flag[p & 1]);
+      const bool all = sees_all(a, iw, 32, j, KT);
+#pragma unroll
+      for (int u = 0; u < SUB; ++u) {
+        const f32x16 S = dots<D, RS>(kb + 32 * u * RS, q, lane);
+        const f32x16 P = dots<D, RS>(vb + 32 * u * RS, g, lane);
+        float w[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float e = is_f32<TI> ? fmaf(S[r], a.scale, -lse) * LOG2E_F : fmaf(S[r], c2, -lse2);
+          w[r] = __builtin_amdgcn_exp2f(e) * (P[r] - delta);
+        }
+        if (!all) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            w[r] = sees(a, row, j + 32 * u + krel(r, half)) ? w[r] : 0.f;
+        }
+        mul_rows<D, RS, NC>(acc, kb + 32 * u * RS, w, lane, bad, [&](int r) {
+          return sees(a, row, j + 32 * u + krel(r, half));
+        });
+      }
+    }
+  }
+  if (row < a.T) store_row<D, NC>(dqrow, acc, half, row < n ? a.scale : 0.f);
+}
+
+// The key block, the part of its query range and the number of parts of a workgroup.
+struct KeyPart {
+  int kb, part, parts, slot;  // slot: of its partial sums, -1 if it leaves none
+  __device__ __forceinline__ KeyPart(const WinArgs &a, int y) {
+    const int first = a.sink_blocks * a.parts_a;
+    const bool A = y < first;
+    parts = A ? a.parts_a : a.parts_b;
+    const int z = A ? y : y - first;
+    kb = (A ? 0 : a.sink_blocks) + z / parts;
+    part = z % parts;
+    slot = parts == 1 ? -1 : z + (!A && a.parts_a > 1 ? first : 0);
+  }
+};
+
+// dK and dV. One workgroup: 128 keys of one key head, 32 to a wave, over a part of the
+// 32-query tiles that see any of them, of every query head that shares the key head.
+// Blocks whose tiles are many (those of the first tokens, which every query sees) are
+// cut into parts, whose sums win_sum_kernel adds in order: no atomics, so that the
+// gradients repeat bit for bit.
+template <typename TI, int D>
+__global__ __launch_bounds__(256, is_f32<TI> && D == 128 ? 1 : 2) void win_dkv_kernel(WinArgs a) {
+  constexpr int NT = 256, NC = D >= 32 ? D / 32 : 1;
+  using R = Rows<TI, D, WIN_QT, NT>;
+  constexpr int RS = R::RS;
+  __shared__ __attribute__((aligned(16))) TI smem[4 * R::SIZE + 32];
+  __shared__ __attribute__((aligned(16))) float stat[2][2][WIN_QT];
+  __shared__ int flag[2][4];
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = a.H / a.Hkv, kvs = a.B * a.Hkv;
+  const int s = blockIdx.x % kvs, b = s / a.Hkv, hk = s % a.Hkv;
+  const KeyPart kp(a, blockIdx.x / kvs);
+  const int n = length_of(a, b);
+  const int j0 = kp.kb * WIN_KB, jw = j0 + 32 * wave, key = jw + l32;
+  // queries j0 .. iend - 1 see some key of the block
+  const int64_t far = j0 < a.sinks ? n : (int64_t)j0 + WIN_KB - 1 + a.window;
+  const int iend = (int)min((int64_t)n, far);
+  const int per = iend > j0 ? (iend - j0 + WIN_QT - 1) / WIN_QT : 0, total = per * G;
+  const int it0 = (int)((int64_t)total * kp.part / kp.parts);
+  const int it1 = (int)((int64_t)total * (kp.part + 1) / kp.parts);
+  f32x16 dk[NC], dv[NC];
+  clear(dk);
+  clear(dv);
+  if (it0 < it1) {
+    RowReg<TI, D> k, v;
+    const int at = min(key, n - 1);
+    k.load(slice_of<TI>(a.k, b, hk) + at * a.k.st, half, key < n);
+    v.load(slice_of<TI>(a.v, b, hk) + at * a.v.st, half, key < n);
+    const float c2 = a.scale * LOG2E_F;
+    R fq, fg;
+    float st = 0.f;  // threads 0..31: lse, 32..63: D of the tile's rows
+    auto fetch = [&](int it) {
+      const int h = hk * G + it / per, i = j0 + it % per * WIN_QT;
+      fq.fetch(slice_of<TI>(a.q, b, h), a.q.st, i, n, tid);
+      fg.fetch(slice_of<TI>(a.dO, b, h), a.dO.st, i, n, tid);
+      if (tid < 64) {
+        const int64_t r = ((int64_t)b * a.H + h) * a.T + i + l32;
+        const bool ok = i + l32 < n;
+        st = ok ? (half ? a.delta : a.lse)[r] : half ? 0.f : INFINITY;
+        if (!half && st == -INFINITY) st = INFINITY;
+        if (!half && !is_f32<TI>) st *= LOG2E_F;
+      }
+    };
+    fetch(it0);
+    for (int it = it0; it < it1; ++it) {
+      const int i = j0 + it % per * WIN_QT, p = (it - it0) & 1;
+      TI *qb = smem + p * 2 * R::SIZE, *gb = qb + R::SIZE;
+      fq.stash(qb, tid);
+      fg.stash(gb, tid);
+      if (tid < 64) stat[p][half][l32] = st;
+      const bool part = !sees_all(a, i, WIN_QT, j0, WIN_KB);
+      if (part) {
+        const bool bad = __any(fq.bad() | fg.bad());
+        if (lane == 0) flag[p][wave] = bad;
+      }
+      if (it + 1 < it1) fetch(it + 1);
+      lds_barrier();
+      if (jw >= n || !sees_some(a, i, WIN_QT, jw, 32)) continue;
+      const bool bad = part && any_flag<4>(flag[p]);
+      const bool all = sees_all(a, i, WIN_QT, jw, 32);
+      const f32x16 S = dots<D, RS>(qb, k, lane);
+      const f32x16 P = dots<D, RS>(gb, v, lane);
+      float w[16], ds[16];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 L = *reinterpret_cast<const f32x4 *>(&stat[p][0][8 * g + 4 * half]);
+        const f32x4 E = *reinterpret_cast<const f32x4 *>(&stat[p][1][8 * g + 4 * half]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * g + e;
+          const float x = is_f32<TI> ? fmaf(S[r], a.scale, -L[e]) * LOG2E_F
+                                     : fmaf(S[r], c2, -L[e]);
+          w[r] = __builtin_amdgcn_exp2f(x);
+          ds[r] = w[r] * (P[r] - E[e]);
+        }
+      }
+      if (!all) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const bool ok = sees(a, i + krel(r, half), key);
+          w[r] = ok ? w[r] : 0.f;
+          ds[r] = ok ? ds[r] : 0.f;
+        }
+      }
+      auto see = [&](int r) { return sees(a, i + krel(r, half), key) && i + krel(r, half) < n; };
+      mul_rows<D, RS, NC>(dv, gb, w, lane, bad, see);
+      mul_rows<D, RS, NC>(dk, qb, ds, lane, bad, see);
+    }
+  }
+  if (kp.slot < 0) {
+    if (key < a.T) {
+      store_row<D, NC>(slice_of<TI>(a.dk, b, hk) + key * a.dk.st, dk, half, key < n ? a.scale : 0.f);
+      store_row<D, NC>(slice_of<TI>(a.dv, b, hk) + key * a.dv.st, dv, half, key < n ? 1.f : 0.f);
+    }
+    return;
+  }
+  const int nkb = (a.T + WIN_KB - 1) / WIN_KB;
+  const int64_t slot = (int64_t)s * win_slots(nkb, a.sink_blocks, a.parts_a, a.parts_b) + kp.slot;
+  float *out = a.part + (slot * 2 * WIN_KB + 32 * wave + l32) * D;
+  store_row<D, NC>(out, dk, half, key < n ? a.scale : 0.f);
+  store_row<D, NC>(out + WIN_KB * D, dv, half, key < n ? 1.f : 0.f);
+}
+
+// The parts' sums of the blocks that have several, in order of the parts.
+template <typename TI, int D> __global__ __launch_bounds__(256) void win_sum_kernel(WinArgs a) {
+  const int kvs = a.B * a.Hkv, s = blockIdx.x % kvs, b = s / a.Hkv, hk = s % a.Hkv;
+  const int nkb = (a.T + WIN_KB - 1) / WIN_KB;
+  constexpr int PER = WIN_KB * D / 4, WGS = (2 * PER + 255) / 256;
+  const int y = blockIdx.x / kvs / WGS, z = (int)(blockIdx.x / kvs) % WGS * 256 + threadIdx.x;
+  // blocks with several parts: those of the first tokens, the others, or both
+  const int kb = a.parts_a > 1 ? y : a.sink_blocks + y;
+  const bool A = kb < a.sink_blocks;
+  const int parts = A ? a.parts_a : a.parts_b;
+  if (kb >= nkb || parts == 1 || z >= 2 * PER) return;
+  const int first = a.parts_a > 1 ? a.sink_blocks * a.parts_a : 0;
+  const int slot = A ? kb * parts : first + (kb - a.sink_blocks) * parts;
+  const float *p = a.part + ((int64_t)s * win_slots(nkb, a.sink_blocks, a.parts_a, a.parts_b) + slot)
+                              * 2 * WIN_KB * D + 4 * z;
+  f32x4 x = *reinterpret_cast<const f32x4 *>(p);
+  for (int i = 1; i < parts; ++i) x += *reinterpret_cast<const f32x4 *>(p + (int64_t)i * 2 * WIN_KB * D);
+  const int key = kb * WIN_KB + z % PER / (D / 4), c = z % (D / 4) * 4;
+  if (key >= a.T) return;
+  const View &out = z < PER ? a.dk : a.dv;
+  TI *dst = slice_of<TI>(out, b, hk) + key * out.st + c;
+  if constexpr (is_f32<TI>) *reinterpret_cast<f32x4 *>(dst) = x;
+  else *reinterpret_cast<u32x2 *>(dst) = u32x2{cvt_bf16x2(x[0], x[1]), cvt_bf16x2(x[2], x[3])};
+}
+
+template <typename TI, int D> void fwd(const WinArgs &a, hipStream_t s) {
+  constexpr int NW = 4;
+  const unsigned grid = (unsigned)(a.B * a.H) * ((a.T + 32 * NW - 1) / (32 * NW));
+  timed_call("kia_window_fwd", s, [&] {
+    hipLaunchKernelGGL((win_fwd_kernel<TI, D, NW>), dim3(grid), dim3(64 * NW), 0, s, a);
+  });
+}
+
+template <typename TI, int D> void bwd(const WinArgs &a, hipStream_t s) {
+  constexpr int NW = 4;
+  const unsigned grid = (unsigned)(a.B * a.H) * ((a.T + 32 * NW - 1) / (32 * NW));
+  timed_call("kia_window_dq", s, [&] {
+    hipLaunchKernelGGL((win_dq_kernel<TI, D, NW>), dim3(grid), dim3(64 * NW), 0, s, a);
+  });
+  const int nkb = (a.T + WIN_KB - 1) / WIN_KB, sb = a.sink_blocks;
+  const unsigned kvs = a.B * a.Hkv;
+  timed_call("kia_window_dkv", s, [&] {
+    hipLaunchKernelGGL((win_dkv_kernel<TI, D>),
+                       dim3(kvs * (sb * a.parts_a + (nkb - sb) * a.parts_b)), dim3(256), 0, s, a);
+  });
+  const int blocks = (a.parts_a > 1 ? sb : 0) + (a.parts_b > 1 ? nkb - sb : 0);
+  if (blocks) {
+    timed_call("kia_window_sum", s, [&] {
+      hipLaunchKernelGGL((win_sum_kernel<TI, D>),
+                         dim3(kvs * blocks * ((2 * WIN_KB * D / 4 + 255) / 256)), dim3(256), 0, s,
+                         a);
+    });
+  }
+}
+
+}  // namespace
+
+template <> void launch_win_fwd<KIA_HEAD>(const WinArgs &a, int dtype, int, hipStream_t s) {
+  if (dtype == KIA_F32) fwd<float, KIA_HEAD>(a, s);
+  else fwd<uint16_t, KIA_HEAD>(a, s);
+}
+template <> void launch_win_bwd<KIA_HEAD>(const WinArgs &a, int dtype, int, hipStream_t s) {
+  if (dtype == KIA_F32) bwd<float, KIA_HEAD>(a, s);
+  else bwd<uint16_t, KIA_HEAD>(a, s);
+}
+
+}  // namespace kia
