@@ -44,8 +44,8 @@ struct WinArgs {
   // each block of either kind is cut into
   int sink_blocks, parts_a, parts_b;
 };
-constexpr int WIN_KB = 128;  // keys of a block of the key gradients
-constexpr int WIN_QT = 32;   // queries of one step there
+constexpr int WIN_KB = 64;  // keys of a block of the key gradients
+constexpr int WIN_QT = 64;  // queries of one step there
 
 // Partial sums that the key blocks of one key head leave (blocks of one part leave none).
 __host__ __device__ inline int win_slots(int nkb, int sb, int pa, int pb) {

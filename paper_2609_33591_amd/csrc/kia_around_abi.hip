@@ -111,9 +111,10 @@ WinArgs window_args(int B, int H, int Hkv, int T, int d, int window, int sinks) 
   const int64_t all = (T + WIN_QT - 1) / WIN_QT;
   const int64_t near = std::min<int64_t>(all, (WIN_KB - 1 + (int64_t)a.window + WIN_QT - 1) / WIN_QT);
   const int64_t total = (int64_t)B * Hkv * G * (a.sink_blocks * all + (nkb - a.sink_blocks) * near);
-  const int64_t most = std::max<int64_t>(16, (total + 511) / 512);
-  a.parts_a = a.sink_blocks ? (int)((G * all + most - 1) / most) : 1;
+  const int64_t most = std::max<int64_t>(8, (total + 511) / 512);
   a.parts_b = nkb > a.sink_blocks ? (int)((G * near + most - 1) / most) : 1;
+  const int64_t fine = std::max<int64_t>(8, G * near / (4 * a.parts_b));
+  a.parts_a = a.sink_blocks ? (int)((G * all + fine - 1) / fine) : 1;
   return a;
 }
 

@@ -37,9 +37,12 @@ template <typename TI> constexpr bool is_f32 = sizeof(TI) == 4;
 
 // ---- rows in LDS ---------------------------------------------------------------
 // A [ROWS, D] block of rows of any stride, rows at or past `end` as zeros. The row
-// stride in LDS is D plus 16 bytes: 16-byte reads of eight rows fall in distinct banks.
+// stride in LDS is D plus 32 bytes in bf16, so that both 16-byte reads of eight rows and
+// transposing reads of four fall in distinct banks (with D plus 16 the latter overlap:
+// the 8k prompt 135 against 130 us), and D plus 16 in fp32, whose columns are read one
+// by one.
 template <typename TI, int D, int ROWS, int NT> struct Rows {
-  static constexpr int V = 16 / sizeof(TI), RS = D + V, SIZE = ROWS * RS;
+  static constexpr int V = 16 / sizeof(TI), RS = D + (is_f32<TI> ? 4 : 16), SIZE = ROWS * RS;
   static constexpr int PER = ROWS * D / V, PF = (PER + NT - 1) / NT, RPP = NT * V / D;
   static_assert(PER % NT == 0 || PF == 1, "whole passes");
   u32x4 x[PF];
@@ -147,66 +150,66 @@ __device__ __forceinline__ f32x16 dots(const float *t, const RowReg<float, D> &b
   return c;
 }
 
-// A value with what is infinite or NaN in it as 0, and a count of the latter: 1 for
-// +inf, 2^7 for -inf, 2^14 for NaN (sums over 32 rows stay apart, and exact in bf16
-// products with fp32 sums).
-__device__ __forceinline__ float count_of(float x) {
-  return fabsf(x) < INFINITY ? 0.f : x == INFINITY ? 1.f : x == -INFINITY ? 128.f : 16384.f;
-}
-// what such a count adds to a sum
-__device__ __forceinline__ float sum_of(float n) {
-  const int k = (int)n;
-  const bool nan = k >= 16384 || ((k & 127) && k >= 128);
-  return nan ? NAN : k >= 128 ? -INFINITY : k ? INFINITY : 0.f;
+// The same with b's rows in LDS too.
+template <int D, int RS>
+__device__ __forceinline__ f32x16 dots(const uint16_t *t, const uint16_t *b, int lane) {
+  f32x16 c = {};
+  const int at = (lane & 31) * RS + 8 * (lane >> 5);
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s)
+    c = mfma16(row_op(t + at + 16 * s), row_op(b + at + 16 * s), c);
+  return c;
 }
 
 // acc[c][channel][row of b's side] += sum over the 32 streamed rows of their
 // channels 32 c .. times the weights w (register r: streamed row krel(r, half)).
-// `bad`: the rows hold infinities or NaNs; see(r) tells whether the pair of register
-// r is one that counts.
+// `bad`: some of the rows hold infinities or NaNs, and some pairs do not count
+// (see(i): streamed row i counts for the lane's row): those values take part as zeros,
+// and are added to the rows that they count for one by one.
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
+template <int D, int RS, int NC, typename TI, class See>
+__device__ __forceinline__ void add_bad(f32x16 (&acc)[NC], const TI *t, int lane, See see) {
+#pragma unroll 1
+  for (int i = 0; i < 32; ++i) {
+    const bool ok = see(i);
+    const TI *row = t + i * RS + 4 * (lane >> 5);
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int g = 0; g < (D < 32 ? D / 8 : 4); ++g) {
+        const f32x4 x = load4(row + 32 * c + 8 * g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[c][4 * g + e] += ok && !finite(x[e]) ? x[e] : 0.f;
+      }
+  }
+}
 template <int D, int RS, int NC, class See>
 __device__ __forceinline__ void mul_rows(f32x16 (&acc)[NC], const uint16_t *t, const float (&w)[16],
                                          int lane, bool bad, See see) {
   const uint16_t *p = t + tr_base<D, RS>(lane);
-  if (!__builtin_expect(bad, 0)) {
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      u32x4 x;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = cvt_bf16x2(w[8 * s + 2 * e], w[8 * s + 2 * e + 1]);
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-        acc[c] = mfma16(tr_op<RS>(p + 16 * s * RS + 32 * c), as_op(x), acc[c]);
-    }
-    return;
-  }
-  bf16x8 x[2], one[2];
+  u32x4 x[2];
 #pragma unroll
   for (int s = 0; s < 2; ++s)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      x[s][e] = (__bf16)w[8 * s + e];
-      one[s][e] = (__bf16)(see(8 * s + e) ? 1.f : 0.f);
-    }
+    for (int e = 0; e < 4; ++e) x[s][e] = cvt_bf16x2(w[8 * s + 2 * e], w[8 * s + 2 * e + 1]);
+  if (!__builtin_expect(bad, 0)) {
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    f32x16 n = {};
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const bf16x8 y = tr_op<RS>(p + 16 * s * RS + 32 * c);
-      bf16x8 f, k;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float v = (float)y[e];
-        f[e] = fabsf(v) < INFINITY ? y[e] : (__bf16)0.f;
-        k[e] = (__bf16)count_of(v);
-      }
-      acc[c] = mfma16(f, x[s], acc[c]);
-      n = mfma16(k, one[s], n);
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[c][r] += sum_of(n[r]);
+      for (int c = 0; c < NC; ++c)
+        acc[c] = mfma16(tr_op<RS>(p + 16 * s * RS + 32 * c), as_op(x[s]), acc[c]);
+    return;
   }
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      bf16x8 y = tr_op<RS>(p + 16 * s * RS + 32 * c);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = finite((float)y[e]) ? y[e] : (__bf16)0.f;
+      acc[c] = mfma16(y, as_op(x[s]), acc[c]);
+    }
+  add_bad<D, RS>(acc, t, lane, see);
 }
 template <int D, int RS, int NC, class See>
 __device__ __forceinline__ void mul_rows(f32x16 (&acc)[NC], const float *t, const float (&w)[16],
@@ -220,17 +223,13 @@ __device__ __forceinline__ void mul_rows(f32x16 (&acc)[NC], const float *t, cons
     return;
   }
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    f32x16 n = {};
+  for (int r = 0; r < 16; ++r)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
+    for (int c = 0; c < NC; ++c) {
       const float v = p[krel0(r) * RS + 32 * c];
-      acc[c] = mfma32(fabsf(v) < INFINITY ? v : 0.f, w[r], acc[c]);
-      n = mfma32(count_of(v), see(r) ? 1.f : 0.f, n);
+      acc[c] = mfma32(finite(v) ? v : 0.f, w[r], acc[c]);
     }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[c][r] += sum_of(n[r]);
-  }
+  add_bad<D, RS>(acc, t, lane, see);
 }
 
 // One lane's row from accumulators (register r of block c: channel
@@ -389,9 +388,8 @@ __global__ __launch_bounds__(64 * NW, 2) void win_fwd_kernel(WinArgs a) {
           sum += w[r];
         }
         l += sum;
-        mul_rows<D, RS, NC>(acc, vb + 32 * u * RS, w, lane, bad, [&](int r) {
-          return sees(a, row, j + 32 * u + krel(r, half));
-        });
+        mul_rows<D, RS, NC>(acc, vb + 32 * u * RS, w, lane, bad,
+                            [&](int i) { return sees(a, row, j + 32 * u + i); });
       }
     }
   }
@@ -478,9 +476,8 @@ __global__ __launch_bounds__(64 * NW, 2) void win_dq_kernel(WinArgs a) {
           for (int r = 0; r < 16; ++r)
             w[r] = sees(a, row, j + 32 * u + krel(r, half)) ? w[r] : 0.f;
         }
-        mul_rows<D, RS, NC>(acc, kb + 32 * u * RS, w, lane, bad, [&](int r) {
-          return sees(a, row, j + 32 * u + krel(r, half));
-        });
+        mul_rows<D, RS, NC>(acc, kb + 32 * u * RS, w, lane, bad,
+                            [&](int i) { return sees(a, row, j + 32 * u + i); });
       }
     }
   }
@@ -501,26 +498,34 @@ struct KeyPart {
   }
 };
 
-// dK and dV. One workgroup: 128 keys of one key head, 32 to a wave, over a part of the
-// 32-query tiles that see any of them, of every query head that shares the key head.
-// Blocks whose tiles are many (those of the first tokens, which every query sees) are
-// cut into parts, whose sums win_sum_kernel adds in order: no atomics, so that the
-// gradients repeat bit for bit.
+// dK and dV. One workgroup: 64 keys of one key head, over a part of the 64-query tiles
+// that see any of them, of every query head that shares the key head; its four waves
+// are two halves of the keys times two halves of each tile's queries, whose sums are
+// added at the end through LDS. Blocks whose tiles are many (those of the first
+// tokens, which every query sees) are cut into parts, whose sums win_sum_kernel adds in
+// order: no atomics, so that the gradients repeat bit for bit.
+// At d = 128 in bf16 the keys and values stay in LDS: with them in registers the sums
+// (128) leave too few.
 template <typename TI, int D>
 __global__ __launch_bounds__(256, is_f32<TI> && D == 128 ? 1 : 2) void win_dkv_kernel(WinArgs a) {
   constexpr int NT = 256, NC = D >= 32 ? D / 32 : 1;
+  constexpr bool KV = !is_f32<TI> && D == 128;
   using R = Rows<TI, D, WIN_QT, NT>;
   constexpr int RS = R::RS;
-  __shared__ __attribute__((aligned(16))) TI smem[4 * R::SIZE + 32];
-  __shared__ __attribute__((aligned(16))) float stat[2][2][WIN_QT];
-  __shared__ int flag[2][4];
+  // queries and dO (and keys and values); then the second half's sums
+  constexpr int SMEM = (KV ? 4 : 2) * R::SIZE * sizeof(TI) + 64;
+  constexpr int RED = 2 * 64 * 2 * NC * 16 * 4;
+  __shared__ __attribute__((aligned(16))) char smem[SMEM > RED ? SMEM : RED];
+  __shared__ __attribute__((aligned(16))) float stat[2][WIN_QT];
+  __shared__ int flag[4];
+  TI *qb = reinterpret_cast<TI *>(smem), *gb = qb + R::SIZE, *kb = gb + R::SIZE, *vb = kb + R::SIZE;
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kg = wave & 1, qg = wave >> 1;
   const int G = a.H / a.Hkv, kvs = a.B * a.Hkv;
   const int s = blockIdx.x % kvs, b = s / a.Hkv, hk = s % a.Hkv;
   const KeyPart kp(a, blockIdx.x / kvs);
   const int n = length_of(a, b);
-  const int j0 = kp.kb * WIN_KB, jw = j0 + 32 * wave, key = jw + l32;
+  const int j0 = kp.kb * WIN_KB, jw = j0 + 32 * kg, key = jw + l32;
   // queries j0 .. iend - 1 see some key of the block
   const int64_t far = j0 < a.sinks ? n : (int64_t)j0 + WIN_KB - 1 + a.window;
   const int iend = (int)min((int64_t)n, far);
@@ -532,48 +537,63 @@ __global__ __launch_bounds__(256, is_f32<TI> && D == 128 ? 1 : 2) void win_dkv_k
   clear(dv);
   if (it0 < it1) {
     RowReg<TI, D> k, v;
-    const int at = min(key, n - 1);
-    k.load(slice_of<TI>(a.k, b, hk) + at * a.k.st, half, key < n);
-    v.load(slice_of<TI>(a.v, b, hk) + at * a.v.st, half, key < n);
-    const float c2 = a.scale * LOG2E_F;
+    const TI *ks = slice_of<TI>(a.k, b, hk), *vs = slice_of<TI>(a.v, b, hk);
     R fq, fg;
-    float st = 0.f;  // threads 0..31: lse, 32..63: D of the tile's rows
+    if constexpr (KV) {
+      fq.fetch(ks, a.k.st, j0, n, tid);
+      fg.fetch(vs, a.v.st, j0, n, tid);
+      fq.stash(kb, tid);
+      fg.stash(vb, tid);
+    } else {
+      const int at = min(key, n - 1);
+      k.load(ks + at * a.k.st, half, key < n);
+      v.load(vs + at * a.v.st, half, key < n);
+    }
+    const float c2 = a.scale * LOG2E_F;
+    float st = 0.f;  // threads 0..63: lse, 64..127: D of the tile's rows
     auto fetch = [&](int it) {
       const int h = hk * G + it / per, i = j0 + it % per * WIN_QT;
       fq.fetch(slice_of<TI>(a.q, b, h), a.q.st, i, n, tid);
       fg.fetch(slice_of<TI>(a.dO, b, h), a.dO.st, i, n, tid);
-      if (tid < 64) {
-        const int64_t r = ((int64_t)b * a.H + h) * a.T + i + l32;
-        const bool ok = i + l32 < n;
-        st = ok ? (half ? a.delta : a.lse)[r] : half ? 0.f : INFINITY;
-        if (!half && st == -INFINITY) st = INFINITY;
-        if (!half && !is_f32<TI>) st *= LOG2E_F;
+      if (wave < 2) {
+        const int64_t r = ((int64_t)b * a.H + h) * a.T + i + lane;
+        const bool ok = i + lane < n;
+        st = ok ? (wave ? a.delta : a.lse)[r] : wave ? 0.f : INFINITY;
+        if (!wave && st == -INFINITY) st = INFINITY;
+        if (!wave && !is_f32<TI>) st *= LOG2E_F;
       }
     };
     fetch(it0);
     for (int it = it0; it < it1; ++it) {
-      const int i = j0 + it % per * WIN_QT, p = (it - it0) & 1;
-      TI *qb = smem + p * 2 * R::SIZE, *gb = qb + R::SIZE;
+      const int i = j0 + it % per * WIN_QT, iw = i + 32 * qg;
+      if (it > it0) lds_barrier();
       fq.stash(qb, tid);
       fg.stash(gb, tid);
-      if (tid < 64) stat[p][half][l32] = st;
+      if (wave < 2) stat[wave][lane] = st;
       const bool part = !sees_all(a, i, WIN_QT, j0, WIN_KB);
       if (part) {
         const bool bad = __any(fq.bad() | fg.bad());
-        if (lane == 0) flag[p][wave] = bad;
+        if (lane == 0) flag[wave] = bad;
       }
       if (it + 1 < it1) fetch(it + 1);
       lds_barrier();
-      if (jw >= n || !sees_some(a, i, WIN_QT, jw, 32)) continue;
-      const bool bad = part && any_flag<4>(flag[p]);
-      const bool all = sees_all(a, i, WIN_QT, jw, 32);
-      const f32x16 S = dots<D, RS>(qb, k, lane);
-      const f32x16 P = dots<D, RS>(gb, v, lane);
+      if (jw >= n || iw >= n || !sees_some(a, iw, 32, jw, 32)) continue;
+      const bool bad = part && any_flag<4>(flag);
+      const bool all = sees_all(a, iw, 32, jw, 32);
+      const TI *qt = qb + 32 * qg * RS, *gt = gb + 32 * qg * RS;
+      f32x16 S, P;
+      if constexpr (KV) {
+        S = dots<D, RS>(qt, kb + 32 * kg * RS, lane);
+        P = dots<D, RS>(gt, vb + 32 * kg * RS, lane);
+      } else {
+        S = dots<D, RS>(qt, k, lane);
+        P = dots<D, RS>(gt, v, lane);
+      }
       float w[16], ds[16];
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const f32x4 L = *reinterpret_cast<const f32x4 *>(&stat[p][0][8 * g + 4 * half]);
-        const f32x4 E = *reinterpret_cast<const f32x4 *>(&stat[p][1][8 * g + 4 * half]);
+        const f32x4 L = *reinterpret_cast<const f32x4 *>(&stat[0][32 * qg + 8 * g + 4 * half]);
+        const f32x4 E = *reinterpret_cast<const f32x4 *>(&stat[1][32 * qg + 8 * g + 4 * half]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int r = 4 * g + e;
@@ -586,16 +606,38 @@ __global__ __launch_bounds__(256, is_f32<TI> && D == 128 ? 1 : 2) void win_dkv_k
       if (!all) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const bool ok = sees(a, i + krel(r, half), key);
+          const bool ok = sees(a, iw + krel(r, half), key);
           w[r] = ok ? w[r] : 0.f;
           ds[r] = ok ? ds[r] : 0.f;
         }
       }
-      auto see = [&](int r) { return sees(a, i + krel(r, half), key) && i + krel(r, half) < n; };
-      mul_rows<D, RS, NC>(dv, gb, w, lane, bad, see);
-      mul_rows<D, RS, NC>(dk, qb, ds, lane, bad, see);
+      auto see = [&](int r) { return sees(a, iw + r, key); };
+      mul_rows<D, RS, NC>(dv, gt, w, lane, bad, see);
+      mul_rows<D, RS, NC>(dk, qt, ds, lane, bad, see);
     }
   }
+  // the halves of the queries: the second hands its sums over
+  __syncthreads();
+  f32x4 *red = reinterpret_cast<f32x4 *>(smem) + kg * 64 * 2 * NC * 4 + lane;
+  if (qg == 1) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        red[64 * (8 * c + g)] = f32x4{dk[c][4 * g], dk[c][4 * g + 1], dk[c][4 * g + 2], dk[c][4 * g + 3]};
+        red[64 * (8 * c + 4 + g)] = f32x4{dv[c][4 * g], dv[c][4 * g + 1], dv[c][4 * g + 2], dv[c][4 * g + 3]};
+      }
+  }
+  __syncthreads();
+  if (qg == 1) return;
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 x = red[64 * (8 * c + g)], y = red[64 * (8 * c + 4 + g)];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dk[c][4 * g + e] += x[e], dv[c][4 * g + e] += y[e];
+    }
   if (kp.slot < 0) {
     if (key < a.T) {
       store_row<D, NC>(slice_of<TI>(a.dk, b, hk) + key * a.dk.st, dk, half, key < n ? a.scale : 0.f);
@@ -605,7 +647,7 @@ __global__ __launch_bounds__(256, is_f32<TI> && D == 128 ? 1 : 2) void win_dkv_k
   }
   const int nkb = (a.T + WIN_KB - 1) / WIN_KB;
   const int64_t slot = (int64_t)s * win_slots(nkb, a.sink_blocks, a.parts_a, a.parts_b) + kp.slot;
-  float *out = a.part + (slot * 2 * WIN_KB + 32 * wave + l32) * D;
+  float *out = a.part + (slot * 2 * WIN_KB + 32 * kg + l32) * D;
   store_row<D, NC>(out, dk, half, key < n ? a.scale : 0.f);
   store_row<D, NC>(out + WIN_KB * D, dv, half, key < n ? 1.f : 0.f);
 }
