@@ -61,8 +61,8 @@ struct CacheArgs {
   View k, v;                           // the tokens to hold, or where to read them to
   int pages, lpage, width, B, Hkv, T;  // lpage: log2 of the tokens of a page
 };
-void launch_cache_write(const CacheArgs &a, int d, int dtype, hipStream_t s);
-void launch_cache_read(const CacheArgs &a, int d, int dtype, hipStream_t s);
+void launch_cache_write(const CacheArgs &a, int d, int dtype, int cus, hipStream_t s);
+void launch_cache_read(const CacheArgs &a, int d, int dtype, int cus, hipStream_t s);
 
 struct CachedArgs {
   const uint8_t *cache;
@@ -73,14 +73,14 @@ struct CachedArgs {
   int window, sinks;  // window: INT_MAX where there is none
   int K, calib, recon;
   float tau, scale;
-  int tiles, splits;  // 16-row tiles of a key head's rows, workgroups that share a tile's keys
+  int tiles, shares;  // 16-row tiles of a key head's rows, parts of its keys (< 256)
 };
 // Floats of the workspace: the parts' extrema, their maxima and sums, their rows.
 struct CachedLayout {
   size_t ext, stat, part, total;
 };
 inline CachedLayout cached_layout(const CachedArgs &a, int d) {
-  const size_t n = (size_t)a.B * a.Hkv * a.tiles * a.splits * 16;
+  const size_t n = (size_t)(a.shares + a.B) * a.Hkv * a.tiles * 16;
   CachedLayout l;
   l.ext = 0;
   l.stat = 2 * n;

@@ -229,7 +229,7 @@ int cache_copy(bool write, const kia_view *k, const kia_view *v, void *cache, in
   }
   if (!starts) return KIA_ERR_NULL;
   if ((uintptr_t)starts & 3u || (uintptr_t)counts & 3u) return KIA_ERR_ALIGN;
-  if ((double)2 * B * Hkv * T * d >= 2147483648.0 * 1024) return KIA_ERR_SHAPE;
+  if (2.0 * B * Hkv * (T / 16 + 1) >= 2147483648.0) return KIA_ERR_SHAPE;
   CacheArgs a{};
   a.cache = static_cast<uint8_t *>(cache);
   a.table = table, a.starts = starts, a.counts = counts;
@@ -237,21 +237,26 @@ int cache_copy(bool write, const kia_view *k, const kia_view *v, void *cache, in
   a.pages = pages, a.lpage = page_log(page), a.width = width;
   a.B = B, a.Hkv = Hkv, a.T = T;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (write) timed_call("kia_cache4_write", s, [&] { launch_cache_write(a, d, dtype, s); });
-  else timed_call("kia_cache4_read", s, [&] { launch_cache_read(a, d, dtype, s); });
+  const int cus = host_cus();
+  if (write) timed_call("kia_cache4_write", s, [&] { launch_cache_write(a, d, dtype, cus, s); });
+  else timed_call("kia_cache4_read", s, [&] { launch_cache_read(a, d, dtype, cus, s); });
   return launched();
 }
 
-// The launch shape: row tiles of 16, and the workgroups that share a tile's keys.
-void cached_shape(CachedArgs &a, int cus) {
+// The launch shape: row tiles of 16, and the parts that their keys are cut into, all
+// resident at once: three workgroups a CU in bf16, two in fp32 (registers). More parts
+// cost more joining than the balance gains (32 sequences of 16 000 keys, softmax, bf16:
+// 67 / 59 / 69 us with two / three / six a CU; fp32, 16 sequences: 42 / 48 with two /
+// three). A part has 128 keys at least, 32 for each wave.
+void cached_shape(CachedArgs &a, int dtype, int cus) {
   a.tiles = (a.T * (a.H / a.Hkv) + 15) / 16;
   const int64_t keys = (int64_t)a.width << a.lpage;
   const int64_t most = a.window == INT_MAX
                            ? keys
-                           : std::min(keys, (int64_t)a.window + a.T + a.sinks + 128);
-  const int64_t chunks = (most + 63) / 64, tiles = (int64_t)a.B * a.Hkv * a.tiles;
-  const int64_t want = (4 * cus + tiles - 1) / tiles;
-  a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, (chunks + 3) / 4, 256}));
+                           : std::min(keys, (int64_t)a.window + a.T + a.sinks + 64);
+  const int64_t groups = (int64_t)a.Hkv * a.tiles, parts = (most + 127) / 128;
+  const int64_t want = std::max<int64_t>(1, (dtype == KIA_F32 ? 2 : 3) * cus / groups);
+  a.shares = parts == 1 ? 1 : (int)std::min<int64_t>({want, parts * a.B, 255});
 }
 
 int check_cached(int H, int Hkv, int K, int calib, float tau, int recon, int window, int sinks) {
@@ -267,14 +272,14 @@ int check_cached(int H, int Hkv, int K, int calib, float tau, int recon, int win
 }
 
 int cached_args(CachedArgs &a, int pages, int page, int width, int B, int H, int Hkv, int T,
-                int window, int sinks) {
+                int window, int sinks, int dtype) {
   a.pages = pages, a.lpage = page_log(page), a.width = width;
   a.B = B, a.H = H, a.Hkv = Hkv, a.T = T;
   a.window = window > 0 ? window : INT_MAX;
   a.sinks = window > 0 ? sinks : 0;
   if ((double)T * (H / Hkv) >= 1 << 24) return KIA_ERR_SHAPE;
-  cached_shape(a, host_cus());
-  if ((double)B * Hkv * a.tiles * a.splits >= 2147483648.0) return KIA_ERR_SHAPE;
+  cached_shape(a, dtype, host_cus());
+  if ((double)(a.shares + B) * Hkv * a.tiles >= 2147483648.0) return KIA_ERR_SHAPE;
   return KIA_OK;
 }
 
@@ -317,7 +322,8 @@ extern "C" int kia_cache4_ws_bytes(int page, int width, int B, int H, int Hkv, i
   if (page_log(page) < 0) return KIA_ERR_CACHE;
   if (width < 1 || (int64_t)width * page > INT_MAX || window < 0 || sinks < 0) return KIA_ERR_SHAPE;
   CachedArgs a{};
-  rc = cached_args(a, 1, page, width, B, H, Hkv, T, window, sinks);
+  // (bf16 takes the more parts)
+  rc = cached_args(a, 1, page, width, B, H, Hkv, T, window, sinks, KIA_BF16);
   if (rc) return rc;
   *bytes = cached_layout(a, d).total * 4;
   return KIA_OK;
@@ -336,7 +342,7 @@ extern "C" int kia_cache4_attn(const kia_view *q, const kia_view *o, const void 
   if (!lengths || !ws) return KIA_ERR_NULL;
   if ((uintptr_t)lengths & 3u || (uintptr_t)ws & 255u) return KIA_ERR_ALIGN;
   CachedArgs a{};
-  rc = cached_args(a, pages, page, width, B, H, Hkv, T, window, sinks);
+  rc = cached_args(a, pages, page, width, B, H, Hkv, T, window, sinks, dtype);
   if (rc) return rc;
   a.cache = static_cast<const uint8_t *>(cache);
   a.table = table, a.lengths = lengths;

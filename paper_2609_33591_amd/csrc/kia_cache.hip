@@ -38,152 +38,188 @@ __device__ __forceinline__ void store8(uint16_t *p, const float (&x)[8]) {
   *reinterpret_cast<u32x4 *>(p) = w;
 }
 
-// The place of eight channels of one token: thread index -> (which, head, token,
-// channels), and whether the table has a page for it.
-template <int D> struct Place {
-  int which, b, h, t, oct;
-  bool in, held;
-  int64_t base;  // of the head's block of the page
-  int tok;
-  __device__ __forceinline__ Place(const CacheArgs &a, int64_t i) {
-    oct = (int)(i % (D / 8));
-    i /= D / 8;
-    t = (int)(i % a.T);
-    i /= a.T;
-    h = (int)(i % a.Hkv);
-    i /= a.Hkv;
-    b = (int)(i % a.B);
-    which = (int)(i / a.B);
-    in = which < 2;
-    held = false;
-    base = 0, tok = 0;
-    if (!in || (a.counts && t >= a.counts[b])) return;
+// The place of a thread: eight channels of REP tokens, TOKENS apart, of one head's keys or
+// values. What is the same for all of a workgroup is in scalar registers.
+template <int D, int REP> struct Place {
+  static constexpr int TOKENS = CACHE_NT * 8 / D;
+  int which, b, h, t0, oct;
+  __device__ __forceinline__ Place(const CacheArgs &a) {
+    const int nb = (a.T + REP * TOKENS - 1) / (REP * TOKENS), s = blockIdx.x / nb;
+    which = s % 2;
+    h = s / 2 % a.Hkv;
+    b = s / 2 / a.Hkv;
+    t0 = (int)(blockIdx.x % nb) * REP * TOKENS + threadIdx.x / (D / 8);
+    oct = threadIdx.x % (D / 8);
+  }
+  __device__ __forceinline__ int token(int i) const { return t0 + i * TOKENS; }
+  // the head's block of the token's page, or nullptr; tok: the token in the page
+  __device__ __forceinline__ uint8_t *held(const CacheArgs &a, int t, int &tok) const {
+    if (t >= a.T || (a.counts && t >= a.counts[b])) return nullptr;
     const int64_t pos = (int64_t)a.starts[b] + t;
-    if (pos < 0 || pos >= (int64_t)a.width << a.lpage) return;
+    if (pos < 0 || pos >= (int64_t)a.width << a.lpage) return nullptr;
     const int page = a.table[(int64_t)b * a.width + (pos >> a.lpage)];
-    if (page < 0 || page >= a.pages) return;
-    held = true;
+    if (page < 0 || page >= a.pages) return nullptr;
     tok = (int)(pos & ((1 << a.lpage) - 1));
-    base = cache_block<D>(page, which, h, a.Hkv, a.lpage);
+    return a.cache + cache_block<D>(page, which, h, a.Hkv, a.lpage);
   }
 };
 
-// The code of a value in units of its group's scale: bit 3 the sign, bits 0-2 the level.
-__device__ __forceinline__ uint32_t code_of(float x) {
-  const float a = fabsf(x);
-  const uint32_t c = (a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) +
-                     (a >= 3.5f) + (a > 5.f);
-  return c | (__float_as_uint(x) >> 31 << 3);
+// Codes of eight values in units of their group's scale (to the nearest level, an even
+// one between two, at most 6), and the values of eight codes: an instruction a pair.
+__device__ __forceinline__ uint32_t codes_of(const float (&x)[8]) {
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], 1.f, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], 1.f, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], 1.f, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], 1.f, 3);
 }
-__device__ __forceinline__ float value_of(uint32_t code) {
-  // 0, .5, 1, 1.5, 2, 3, 4, 6: levels 2 and up are 1.m 2^(e - 1)
-  const uint32_t l = code & 7;
-  const float v = l < 2 ? 0.5f * l : __uint_as_float((127u - 1u + (l >> 1)) << 23 | (l & 1) << 22);
-  return code & 8 ? -v : v;
+template <int S> __device__ __forceinline__ void pair_of(uint32_t w, float f, float (&x)[8]) {
+  const auto v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, S);
+  x[2 * S] = v[0] * f;
+  x[2 * S + 1] = v[1] * f;
+}
+__device__ __forceinline__ void values_of(uint32_t w, float f, float (&x)[8]) {
+  pair_of<0>(w, f, x);
+  pair_of<1>(w, f, x);
+  pair_of<2>(w, f, x);
+  pair_of<3>(w, f, x);
 }
 
-template <typename TI, int D> __global__ __launch_bounds__(CACHE_NT) void write_kernel(CacheArgs a) {
-  const Place<D> p(a, (int64_t)blockIdx.x * CACHE_NT + threadIdx.x);
-  float x[8] = {};
-  if (p.held) {
-    const View &v = p.which ? a.v : a.k;
-    load8(slice_of<TI>(v, p.b, p.h) + p.t * v.st + 8 * p.oct, x);
-  }
+// Eight channels of one token into its page's block c.
+template <int D>
+__device__ __forceinline__ void hold(const float (&x)[8], uint8_t *c, int tok, int which, int oct,
+                                     int lpage) {
   // (as bits: NaN above infinity above every finite value)
   uint32_t top = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
   top = max(top, (uint32_t)__shfl_xor((int)top, 1));
   top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-  if (!p.held) return;
+  if (!c) return;
   // top = 1.m 2^k: at most 6 2^(k - 2) if 1.m <= 1.5, and 6 2^(k - 1) otherwise
   int e = (int)(top >> 23) - 127 - ((top & 0x7fffffu) <= 0x400000u ? 2 : 1);
   e = min(max(e, -126), 125);
   const bool bad = top >= 0x7f800000u;
-  // (2^-e in two factors: 2^126 is the largest, and tiny values are not lost)
   const float f = __uint_as_float((uint32_t)(127 - e) << 23);
-  uint32_t w = 0;
+  float y[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w |= bad ? 0u : code_of(x[i] * f) << (4 * i);
+  for (int i = 0; i < 8; ++i) y[i] = x[i] * f;
+  const uint32_t w = bad ? 0u : codes_of(y);
   const uint8_t s = bad ? 255 : (uint8_t)(e + 127);
-  uint8_t *c = a.cache + p.base;
-  const int codes = D / 2 << a.lpage, g = p.oct / 4;
-  if (p.which == 0) {
-    *reinterpret_cast<uint32_t *>(c + p.tok * (D / 2) + 4 * p.oct) = w;
-    if (p.oct % 4 == 0) c[codes + p.tok * (D / 32) + g] = s;
+  const int codes = D / 2 << lpage, g = oct / 4;
+  if (which == 0) {
+    *reinterpret_cast<uint32_t *>(c + tok * (D / 2) + 4 * oct) = w;
+    if (oct % 4 == 0) c[codes + tok * (D / 32) + g] = s;
   } else {
     // four tokens side by side: column r holds D / 16 channels, D / 32 bytes a token
-    uint8_t *d = c + p.tok / 4 * (2 * D) + p.tok % 4 * (D / 32);
+    uint8_t *d = c + tok / 4 * (2 * D) + tok % 4 * (D / 32);
     if constexpr (D == 128) {
-      *reinterpret_cast<uint32_t *>(d + p.oct * 16) = w;
+      *reinterpret_cast<uint32_t *>(d + oct * 16) = w;
     } else if constexpr (D == 64) {
-      *reinterpret_cast<uint16_t *>(d + 2 * p.oct * 8) = (uint16_t)w;
-      *reinterpret_cast<uint16_t *>(d + (2 * p.oct + 1) * 8) = (uint16_t)(w >> 16);
+      *reinterpret_cast<uint16_t *>(d + 2 * oct * 8) = (uint16_t)w;
+      *reinterpret_cast<uint16_t *>(d + (2 * oct + 1) * 8) = (uint16_t)(w >> 16);
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) d[(4 * p.oct + i) * 4] = (uint8_t)(w >> (8 * i));
+      for (int i = 0; i < 4; ++i) d[(4 * oct + i) * 4] = (uint8_t)(w >> (8 * i));
     }
-    if (p.oct % 4 == 0) c[codes + p.tok / 4 * (D / 8) + 4 * g + p.tok % 4] = s;
+    if (oct % 4 == 0) c[codes + tok / 4 * (D / 8) + 4 * g + tok % 4] = s;
   }
 }
 
-template <typename TI, int D> __global__ __launch_bounds__(CACHE_NT) void read_kernel(CacheArgs a) {
-  const Place<D> p(a, (int64_t)blockIdx.x * CACHE_NT + threadIdx.x);
-  if (!p.in) return;
-  float x[8] = {};
-  if (p.held) {
-    const uint8_t *c = a.cache + p.base;
-    const int codes = D / 2 << a.lpage, g = p.oct / 4;
-    uint32_t w = 0;
-    uint8_t s;
-    if (p.which == 0) {
-      w = *reinterpret_cast<const uint32_t *>(c + p.tok * (D / 2) + 4 * p.oct);
-      s = c[codes + p.tok * (D / 32) + g];
-    } else {
-      const uint8_t *d = c + p.tok / 4 * (2 * D) + p.tok % 4 * (D / 32);
-      if constexpr (D == 128) {
-        w = *reinterpret_cast<const uint32_t *>(d + p.oct * 16);
-      } else if constexpr (D == 64) {
-        w = *reinterpret_cast<const uint16_t *>(d + 2 * p.oct * 8) |
-            (uint32_t)*reinterpret_cast<const uint16_t *>(d + (2 * p.oct + 1) * 8) << 16;
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w |= (uint32_t)d[(4 * p.oct + i) * 4] << (8 * i);
-      }
-      s = c[codes + p.tok / 4 * (D / 8) + 4 * g + p.tok % 4];
-    }
-    const float f = s == 255 ? NAN : __uint_as_float((uint32_t)s << 23);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = value_of(w >> (4 * i)) * f;
+// The codes of eight channels of a token in block c, and their group's scale byte.
+template <int D>
+__device__ __forceinline__ void held_of(const uint8_t *c, int tok, int which, int oct, int lpage,
+                                         uint32_t &w, uint32_t &s) {
+  const int codes = D / 2 << lpage, g = oct / 4;
+  if (which == 0) {
+    w = *reinterpret_cast<const uint32_t *>(c + tok * (D / 2) + 4 * oct);
+    s = c[codes + tok * (D / 32) + g];
+    return;
   }
-  const View &v = p.which ? a.v : a.k;
-  store8(slice_of<TI>(v, p.b, p.h) + p.t * v.st + 8 * p.oct, x);
-}
-
-template <int D> void launch(const CacheArgs &a, bool write, int dtype, hipStream_t s) {
-  const int64_t n = (int64_t)2 * a.B * a.Hkv * a.T * (D / 8);
-  const dim3 grid((unsigned)((n + CACHE_NT - 1) / CACHE_NT)), block(CACHE_NT);
-  if (write) {
-    if (dtype == KIA_F32) hipLaunchKernelGGL((write_kernel<float, D>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((write_kernel<uint16_t, D>), grid, block, 0, s, a);
+  const uint8_t *d = c + tok / 4 * (2 * D) + tok % 4 * (D / 32);
+  if constexpr (D == 128) {
+    w = *reinterpret_cast<const uint32_t *>(d + oct * 16);
+  } else if constexpr (D == 64) {
+    w = *reinterpret_cast<const uint16_t *>(d + 2 * oct * 8) |
+        (uint32_t)*reinterpret_cast<const uint16_t *>(d + (2 * oct + 1) * 8) << 16;
   } else {
-    if (dtype == KIA_F32) hipLaunchKernelGGL((read_kernel<float, D>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((read_kernel<uint16_t, D>), grid, block, 0, s, a);
+    w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w |= (uint32_t)d[(4 * oct + i) * 4] << (8 * i);
+  }
+  s = c[codes + tok / 4 * (D / 8) + 4 * g + tok % 4];
+}
+
+template <typename TI, int D, int REP>
+__global__ __launch_bounds__(CACHE_NT) void write_kernel(CacheArgs a) {
+  const Place<D, REP> p(a);
+  const View &v = p.which ? a.v : a.k;
+  const TI *src = slice_of<TI>(v, p.b, p.h) + 8 * p.oct;
+  // (rows are read whether they are held or not: their way does not wait for the table's)
+  float x[REP][8] = {};
+#pragma unroll
+  for (int i = 0; i < REP; ++i)
+    if (p.token(i) < a.T) load8(src + p.token(i) * v.st, x[i]);
+#pragma unroll
+  for (int i = 0; i < REP; ++i) {
+    int tok = 0;
+    uint8_t *c = p.held(a, p.token(i), tok);
+    hold<D>(x[i], c, tok, p.which, p.oct, a.lpage);
   }
 }
-void launch_any(const CacheArgs &a, bool write, int d, int dtype, hipStream_t s) {
-  if (d == 32) launch<32>(a, write, dtype, s);
-  else if (d == 64) launch<64>(a, write, dtype, s);
-  else launch<128>(a, write, dtype, s);
+
+template <typename TI, int D, int REP>
+__global__ __launch_bounds__(CACHE_NT) void read_kernel(CacheArgs a) {
+  const Place<D, REP> p(a);
+  const View &v = p.which ? a.v : a.k;
+  TI *dst = slice_of<TI>(v, p.b, p.h) + 8 * p.oct;
+  uint32_t w[REP] = {}, s[REP] = {};
+#pragma unroll
+  for (int i = 0; i < REP; ++i) {
+    int tok = 0;
+    if (const uint8_t *c = p.held(a, p.token(i), tok))
+      held_of<D>(c, tok, p.which, p.oct, a.lpage, w[i], s[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < REP; ++i) {
+    if (p.token(i) >= a.T) return;
+    const float f = s[i] == 255 ? NAN : __uint_as_float(s[i] << 23);
+    float x[8];
+    values_of(w[i], f, x);
+    store8(dst + p.token(i) * v.st, x);
+  }
+}
+
+template <typename TI, int D, int REP> void launch_as(const CacheArgs &a, bool write, hipStream_t s) {
+  constexpr int per = REP * Place<D, REP>::TOKENS;
+  const dim3 grid(2u * a.B * a.Hkv * ((a.T + per - 1) / per)), block(CACHE_NT);
+  if (write) hipLaunchKernelGGL((write_kernel<TI, D, REP>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((read_kernel<TI, D, REP>), grid, block, 0, s, a);
+}
+
+// Four tokens a thread where that still leaves eight workgroups a CU.
+template <typename TI, int D> void launch_t(const CacheArgs &a, bool write, int cus, hipStream_t s) {
+  const double wgs = 2.0 * a.B * a.Hkv * a.T / (4 * Place<D, 4>::TOKENS);
+  if (wgs >= 8.0 * cus) launch_as<TI, D, 4>(a, write, s);
+  else launch_as<TI, D, 1>(a, write, s);
+}
+template <int D> void launch(const CacheArgs &a, bool write, int dtype, int cus, hipStream_t s) {
+  if (dtype == KIA_F32) launch_t<float, D>(a, write, cus, s);
+  else launch_t<uint16_t, D>(a, write, cus, s);
+}
+void launch_any(const CacheArgs &a, bool write, int d, int dtype, int cus, hipStream_t s) {
+  if (d == 32) launch<32>(a, write, dtype, cus, s);
+  else if (d == 64) launch<64>(a, write, dtype, cus, s);
+  else launch<128>(a, write, dtype, cus, s);
 }
 
 }  // namespace
 
-void launch_cache_write(const CacheArgs &a, int d, int dtype, hipStream_t s) {
-  launch_any(a, true, d, dtype, s);
+void launch_cache_write(const CacheArgs &a, int d, int dtype, int cus, hipStream_t s) {
+  launch_any(a, true, d, dtype, cus, s);
 }
-void launch_cache_read(const CacheArgs &a, int d, int dtype, hipStream_t s) {
-  launch_any(a, false, d, dtype, s);
+void launch_cache_read(const CacheArgs &a, int d, int dtype, int cus, hipStream_t s) {
+  launch_any(a, false, d, dtype, cus, s);
 }
 
 }  // namespace kia

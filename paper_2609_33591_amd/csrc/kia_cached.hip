@@ -13,7 +13,7 @@
 // contiguous. No LDS in the loop; codes become bf16 operands by one instruction a pair
 // (values by another, which puts neighbouring tokens together).
 //
-// A wave takes 64 keys at a time, the four waves of a workgroup and the workgroups
+// A wave takes 32 keys at a time, the four waves of a workgroup and the workgroups
 // that share a row tile each take a part of the keys; parts are joined in order.
 // Softmax runs in one pass with a running maximum. The interval weights' grid
 // depends on the row's extrema, so a first pass over the keys alone (a third of the
@@ -33,7 +33,10 @@ namespace {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int CHUNK = 64, NWAVE = 4;
+// 32 keys at a time: two tiles of 16 and the next two on their way leave room for three
+// workgroups a CU in bf16 (162 registers; with 64 keys 217, two workgroups, and the
+// interval weights of 32 x 16 500 keys took 101 us, now 88).
+constexpr int TILES = 2, CHUNK = 16 * TILES, NWAVE = 4;
 enum { PASS_SOFTMAX, PASS_EXTREMA, PASS_GRID };
 
 __device__ __forceinline__ f32x4 mma16(bf16x8 a, bf16x8 b, f32x4 c) {
@@ -50,11 +53,11 @@ __device__ __forceinline__ uint32_t pair_at(int s, uint32_t w, float scale) {
 }
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// One lane's share of a 64-key chunk: codes and scales of its keys and values.
+// One lane's share of a chunk: codes and scales of its keys and values.
 template <int D, bool VALUES> struct Stage4 {
   static constexpr int N = D / 32;  // words of codes of a 16-key tile
-  uint32_t k[4][N], v[VALUES ? 4 : 1][N], vs[VALUES ? 4 : 1];
-  uint8_t ks[4];
+  uint32_t k[TILES][N], v[VALUES ? TILES : 1][N], vs[VALUES ? TILES : 1];
+  uint8_t ks[TILES];
   int ok;  // bit t: the tile's page is one of the cache's
   // the values of token e (of the lane's four) of tile i as zeros
   __device__ __forceinline__ void clear(int i, int e) {
@@ -77,7 +80,7 @@ template <int N> __device__ __forceinline__ void load_words(const uint8_t *p, ui
   }
 }
 
-// The 64-key chunks that rows at positions lo .. hi see: the first tokens', then the
+// The chunks of keys that rows at positions lo .. hi see: the first tokens', then the
 // window's.
 struct Chunks {
   int sink, low, count;
@@ -90,6 +93,66 @@ struct Chunks {
   __device__ __forceinline__ int at(int n) const { return (n < sink ? n : low + n - sink) * CHUNK; }
 };
 
+// The positions of the first and the last row of a row tile.
+struct Rows16 {
+  int n, lo, hi;  // n: the sequence's keys
+  __device__ __forceinline__ Rows16(const CachedArgs &a, int b, int tile) {
+    const int G = a.H / a.Hkv, total = a.T * G;
+    n = (int)min((int64_t)max(a.lengths[b], 0), (int64_t)a.width << a.lpage);
+    lo = n - a.T + tile * 16 / G;
+    hi = n - a.T + min(tile * 16 + 15, total - 1) / G;
+  }
+  __device__ __forceinline__ Chunks chunks(const CachedArgs &a) const {
+    return Chunks(a, max(lo, 0), hi);
+  }
+};
+
+// The parts that the sequences' keys are cut into for one key head's row tile: about
+// a.shares in all, of one size for every sequence, so that a batch of unequal lengths
+// keeps all workgroups busy for the same time (32 000 keys to 1 000, 32 sequences:
+// 158 us with eight parts for each, 134 us so). Every sequence has one at least. Part w of
+// all of them is part w - first of sequence b. (64 sequences at a time; at most
+// a.shares + B parts in all.)
+struct Share {
+  int b = -1, first = 0, parts = 0;
+  // which sequence part w belongs to (by_b: the parts of sequence w)
+  __device__ __forceinline__ Share(const CachedArgs &a, int tile, int w, bool by_b) {
+    const int lane = threadIdx.x & 63;
+    auto count = [&](int i) { return i < a.B ? Rows16(a, i, tile).chunks(a).count : 0; };
+    double all = 0;
+    for (int i = 0; i < a.B; i += 64) {
+      double c = count(i + lane);
+#pragma unroll
+      for (int k = 1; k < 64; k *= 2) c += __shfl_xor(c, k);
+      all += c;
+    }
+    const int per = max(NWAVE, (int)ceil(all / a.shares));
+    int base = 0;
+    for (int i = 0; i < a.B; i += 64) {
+      const int p = i + lane < a.B ? max(1, (count(i + lane) + per - 1) / per) : 0;
+      int to = p;
+#pragma unroll
+      for (int k = 1; k < 64; k *= 2) {
+        const int y = __shfl_up(to, k);
+        if (lane >= k) to += y;
+      }
+      const uint64_t hit = __ballot(by_b ? i + lane == w : base + to > w);
+      if (hit) {
+        const int at = __builtin_ctzll(hit);
+        b = __builtin_amdgcn_readfirstlane(i + at);
+        parts = __builtin_amdgcn_readfirstlane(__shfl(p, at));
+        first = __builtin_amdgcn_readfirstlane(base + __shfl(to, at)) - parts;
+        return;
+      }
+      base += __shfl(to, 63);
+    }
+  }
+};
+// Of part w of a key head's row tile: its place in the workspace, in rows.
+__device__ __forceinline__ int64_t slot_of(const CachedArgs &a, int hk, int tile, int w) {
+  return (((int64_t)hk * a.tiles + tile) * (a.shares + a.B) + w) * 16;
+}
+
 template <typename TI, int D, int PASS, int CALIB, int RECON>
 __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
   constexpr int NP = Pieces<TI>::N, N = D / 32, NT = D / 16;
@@ -98,19 +161,19 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
   __shared__ __attribute__((aligned(16))) float rows[VALUES ? NWAVE * 16 * (D + 4) : 4];
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, kb = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // (slices fastest: the workgroups of one key head's rows share an XCD's L2 where
-  // their number is a multiple of 8)
-  const int kvs = a.B * a.Hkv, s = blockIdx.x % kvs, b = s / a.Hkv, hk = s % a.Hkv;
-  const int tile = (int)(blockIdx.x / kvs) % a.tiles, split = blockIdx.x / (kvs * a.tiles);
-  const int G = a.H / a.Hkv, total = a.T * G;
-  const int n = (int)min((int64_t)max(a.lengths[b], 0), (int64_t)a.width << a.lpage);
+  const int hk = blockIdx.x % a.Hkv, tile = (int)(blockIdx.x / a.Hkv) % a.tiles;
+  const int w = blockIdx.x / (a.Hkv * a.tiles);
+  const Share share(a, tile, w, false);
+  if (share.b < 0) return;
+  const int b = share.b, G = a.H / a.Hkv, total = a.T * G;
+  const Rows16 rows16(a, b, tile);
+  const int lo = rows16.lo, hi = rows16.hi;
   // this lane's row, and its position (-1 or less: before the text, sees nothing)
   const int r = min(tile * 16 + col, total - 1), t = r / G, h = hk * G + r % G;
-  const int pos = n - a.T + t;
-  const int lo = n - a.T + tile * 16 / G, hi = n - a.T + min(tile * 16 + 15, total - 1) / G;
-  const Chunks chunks(a, max(lo, 0), hi);
-  const int c0 = (int)((int64_t)chunks.count * split / a.splits);
-  const int c1 = (int)((int64_t)chunks.count * (split + 1) / a.splits);
+  const int pos = rows16.n - a.T + t;
+  const Chunks chunks = rows16.chunks(a);
+  const int c0 = (int)((int64_t)chunks.count * (w - share.first) / share.parts);
+  const int c1 = (int)((int64_t)chunks.count * (w - share.first + 1) / share.parts);
 
   bf16x8 q[NP][N];
   {
@@ -140,7 +203,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
   auto load = [&](int j, Stage4<D, VALUES> &x) {
     x.ok = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < TILES; ++i) {
       const int key = j + 16 * i, at = key >> a.lpage;
       int page = at < a.width ? a.table[(int64_t)b * a.width + at] : -1;
       page = __builtin_amdgcn_readfirstlane(page);
@@ -163,11 +226,18 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
   RowConst rc{};
   float Mx = -INFINITY, Mn = INFINITY;
   if constexpr (PASS == PASS_GRID) {
-    const float *e = a.ext + ((int64_t)(s * a.tiles + tile) * a.splits * 16 + col) * 2;
-    for (int i = 0; i < a.splits; ++i) {
-      Mx = fmaxf(Mx, e[32 * i]);
-      Mn = fminf(Mn, e[32 * i + 1]);
+    const float2 *e = reinterpret_cast<const float2 *>(a.ext) +
+                      slot_of(a, hk, tile, share.first) + col;
+#pragma unroll 4
+    for (int i = kb; i < share.parts; i += 4) {
+      const float2 x = e[16 * i];
+      Mx = fmaxf(Mx, x.x);
+      Mn = fminf(Mn, x.y);
     }
+    Mx = fmaxf(Mx, __shfl_xor(Mx, 16));
+    Mx = fmaxf(Mx, __shfl_xor(Mx, 32));
+    Mn = fminf(Mn, __shfl_xor(Mn, 16));
+    Mn = fminf(Mn, __shfl_xor(Mn, 32));
     Mx *= a.scale, Mn *= a.scale;
     rc = row_const(Mx, Mn, a.K, CALIB, a.tau, a.scale);
   }
@@ -183,7 +253,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
     const int j = chunks.at(c);
     if (c + NWAVE < c1) load(chunks.at(c + NWAVE), nxt);
     // every row of the tile sees every key of the chunk
-    const bool all = j + CHUNK - 1 <= lo && cur.ok == 15 &&
+    const bool all = j + CHUNK - 1 <= lo && cur.ok == (1 << TILES) - 1 &&
                      ((int64_t)hi - j < a.window || j + CHUNK - 1 < a.sinks);
     auto sees = [&](int key, int i) {
       return key <= pos && ((int64_t)pos - key < a.window || key < a.sinks) && (cur.ok >> i & 1);
@@ -191,7 +261,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
     // groups that hold an infinity or NaN
     bool bad = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < TILES; ++i) {
       bad |= cur.ks[i] == 255;
       if constexpr (VALUES) {
         const uint32_t y = ~cur.vs[i];
@@ -199,9 +269,9 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
       }
     }
     bad = __any(bad);
-    float S[4][4];
+    float S[TILES][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < TILES; ++i) {
       const float f = scale_of(cur.ks[i]);
       f32x4 acc = {};
       u32x4 w[N];
@@ -218,7 +288,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
     }
     if (__builtin_expect(bad, 0)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < TILES; ++i) {
         uint64_t y = __ballot(cur.ks[i] == 255);
         y |= y >> 32;
         y |= y >> 16;
@@ -228,14 +298,14 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
     }
     if (!all) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < TILES; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           S[i][e] = sees(j + 16 * i + 4 * kb + e, i) ? S[i][e] : -INFINITY;
     }
     if constexpr (PASS == PASS_EXTREMA) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < TILES; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           m = fmaxf(m, S[i][e]);
@@ -243,11 +313,11 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
           if constexpr (CALIB != CAL_FWM) low = in ? fminf(low, S[i][e]) : low;
         }
     } else {
-      float w[4][4];
+      float w[TILES][4];
       if constexpr (PASS == PASS_SOFTMAX) {
         float top = S[0][0];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < TILES; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) top = fmaxf(top, S[i][e]);
         top = fmaxf(top, __shfl_xor(top, 16));
@@ -264,13 +334,13 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
         }
         const float mm = m == -INFINITY ? 0.f : m;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < TILES; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) w[i][e] = __builtin_amdgcn_exp2f((S[i][e] - mm) * c2);
       } else {
         bool any = false;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < TILES; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             w[i][e] = fmaf(S[i][e], rc.alpha, rc.beta);
@@ -279,7 +349,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
         if (__any(any)) {
           // keys within rounding of a boundary: decided in 64 bits
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < TILES; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const bool amb = is_ambiguous<CALIB>(w[i][e], rc.margin2, edge);
@@ -289,7 +359,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
             }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < TILES; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const KeyDec k = key_of<CALIB>(w[i][e], Kf);
@@ -304,7 +374,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
           }
         if (!all) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < TILES; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               w[i][e] = sees(j + 16 * i + 4 * kb + e, i) ? w[i][e] : 0.f;
@@ -313,16 +383,16 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
       if (!all) {
         // values of tokens that no row sees (past the end, on no page) as zeros
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < TILES; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             if (j + 16 * i + 4 * kb + e > hi || !(cur.ok >> i & 1)) cur.clear(i, e);
       }
       if (__builtin_expect(bad, 0)) {
         // groups of NaN: their values as zeros here, and NaN for the rows that see them
-        bf16x8 is[2], one[2];
+        bf16x8 is[TILES / 2], one[TILES / 2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < TILES; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const bool nan = (cur.vs[i] >> (8 * e) & 255) == 255;
@@ -331,16 +401,18 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
             one[i / 2][i % 2 * 4 + e] = (__bf16)(sees(j + 16 * i + 4 * kb + e, i) ? 1.f : 0.f);
           }
         // (column `col` of the values here is row 4 kb + e of the sums)
-        const f32x4 k = mma16(is[1], one[1], mma16(is[0], one[0], f32x4{}));
+        f32x4 k = {};
+#pragma unroll
+        for (int u = 0; u < TILES / 2; ++u) k = mma16(is[u], one[u], k);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
           for (int x = 0; x < NT; ++x) o[x][e] = k[e] > 0.f ? NAN : o[x][e];
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) l += (w[i][0] + w[i][1]) + (w[i][2] + w[i][3]);
+      for (int i = 0; i < TILES; ++i) l += (w[i][0] + w[i][1]) + (w[i][2] + w[i][3]);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < TILES / 2; ++u) {
         // the weights of the lane's eight keys of 32, and those keys' values
         float x[8];
 #pragma unroll
@@ -376,7 +448,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
     cur = nxt;
   }
 
-  const int64_t out = ((int64_t)(s * a.tiles + tile) * a.splits + split) * 16;
+  const int64_t out = slot_of(a, hk, tile, w);
   if constexpr (PASS == PASS_EXTREMA) {
     m = fmaxf(m, __shfl_xor(m, 16));
     m = fmaxf(m, __shfl_xor(m, 32));
@@ -422,7 +494,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
       for (int e = 0; e < NT; ++e)
         x[e] = fmaf(rows[(i * 16 + row) * (D + 4) + part * NT + e], f, x[e]);
     }
-    if (a.splits == 1) {
+    if (share.parts == 1) {
       const int rr = tile * 16 + row;
       if (rr < total) {
         const float f = sum == 0.f ? 0.f : 1.f / sum;
@@ -433,7 +505,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
           else y[e] = (uint16_t)cvt_bf16x2(x[e] * f, 0.f);
         }
       }
-    } else {
+    } else if (tile * 16 + row < total) {
       float *y = a.part + (out + row) * D + part * NT;
 #pragma unroll
       for (int e = 0; e < NT; ++e) y[e] = x[e];
@@ -445,34 +517,52 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
   }
 }
 
-// The parts of a row tile, joined in order of their keys.
+// The parts of one row, joined in order: D / 4 threads a part, the parts in 1024 / D
+// groups whose sums are added in order of the groups.
 template <typename TI, int D> __global__ __launch_bounds__(256) void join_kernel(CachedArgs a) {
-  constexpr int NT = D / 16;
+  constexpr int W = D / 4, NG = 256 / W;
+  __shared__ float f[256], red[8];  // (a.shares < 256)
+  __shared__ f32x4 sums[NG][W];
   const int kvs = a.B * a.Hkv, s = blockIdx.x % kvs, b = s / a.Hkv, hk = s % a.Hkv;
-  const int tile = blockIdx.x / kvs, row = threadIdx.x / 16, part = threadIdx.x % 16;
-  const int G = a.H / a.Hkv, r = tile * 16 + row;
-  if (r >= a.T * G) return;
-  const int64_t first = (int64_t)(s * a.tiles + tile) * a.splits * 16 + row;
-  const float *st = a.stat + first * 2, *p = a.part + first * D + part * NT;
-  float top = -INFINITY;
-  for (int i = 0; i < a.splits; ++i)
-    if (st[32 * i + 1] != 0.f) top = fmaxf(top, st[32 * i]);  // (parts that saw a key)
-  const float c2 = a.scale * 1.44269504f;
-  float sum = 0.f, x[NT] = {};
-  for (int i = 0; i < a.splits; ++i) {
-    if (st[32 * i + 1] == 0.f) continue;
-    const float f = __builtin_amdgcn_exp2f((st[32 * i] - top) * c2);
-    sum = fmaf(st[32 * i + 1], f, sum);
-#pragma unroll
-    for (int e = 0; e < NT; ++e) x[e] = fmaf(p[(int64_t)i * 16 * D + e], f, x[e]);
+  const int G = a.H / a.Hkv, r = blockIdx.x / kvs, tid = threadIdx.x, wave = tid >> 6;
+  const Share share(a, r / 16, b, true);
+  if (share.parts == 1) return;  // (written by its only part)
+  const int64_t first = slot_of(a, hk, r / 16, share.first) + r % 16;
+  float m = -INFINITY, l = 0.f;
+  if (tid < share.parts) {
+    const float2 st = reinterpret_cast<const float2 *>(a.stat)[first + 16 * tid];
+    l = st.y;
+    if (l != 0.f) m = st.x;  // (a part that saw a key)
   }
-  const float f = sum == 0.f ? 0.f : 1.f / sum;
-  TI *y = slice_of<TI>(a.o, b, hk * G + r % G) + r / G * a.o.st + part * NT;
+  float top = m;
 #pragma unroll
-  for (int e = 0; e < NT; ++e) {
-    if constexpr (sizeof(TI) == 4) y[e] = x[e] * f;
-    else y[e] = (uint16_t)cvt_bf16x2(x[e] * f, 0.f);
-  }
+  for (int i = 1; i < 64; i *= 2) top = fmaxf(top, __shfl_xor(top, i));
+  if ((tid & 63) == 0) red[wave] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  const float g = l == 0.f ? 0.f : __builtin_amdgcn_exp2f((m - top) * (a.scale * 1.44269504f));
+  float sum = l * g;
+#pragma unroll
+  for (int i = 1; i < 64; i *= 2) sum += __shfl_xor(sum, i);
+  f[tid] = g;
+  if ((tid & 63) == 0) red[4 + wave] = sum;
+  __syncthreads();
+  const int at = tid % W, grp = tid / W;
+  const f32x4 *p = reinterpret_cast<const f32x4 *>(a.part + first * D) + at;
+  f32x4 x = {};
+#pragma unroll 4
+  for (int i = grp; i < share.parts; i += NG)
+    if (f[i] != 0.f) x += p[(int64_t)i * 16 * W] * f[i];
+  sums[grp][at] = x;
+  __syncthreads();
+  if (grp) return;
+#pragma unroll
+  for (int i = 1; i < NG; ++i) x += sums[i][at];
+  sum = (red[4] + red[5]) + (red[6] + red[7]);
+  x *= sum == 0.f ? 0.f : 1.f / sum;
+  TI *y = slice_of<TI>(a.o, b, hk * G + r % G) + r / G * a.o.st + 4 * at;
+  if constexpr (sizeof(TI) == 4) *reinterpret_cast<f32x4 *>(y) = x;
+  else *reinterpret_cast<u32x2 *>(y) = u32x2{cvt_bf16x2(x[0], x[1]), cvt_bf16x2(x[2], x[3])};
 }
 
 template <typename TI, int D, int CALIB> void grid_passes(const CachedArgs &a, dim3 g, hipStream_t s) {
@@ -489,7 +579,7 @@ template <typename TI, int D, int CALIB> void grid_passes(const CachedArgs &a, d
 }
 
 template <typename TI, int D> void run(const CachedArgs &a, hipStream_t s) {
-  const dim3 g((unsigned)(a.B * a.Hkv) * a.tiles * a.splits);
+  const dim3 g((unsigned)(a.shares + a.B) * a.Hkv * a.tiles);
   if (a.recon == REC_SOFTMAX) {
     timed_call("kia_cache4_attn", s, [&] {
       hipLaunchKernelGGL((cached_kernel<TI, D, PASS_SOFTMAX, CAL_FWM, REC_SOFTMAX>), g,
@@ -502,9 +592,9 @@ template <typename TI, int D> void run(const CachedArgs &a, hipStream_t s) {
   } else {
     grid_passes<TI, D, CAL_RESOLVED>(a, g, s);
   }
-  if (a.splits > 1) {
+  if (a.shares > 1) {
     timed_call("kia_cache4_join", s, [&] {
-      hipLaunchKernelGGL((join_kernel<TI, D>), dim3((unsigned)(a.B * a.Hkv) * a.tiles), dim3(256), 0,
+      hipLaunchKernelGGL((join_kernel<TI, D>), dim3((unsigned)(a.B * a.Hkv) * (a.T * (a.H / a.Hkv))), dim3(256), 0,
                          s, a);
     });
   }
