@@ -48,52 +48,86 @@ def declare(lib):
 
 
 # ---- checks -------------------------------------------------------------------
-def _dtype(q):
+# (What goes by shapes, strides and types alone is looked up: a serving loop repeats it
+# call after call, and a call for a token is as long as its host work.)
+@functools.lru_cache(maxsize=4096)
+def _fit(shape, stride, dtype):
+    """The strides of B, heads and T of a tensor's layout, or why the kernels cannot
+    take it."""
     import torch
-    if q.dtype == torch.float32:
-        return 0
-    if q.dtype == torch.bfloat16:
-        return 1
-    raise KiaError(f"tensors must be float32 or bfloat16, got {q.dtype}")
-
-
-def _unsuited(t):
-    """Why the kernels cannot take the tensor's layout (None: they can)."""
-    B, H, T, d = t.shape
-    sb, sh, st, sd = t.stride()
-    unit = 16 // t.element_size()
+    if len(shape) != 4:
+        return f"must be [B, heads, T, d], got shape {tuple(shape)}"
+    if dtype not in (torch.float32, torch.bfloat16):
+        return f"must be float32 or bfloat16, got {dtype}"
+    B, H, T, d = shape
+    sb, sh, st, sd = stride
+    unit = 4 if dtype == torch.float32 else 8
     if sd != 1:
         return "has channels that are not contiguous"
     if T > 1 and (st < d or st % unit or st > 1 << 22):
         return f"has rows {st} elements apart"
-    if (H > 1 and sh % unit) or (B > 1 and sb % unit) or t.data_ptr() % 16:
+    if (H > 1 and sh % unit) or (B > 1 and sb % unit):
         return "is not 16-byte aligned"
-    return None
+    return sb, sh, st
 
 
-def _view(name, t, like, heads=None, out=False):
-    """A tensor as a kia_view: of like's type, device, batch and tokens, with
-    `heads` heads (None: like's)."""
-    if t.dim() != 4:
-        raise KiaError(f"{name} must be [B, heads, T, d], got shape {tuple(t.shape)}")
-    if t is not like:
-        B, H, T, d = like.shape
-        want = (B, H if heads is None else heads, T, d)
-        if tuple(t.shape) != want:
-            raise KiaError(f"{name} has shape {tuple(t.shape)}, expected {want}")
-        if t.dtype != like.dtype:
-            raise KiaError(f"{name} has dtype {t.dtype}, expected {like.dtype}")
-        if t.device != like.device:
-            raise KiaError(f"{name} is on {t.device}, expected {like.device}")
-    if not t.is_cuda:
-        raise KiaError("libkia takes device tensors only")
-    why = _unsuited(t)
-    if why:
-        raise KiaError(f"{name} {why}")
-    sb, sh, st, _ = t.stride()
-    if out and ((t.shape[0] > 1 and sb == 0) or (t.shape[1] > 1 and sh == 0)):
-        raise KiaError(f"{name} is written to and must not be expanded")
-    return View(t.data_ptr(), sb, sh, st)
+@functools.lru_cache(maxsize=4096)
+def _dense(shape):
+    B, H, T, d = shape
+    return H * T * d, T * d, d
+
+
+class _Like:
+    """What every tensor of a call has in common: the first one's type and device,
+    batch, tokens and channels."""
+    __slots__ = ("shape", "dtype", "device", "code")
+
+    def __init__(self, name, t):
+        import torch
+        if t.dim() != 4:
+            raise KiaError(f"{name} must be [B, heads, T, d], got shape {tuple(t.shape)}")
+        self.shape, self.dtype, self.device = t.shape, t.dtype, t.device
+        if self.dtype == torch.float32:
+            self.code = 0
+        elif self.dtype == torch.bfloat16:
+            self.code = 1
+        else:
+            raise KiaError(f"tensors must be float32 or bfloat16, got {self.dtype}")
+
+    def view(self, name, t, heads=None, out=False):
+        """A tensor as a kia_view, with `heads` heads (None: the first one's)."""
+        want = self.shape if heads is None else (self.shape[0], heads, self.shape[2], self.shape[3])
+        if t.shape != want:
+            raise KiaError(f"{name} has shape {tuple(t.shape)}, expected {tuple(want)}")
+        if t.dtype != self.dtype:
+            raise KiaError(f"{name} has dtype {t.dtype}, expected {self.dtype}")
+        if t.device != self.device:
+            raise KiaError(f"{name} is on {t.device}, expected {self.device}")
+        fit, ptr = _fit(t.shape, t.stride(), t.dtype), t.data_ptr()
+        if type(fit) is str or ptr % 16:
+            raise KiaError(f"{name} {fit if type(fit) is str else 'is not 16-byte aligned'}")
+        if out and ((want[0] > 1 and fit[0] == 0) or (want[1] > 1 and fit[1] == 0)):
+            raise KiaError(f"{name} is written to and must not be expanded")
+        return View(ptr, *fit)
+
+    def take(self, name, t, heads=None):
+        """view() of a tensor to be read, or of a contiguous copy where the kernels
+        cannot take its layout (kept alive by the caller: (tensor, view))."""
+        import torch
+        want = self.shape if heads is None else (self.shape[0], heads, self.shape[2], self.shape[3])
+        if t.shape == want and t.dtype == self.dtype and t.device == self.device:
+            fit, ptr = _fit(t.shape, t.stride(), t.dtype), t.data_ptr()
+            if type(fit) is tuple and ptr % 16 == 0:
+                return t, View(ptr, *fit)
+            t = t.clone(memory_format=torch.contiguous_format)
+        return t, self.view(name, t, heads)
+
+
+def _new(ref):
+    """A new contiguous tensor of ref's shape and its view."""
+    import torch
+    t = torch.empty_like(ref, memory_format=torch.contiguous_format)
+    return t, View(t.data_ptr(), *_dense(t.shape))
 
 
 def _heads(q, k):
@@ -107,10 +141,10 @@ def _ints(name, t, shape, device):
     import torch
     if t is None:
         return None
-    if not torch.is_tensor(t) or t.dtype != torch.int32:
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32:
         raise KiaError(f"{name} must be an int32 tensor")
-    if tuple(t.shape) != shape:
-        raise KiaError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    if t.shape != shape:
+        raise KiaError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.device != device:
         raise KiaError(f"{name} is on {t.device}, expected {device}")
     if not t.is_contiguous():
@@ -119,41 +153,40 @@ def _ints(name, t, shape, device):
 
 
 def _buffer(name, t, dtype, least, device, align):
-    import torch
     if t.dtype != dtype or not t.is_contiguous() or t.device != device:
         raise KiaError(f"{name} must be a contiguous {dtype} tensor on {device}")
     if t.numel() < least:
         raise KiaError(f"{name} holds {t.numel()} elements, the call needs {least}")
-    if t.data_ptr() % align:
+    ptr = t.data_ptr()
+    if ptr % align:
         raise KiaError(f"{name} must be {align}-byte aligned")
-    return t.data_ptr()
+    return ptr
 
 
 def _call(fn, device, stream, *args):
     """The call on `device`, on its current stream if none is given."""
     import torch
+    if device.type != "cuda":
+        raise KiaError("libkia takes device tensors only")
     if stream is not None and getattr(stream, "device", device) != device:
         raise KiaError(f"the stream is on {stream.device}, the tensors on {device}")
     if torch._C._cuda_getDevice() == device.index:
-        _kia._check(fn(*args, _kia._stream(stream)))
+        rc = fn(*args, _kia._stream(stream))
     else:
         with torch.cuda.device(device):
-            _kia._check(fn(*args, _kia._stream(stream)))
-
-
-def _suited(t):
-    """The tensor, or a contiguous copy where the kernels cannot take its layout."""
-    return t if t.dim() != 4 or _unsuited(t) is None else t.contiguous()
+            rc = fn(*args, _kia._stream(stream))
+    if rc:
+        _kia._check(rc)
 
 
 def _int(name, x, low):
-    if isinstance(x, bool) or not isinstance(x, int) or not low <= x < 1 << 31:
+    if type(x) is not int or not low <= x < 1 << 31:
         raise KiaError(f"{name} must be an integer of at least {low}, got {x!r}")
     return x
 
 
 # ---- rotary positions -----------------------------------------------------------
-@dataclass(frozen=True)
+@dataclass(eq=False)
 class RotaryPlan:
     """Frequencies (float64 [rot / 2] on the device, radians per position), the
     layout of a pair ("half": channels n and n + rot/2; "interleaved": 2n and
@@ -200,46 +233,53 @@ def rotary_plan(rot, base=10000.0, layout="half", scaling="none", stretch=1.0, o
     return RotaryPlan(torch.tensor(freq, dtype=torch.float64, device=device), layout, factor)
 
 
-def kia_rotary(q, k, q_out, k_out, plan, positions=None, back=False, stream=None):
-    """Rotates q (and k; None: only q) into q_out (k_out), which may be q and k.
-    positions: int32 [B, T] or [T], the first position as an integer, or None
-    (0). back: by the negative angle, the gradient of the rotation."""
+def _rotary_call(like, views, Hkv, plan, positions, back, stream=None):
     import torch
-    vq = _view("q", q, q)
-    B, H, T, d = q.shape
-    vo = _view("q_out", q_out, q, out=True)
-    Hkv, vk, vy = 0, None, None
-    if k is not None:
-        Hkv = _heads(q, k)
-        vk, vy = _view("k", k, q, Hkv), _view("k_out", k_out, q, Hkv, out=True)
+    B, H, T, d = like.shape
     freq = plan.freq
     if freq.dim() != 1:
         raise KiaError("a plan's frequencies must be one-dimensional")
-    fp = _buffer("the plan's frequencies", freq, torch.float64, 1, q.device, 8)
+    fp = _buffer("the plan's frequencies", freq, torch.float64, 1, like.device, 8)
     first, ptr, sb = 0, None, 0
-    if torch.is_tensor(positions):
+    if isinstance(positions, torch.Tensor):
         if positions.dim() == 1:
-            ptr = _ints("positions", positions, (T,), q.device)
+            ptr = _ints("positions", positions, (T,), like.device)
         else:
-            ptr, sb = _ints("positions", positions, (B, T), q.device), T
+            ptr, sb = _ints("positions", positions, (B, T), like.device), T
     elif positions is not None:
-        if isinstance(positions, bool) or not isinstance(positions, int) or \
-                not -(1 << 31) <= positions < 1 << 31:
+        if type(positions) is not int or not -(1 << 31) <= positions < 1 << 31:
             raise KiaError(f"positions must be an int32 tensor or an integer, got {positions!r}")
         first = positions
     if plan.layout not in LAYOUT:
         raise KiaError(f"layout must be one of {sorted(LAYOUT)}, got {plan.layout!r}")
-    _call(_kia.load().kia_rotary, q.device, stream, vq, vo, vk, vy, ptr, sb, first, fp,
-          float(plan.factor), LAYOUT[plan.layout], int(bool(back)), B, H, Hkv, T, d,
-          2 * freq.shape[0], _dtype(q))
+    _call(_kia.load().kia_rotary, like.device, stream, *views, ptr, sb, first, fp,
+          float(plan.factor), LAYOUT[plan.layout], 1 if back else 0, B, H, Hkv, T, d,
+          2 * freq.shape[0], like.code)
+
+
+def kia_rotary(q, k, q_out, k_out, plan, positions=None, back=False, stream=None):
+    """Rotates q (and k; None: only q) into q_out (k_out), which may be q and k.
+    positions: int32 [B, T] or [T], the first position as an integer, or None
+    (0). back: by the negative angle, the gradient of the rotation."""
+    like = _Like("q", q)
+    views, Hkv = [like.view("q", q), like.view("q_out", q_out, out=True), None, None], 0
+    if k is not None:
+        Hkv = _heads(q, k)
+        views[2:] = like.view("k", k, Hkv), like.view("k_out", k_out, Hkv, True)
+    _rotary_call(like, views, Hkv, plan, positions, back, stream)
 
 
 def _rotated(q, k, plan, positions, back):
-    import torch
-    q, k = _suited(q), None if k is None else _suited(k)
-    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    k_out = None if k is None else torch.empty(k.shape, dtype=k.dtype, device=k.device)
-    kia_rotary(q, k, q_out, k_out, plan, positions, back)
+    like = _Like("q", q)
+    q, vq = like.take("q", q)
+    q_out, vo = _new(q)
+    if k is None:
+        _rotary_call(like, (vq, vo, None, None), 0, plan, positions, back)
+        return q_out, None
+    Hkv = _heads(q, k)
+    k, vk = like.take("k", k, Hkv)
+    k_out, vy = _new(k)
+    _rotary_call(like, (vq, vo, vk, vy), Hkv, plan, positions, back)
     return q_out, k_out
 
 
@@ -254,7 +294,7 @@ def _rotary_function():
         @staticmethod
         def forward(ctx, q, k, plan, positions, back):
             ctx.plan, ctx.back = plan, back
-            ctx.tensor = torch.is_tensor(positions)
+            ctx.tensor = isinstance(positions, torch.Tensor)
             if ctx.tensor:
                 ctx.save_for_backward(positions)
             else:
@@ -290,22 +330,39 @@ def kia_window_ws_bytes(B, H, Hkv, T, d, window, sinks) -> int:
     return n.value
 
 
-def _window_args(q, k, window, sinks, lengths):
-    Hkv = _heads(q, k)
-    return Hkv, _int("window", window, 1), _int("sinks", sinks, 0), \
-        _ints("lengths", lengths, (q.shape[0],), q.device)
+def _window_checked(q, k, window, sinks, lengths):
+    """(what the tensors have in common, key heads, the window, the first tokens,
+    pointer of the lengths)"""
+    like, Hkv = _Like("q", q), _heads(q, k)
+    return like, Hkv, _int("window", window, 1), _int("sinks", sinks, 0), \
+        _ints("lengths", lengths, (like.shape[0],), like.device)
+
+
+def _window_fwd(c, views, lse, stream=None):
+    like, Hkv, window, sinks, n = c
+    B, H, T, d = like.shape
+    _call(_kia.load().kia_window_fwd, like.device, stream, *views, lse, n, B, H, Hkv, T, d, window,
+          sinks, like.code)
+
+
+def _window_bwd(c, views, lse, ws, grads, stream=None):
+    import torch
+    like, Hkv, window, sinks, n = c
+    B, H, T, d = like.shape
+    lse = _buffer("lse", lse, torch.float32, B * H * T, like.device, 16)
+    _call(_kia.load().kia_window_bwd, like.device, stream, *views, lse, n, ws, *grads, B, H, Hkv, T,
+          d, window, sinks, like.code)
 
 
 def kia_window_fwd(q, k, v, o, lse, window, sinks=0, lengths=None, stream=None):
     """Forward into o (as q) and lse ([B, H, T] float32)."""
     import torch
-    Hkv, window, sinks, n = _window_args(q, k, window, sinks, lengths)
-    B, H, T, d = q.shape
-    views = (_view("q", q, q), _view("k", k, q, Hkv), _view("v", v, q, Hkv),
-             _view("o", o, q, out=True))
-    p = _buffer("lse", lse, torch.float32, B * H * T, q.device, 16)
-    _call(_kia.load().kia_window_fwd, q.device, stream, *views, p, n, B, H, Hkv, T, d, window,
-          sinks, _dtype(q))
+    c = _window_checked(q, k, window, sinks, lengths)
+    like, Hkv = c[:2]
+    B, H, T, _ = q.shape
+    views = (like.view("q", q), like.view("k", k, Hkv), like.view("v", v, Hkv),
+             like.view("o", o, out=True))
+    _window_fwd(c, views, _buffer("lse", lse, torch.float32, B * H * T, q.device, 16), stream)
 
 
 def kia_window_bwd(q, k, v, o, dO, lse, ws, dq, dk, dv, window, sinks=0, lengths=None,
@@ -313,41 +370,46 @@ def kia_window_bwd(q, k, v, o, dO, lse, ws, dq, dk, dv, window, sinks=0, lengths
     """Backward from the forward's o and lse into dq (as q), dk and dv (as k); ws:
     a uint8 device buffer of kia_window_ws_bytes bytes, 256-byte aligned."""
     import torch
-    Hkv, window, sinks, n = _window_args(q, k, window, sinks, lengths)
-    B, H, T, d = q.shape
-    ins = (_view("q", q, q), _view("k", k, q, Hkv), _view("v", v, q, Hkv), _view("o", o, q),
-           _view("dO", dO, q))
-    outs = (_view("dq", dq, q, out=True), _view("dk", dk, q, Hkv, out=True),
-            _view("dv", dv, q, Hkv, out=True))
-    p = _buffer("lse", lse, torch.float32, B * H * T, q.device, 16)
-    w = _buffer("ws", ws, torch.uint8, kia_window_ws_bytes(B, H, Hkv, T, d, window, sinks),
-                q.device, 256)
-    _call(_kia.load().kia_window_bwd, q.device, stream, *ins, p, n, w, *outs, B, H, Hkv, T, d,
-          window, sinks, _dtype(q))
+    c = _window_checked(q, k, window, sinks, lengths)
+    like, Hkv, window, sinks, _ = c
+    B, H, T, d = like.shape
+    views = (like.view("q", q), like.view("k", k, Hkv), like.view("v", v, Hkv), like.view("o", o),
+             like.view("dO", dO))
+    grads = (like.view("dq", dq, out=True), like.view("dk", dk, Hkv, True),
+             like.view("dv", dv, Hkv, True))
+    need = kia_window_ws_bytes(B, H, Hkv, T, d, window, sinks)
+    _window_bwd(c, views, lse, _buffer("ws", ws, torch.uint8, need, like.device, 256), grads, stream)
 
 
 def window_forward(q, k, v, window, sinks=0, lengths=None):
     """Allocates o and lse and runs kia_window_fwd; returns (o, lse)."""
     import torch
-    q, k, v = _suited(q), _suited(k), _suited(v)
-    _heads(q, k)
-    o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
-    kia_window_fwd(q, k, v, o, lse, window, sinks, lengths)
+    c = _window_checked(q, k, window, sinks, lengths)
+    like, Hkv = c[:2]
+    q, vq = like.take("q", q)
+    k, vk = like.take("k", k, Hkv)
+    v, vv = like.take("v", v, Hkv)
+    o, vo = _new(q)
+    lse = torch.empty(*like.shape[:3], dtype=torch.float32, device=like.device)
+    _window_fwd(c, (vq, vk, vv, vo), lse.data_ptr())
     return o, lse
 
 
 def window_backward(q, k, v, o, dO, lse, window, sinks=0, lengths=None):
     """Allocates dq, dk, dv and runs kia_window_bwd; returns (dq, dk, dv)."""
     import torch
-    q, k, v, o, dO = (_suited(x) for x in (q, k, v, o, dO))
-    Hkv, window, sinks, _ = _window_args(q, k, window, sinks, lengths)
-    B, H, T, d = q.shape
-    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    dk, dv = (torch.empty(k.shape, dtype=q.dtype, device=q.device) for _ in range(2))
+    c = _window_checked(q, k, window, sinks, lengths)
+    like, Hkv, window, sinks, _ = c
+    B, H, T, d = like.shape
+    q, vq = like.take("q", q)
+    k, vk = like.take("k", k, Hkv)
+    v, vv = like.take("v", v, Hkv)
+    o, vo = like.take("o", o)
+    dO, vg = like.take("dO", dO)
+    (dq, gq), (dk, gk), (dv, gv) = _new(q), _new(k), _new(k)
     ws = torch.empty(kia_window_ws_bytes(B, H, Hkv, T, d, window, sinks), dtype=torch.uint8,
-                     device=q.device)
-    kia_window_bwd(q, k, v, o, dO, lse, ws, dq, dk, dv, window, sinks, lengths)
+                     device=like.device)
+    _window_bwd(c, (vq, vk, vv, vo, vg), lse, ws.data_ptr(), (gq, gk, gv))
     return dq, dk, dv
 
 
@@ -399,6 +461,7 @@ PAGES = (16, 32, 64, 128, 256)
 class Cache4:
     """A paged key/value cache in 4 bits: `data`, uint8 [pages, 2, heads,
     page * (d/2 + d/32)], and the head dimension (the layout is kia.h's)."""
+    __slots__ = ("data", "d", "page", "pages", "heads")
 
     def __init__(self, data, d):
         import torch
@@ -407,11 +470,11 @@ class Cache4:
         if data.dtype != torch.uint8 or data.dim() != 4 or data.shape[1] != 2 or \
                 not data.is_contiguous():
             raise KiaError("a cache's data must be contiguous uint8 [pages, 2, heads, bytes]")
-        page, rest = divmod(data.shape[3], d // 2 + d // 32)
-        if rest or page not in PAGES or data.shape[0] < 1 or data.shape[2] < 1:
+        pages, _, heads, size = data.shape
+        page, rest = divmod(size, d // 2 + d // 32)
+        if rest or page not in PAGES or pages < 1 or heads < 1:
             raise KiaError(f"no cache of heads of {d} channels has shape {tuple(data.shape)}")
-        self.data, self.d, self.page = data, d, page
-        self.pages, self.heads = data.shape[0], data.shape[2]
+        self.data, self.d, self.page, self.pages, self.heads = data, d, page, pages, heads
 
 
 def kia_cache4_bytes(pages, page, Hkv, d) -> int:
@@ -428,70 +491,90 @@ def new_cache4(pages, heads, page, d, device="cuda"):
                               device=device), d)
 
 
-def _cache_args(cache, table, B, like):
+def _cache_args(cache, table, like, heads=None):
     """(data, pages, page, table, width) after the checks that go by the cache."""
-    if cache.data.device != like.device:
-        raise KiaError(f"the cache is on {cache.data.device}, expected {like.device}")
-    if cache.data.data_ptr() % 16:
+    import torch
+    data = cache.data
+    if data.device != like.device:
+        raise KiaError(f"the cache is on {data.device}, expected {like.device}")
+    ptr = data.data_ptr()
+    if ptr % 16:
         raise KiaError("the cache must be 16-byte aligned")
     if like.shape[3] != cache.d:
         raise KiaError(f"the cache holds heads of {cache.d} channels, got {like.shape[3]}")
-    width = table.shape[-1] if table.dim() == 2 else 0
-    return (cache.data.data_ptr(), cache.pages, cache.page,
-            _ints("table", table, (B, width), like.device), width)
+    if heads is not None and heads != cache.heads:
+        raise KiaError(f"the cache holds {cache.heads} heads, got {heads}")
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise KiaError("table must be an int32 tensor [B, width]")
+    width = table.shape[1]
+    return ptr, cache.pages, cache.page, \
+        _ints("table", table, (like.shape[0], width), like.device), width
+
+
+def _starts(name, starts, like):
+    if starts is None:
+        raise KiaError(f"{name} must be an int32 tensor")
+    return _ints(name, starts, (like.shape[0],), like.device)
+
+
+def _cache4_write(like, vk, vv, cache, table, starts, counts, stream=None):
+    B, Hkv, T, d = like.shape
+    args = _cache_args(cache, table, like, Hkv)
+    _call(_kia.load().kia_cache4_write, like.device, stream, vk, vv, *args,
+          _starts("starts", starts, like), _ints("counts", counts, (B,), like.device), B, Hkv, T, d,
+          like.code)
 
 
 def kia_cache4_write(k, v, cache, table, starts, counts=None, stream=None):
     """Writes tokens t < counts[b] (None: all) of k, v [B, heads, T, d] to positions
     starts[b] + t of the sequences whose pages table [B, width] (int32) names."""
-    vk, vv = _view("k", k, k), _view("v", v, k)
-    B, Hkv, T, d = k.shape
-    if Hkv != cache.heads:
-        raise KiaError(f"the cache holds {cache.heads} heads, got {Hkv}")
-    data, pages, page, tp, width = _cache_args(cache, table, B, k)
-    if starts is None:
-        raise KiaError("starts must be an int32 tensor")
-    _call(_kia.load().kia_cache4_write, k.device, stream, vk, vv, data, pages, page, tp, width,
-          _ints("starts", starts, (B,), k.device), _ints("counts", counts, (B,), k.device), B, Hkv,
-          T, d, _dtype(k))
+    like = _Like("k", k)
+    _cache4_write(like, like.view("k", k), like.view("v", v), cache, table, starts, counts, stream)
+
+
+def _cache4_read(like, vk, vv, cache, table, starts, counts, stream=None):
+    B, Hkv, T, d = like.shape
+    args = _cache_args(cache, table, like, Hkv)
+    _call(_kia.load().kia_cache4_read, like.device, stream, *args, _starts("starts", starts, like),
+          _ints("counts", counts, (B,), like.device), vk, vv, B, Hkv, T, d, like.code)
 
 
 def kia_cache4_read(cache, table, starts, k, v, counts=None, stream=None):
     """The values that the cache stands for at positions starts[b] + t into k, v
     [B, heads, T, d]; 0 where kia_cache4_write would have dropped the token."""
-    vk, vv = _view("k", k, k, out=True), _view("v", v, k, out=True)
-    B, Hkv, T, d = k.shape
-    if Hkv != cache.heads:
-        raise KiaError(f"the cache holds {cache.heads} heads, got {Hkv}")
-    data, pages, page, tp, width = _cache_args(cache, table, B, k)
-    if starts is None:
-        raise KiaError("starts must be an int32 tensor")
-    _call(_kia.load().kia_cache4_read, k.device, stream, data, pages, page, tp, width,
-          _ints("starts", starts, (B,), k.device), _ints("counts", counts, (B,), k.device), vk, vv,
-          B, Hkv, T, d, _dtype(k))
+    like = _Like("k", k)
+    _cache4_read(like, like.view("k", k, out=True), like.view("v", v, out=True), cache, table,
+                 starts, counts, stream)
 
 
 def cache4_write(k, v, cache, table, starts, counts=None):
     """kia_cache4_write, for tensors of any layout."""
-    kia_cache4_write(_suited(k), _suited(v), cache, table, starts, counts)
+    like = _Like("k", k)
+    k, vk = like.take("k", k)
+    v, vv = like.take("v", v)
+    _cache4_write(like, vk, vv, cache, table, starts, counts)
 
 
 def cache4_read(cache, table, starts, T, dtype, counts=None):
     """Allocates k and v [B, heads, T, d] of `dtype` and runs kia_cache4_read."""
     import torch
-    shape = (table.shape[0], cache.heads, _int("T", T, 1), cache.d)
-    k, v = (torch.empty(shape, dtype=dtype, device=cache.data.device) for _ in range(2))
-    kia_cache4_read(cache, table, starts, k, v, counts)
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise KiaError("table must be an int32 tensor [B, width]")
+    k = torch.empty(table.shape[0], cache.heads, _int("T", T, 1), cache.d, dtype=dtype,
+                    device=cache.data.device)
+    like = _Like("k", k)
+    v, vv = _new(k)
+    _cache4_read(like, View(k.data_ptr(), *_dense(k.shape)), vv, cache, table, starts, counts)
     return k, v
 
 
 @functools.lru_cache(maxsize=1024)
 def _cache4_ws_bytes(device, *args) -> int:
     import torch
-    n = ctypes.c_size_t(0)
-    with torch.cuda.device(device):
-        _kia._check(_kia.load().kia_cache4_ws_bytes(*args, ctypes.byref(n)))
-    return n.value
+    if device.type != "cuda":
+        raise KiaError("libkia takes device tensors only")
+    with torch.cuda.device(device):  # (the size goes by the device's compute units)
+        return kia_cache4_ws_bytes(*args)
 
 
 def kia_cache4_ws_bytes(page, width, B, H, Hkv, T, d, window=0, sinks=0) -> int:
@@ -501,24 +584,33 @@ def kia_cache4_ws_bytes(page, width, B, H, Hkv, T, d, window=0, sinks=0) -> int:
     return n.value
 
 
+def _cache4_checked(q, cache, table, lengths, window, sinks):
+    """(what the tensors have in common, arguments up to the lengths, bytes of workspace)"""
+    like = _Like("q", q)
+    B, H, T, d = like.shape
+    args = _cache_args(cache, table, like)
+    need = _cache4_ws_bytes(like.device, cache.page, args[4], B, H, cache.heads, T, d,
+                            _int("window", window, 0), _int("sinks", sinks, 0))
+    return like, (*args, _starts("lengths", lengths, like)), need
+
+
+def _cache4_attn(like, args, vq, vo, ws, heads, op, window, sinks, stream=None):
+    B, H, T, d = like.shape
+    K, calib, tau, recon, _, _, _ = _kia._op(*op, 0, 0, 0)
+    _call(_kia.load().kia_cache4_attn, like.device, stream, vq, vo, *args, ws, B, H, heads, T, d, K,
+          calib, tau, recon, window, sinks, like.code)
+
+
 def kia_cache4_attn(q, o, cache, table, lengths, ws, K=4, calib="fwm", tau=8.0, recon="nearest",
                     window=0, sinks=0, stream=None):
     """Attention of the last T tokens of each sequence, q [B, H, T, d], over its
     lengths[b] keys (the new tokens' own among them) into o; ws: a uint8 device
     buffer of kia_cache4_ws_bytes bytes, 256-byte aligned."""
     import torch
-    vq, vo = _view("q", q, q), _view("o", o, q, out=True)
-    B, H, T, d = q.shape
-    data, pages, page, tp, width = _cache_args(cache, table, B, q)
-    K, calib, tau, recon, _, _, _ = _kia._op(K, calib, tau, recon, 0, 0, 0)
-    window, sinks = _int("window", window, 0), _int("sinks", sinks, 0)
-    if lengths is None:
-        raise KiaError("lengths must be an int32 tensor")
-    n = _ints("lengths", lengths, (B,), q.device)
-    need = _cache4_ws_bytes(q.device, page, width, B, H, cache.heads, T, d, window, sinks)
-    w = _buffer("ws", ws, torch.uint8, need, q.device, 256)
-    _call(_kia.load().kia_cache4_attn, q.device, stream, vq, vo, data, pages, page, tp, width, n,
-          w, B, H, cache.heads, T, d, K, calib, tau, recon, window, sinks, _dtype(q))
+    like, args, need = _cache4_checked(q, cache, table, lengths, window, sinks)
+    _cache4_attn(like, args, like.view("q", q), like.view("o", o, out=True),
+                 _buffer("ws", ws, torch.uint8, need, like.device, 256), cache.heads,
+                 (K, calib, tau, recon), window, sinks, stream)
 
 
 def cache4_attention(q, cache, table, lengths, K=4, calib="fwm", tau=8.0, recon="nearest",
@@ -526,16 +618,12 @@ def cache4_attention(q, cache, table, lengths, K=4, calib="fwm", tau=8.0, recon=
     """Allocates the output (as q) and the workspace and runs kia_cache4_attn; the
     operator's arguments are those of k_interval_attention. Forward only."""
     import torch
-    if torch.is_grad_enabled() and q.requires_grad:
+    if q.requires_grad and torch.is_grad_enabled():
         raise KiaError("attention over a 4-bit cache is forward only: call it under torch.no_grad")
-    q = _suited(q)
-    if q.dim() != 4:
-        raise KiaError(f"q must be [B, H, T, d], got shape {tuple(q.shape)}")
-    B, H, T, d = q.shape
-    width = _cache_args(cache, table, B, q)[4]
-    window, sinks = _int("window", window, 0), _int("sinks", sinks, 0)
-    o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    ws = torch.empty(_cache4_ws_bytes(q.device, cache.page, width, B, H, cache.heads, T, d, window,
-                                      sinks), dtype=torch.uint8, device=q.device)
-    kia_cache4_attn(q, o, cache, table, lengths, ws, K, calib, tau, recon, window, sinks)
+    like, args, need = _cache4_checked(q, cache, table, lengths, window, sinks)
+    q, vq = like.take("q", q)
+    o, vo = _new(q)
+    ws = torch.empty(need, dtype=torch.uint8, device=like.device)
+    _cache4_attn(like, args, vq, vo, ws.data_ptr(), cache.heads,
+                 (K, calib, tau, recon), window, sinks)
     return o

@@ -161,10 +161,19 @@ def test_binding_refusals():
 
 def test_view_checks_without_a_device():
     """Layouts that the kernels cannot take are found (and copied by the allocating calls)."""
-    from paper_2609_33591_amd.around import _suited, _unsuited
+    from paper_2609_33591_amd.around import _Like
     x = torch.zeros(2, 8, 4, 64)
-    assert _unsuited(x) is None and _unsuited(x.transpose(1, 2)) is None
-    assert _suited(x.transpose(1, 2)).data_ptr() == x.data_ptr()
+    for y in (x, x.transpose(1, 2), x[:1].expand(2, 8, 4, 64)):
+        like = _Like("y", y)
+        assert like.take("y", y)[0] is y
+        v = like.view("y", y)
+        assert (v.data, v.sb, v.sh, v.st) == (y.data_ptr(), *y.stride()[:3])
     for y in (x.transpose(2, 3), torch.zeros(2, 8, 4, 65)[..., :64], torch.zeros(2, 8, 4, 66)[..., 2:],
               x[:, :, :1].expand(2, 8, 4, 64)):
-        assert _unsuited(y) is not None and _unsuited(_suited(y)) is None
+        like = _Like("y", y)
+        refuses("y ", like.view, "y", y)
+        z, v = like.take("y", y)
+        assert z is not y and torch.equal(z, y) and v.data == z.data_ptr()
+    y = torch.arange(2 * 8 * 4 * 64 + 1.0)[1:].view(2, 8, 4, 64)  # contiguous, 4 bytes off
+    assert y.is_contiguous() and _Like("y", y).take("y", y)[0] is not y
+    refuses("must not be expanded", _Like("x", x).view, "x", x[:1].expand(2, 8, 4, 64), None, True)
