@@ -19,10 +19,11 @@
 // computed operands, are rounded to bf16 (2^-8 of each), all sums and statistics are
 // fp32. fp32 runs on v_mfma_f32_32x32x2_f32 throughout and rounds nothing.
 //
-// A key that a query does not see has no influence on it, whatever it holds: its
-// score is replaced before it is used, and in blocks where some pair is masked, rows
-// that hold infinities or NaNs take part with those values as zeros, and add them
-// only to the rows that see them (mul_rows, `bad`).
+// A key that a query does not see has no influence on it, whatever it holds: its score
+// is replaced before it is used, and in tiles where some pair is masked, rows that hold
+// infinities or NaNs go to LDS with zeros in their place, and what they do to the rows
+// that see them is done apart (add_bad, bad_rows): a branch that few calls ever take,
+// kept small because its registers count for the loop it stands in.
 #include <type_traits>
 
 #include "kia_around.hpp"
@@ -68,6 +69,21 @@ template <typename TI, int D, int ROWS, int NT> struct Rows {
       const int i = tid + NT * e;
       *reinterpret_cast<u32x4 *>(dst + i / (D / V) * RS + i % (D / V) * V) = x[e];
     }
+  }
+  // infinities and NaNs as zeros
+  __device__ __forceinline__ void clean() {
+#pragma unroll
+    for (int e = 0; e < PF; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t w = x[e][i];
+        if constexpr (is_f32<TI>) {
+          x[e][i] = (w & 0x7f800000u) == 0x7f800000u ? 0u : w;
+        } else {
+          x[e][i] = ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u) |
+                    ((w & 0x00007f80u) == 0x00007f80u ? 0u : w & 0x0000ffffu);
+        }
+      }
   }
   // whether any of the thread's values is infinite or NaN
   __device__ __forceinline__ bool bad() const {
@@ -163,16 +179,41 @@ __device__ __forceinline__ f32x16 dots(const uint16_t *t, const uint16_t *b, int
 
 // acc[c][channel][row of b's side] += sum over the 32 streamed rows of their
 // channels 32 c .. times the weights w (register r: streamed row krel(r, half)).
-// `bad`: some of the rows hold infinities or NaNs, and some pairs do not count
-// (see(i): streamed row i counts for the lane's row): those values take part as zeros,
-// and are added to the rows that they count for one by one.
+template <int D, int RS, int NC>
+__device__ __forceinline__ void mul_rows(f32x16 (&acc)[NC], const uint16_t *t, const float (&w)[16],
+                                         int lane) {
+  const uint16_t *p = t + tr_base<D, RS>(lane);
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    u32x4 x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = cvt_bf16x2(w[8 * s + 2 * e], w[8 * s + 2 * e + 1]);
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      acc[c] = mfma16(tr_op<RS>(p + 16 * s * RS + 32 * c), as_op(x), acc[c]);
+  }
+}
+template <int D, int RS, int NC>
+__device__ __forceinline__ void mul_rows(f32x16 (&acc)[NC], const float *t, const float (&w)[16],
+                                         int lane) {
+  const float *p = t + 4 * (lane >> 5) * RS + (lane & 31) % D;
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) acc[c] = mfma32(p[krel0(r) * RS + 32 * c], w[r], acc[c]);
+}
+
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
-template <int D, int RS, int NC, typename TI, class See>
-__device__ __forceinline__ void add_bad(f32x16 (&acc)[NC], const TI *t, int lane, See see) {
+// The infinities and NaNs of the 32 streamed rows at `rows` (stride st, only the first
+// `count`), which mul_rows took as zeros: added to the lane's row where see(i) says
+// that streamed row i counts for it.
+template <int D, int NC, typename TI, class See>
+__device__ __forceinline__ void add_bad(f32x16 (&acc)[NC], const TI *rows, int64_t st, int count,
+                                        int lane, See see) {
 #pragma unroll 1
-  for (int i = 0; i < 32; ++i) {
+  for (int i = 0; i < min(32, count); ++i) {
     const bool ok = see(i);
-    const TI *row = t + i * RS + 4 * (lane >> 5);
+    const TI *row = rows + i * st + 4 * (lane >> 5);
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -183,53 +224,17 @@ __device__ __forceinline__ void add_bad(f32x16 (&acc)[NC], const TI *t, int lane
       }
   }
 }
-template <int D, int RS, int NC, class See>
-__device__ __forceinline__ void mul_rows(f32x16 (&acc)[NC], const uint16_t *t, const float (&w)[16],
-                                         int lane, bool bad, See see) {
-  const uint16_t *p = t + tr_base<D, RS>(lane);
-  u32x4 x[2];
-#pragma unroll
-  for (int s = 0; s < 2; ++s)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[s][e] = cvt_bf16x2(w[8 * s + 2 * e], w[8 * s + 2 * e + 1]);
-  if (!__builtin_expect(bad, 0)) {
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-        acc[c] = mfma16(tr_op<RS>(p + 16 * s * RS + 32 * c), as_op(x[s]), acc[c]);
-    return;
+// Which of those rows hold any (bit i: row i).
+template <int D, typename TI>
+__device__ __forceinline__ uint32_t bad_rows(const TI *rows, int64_t st, int count, int lane) {
+  bool bad = false;
+  if ((lane & 31) < count) {
+    const TI *row = rows + (lane & 31) * st + (lane >> 5) * (D / 2);
+#pragma unroll 1
+    for (int c = 0; c < D / 2; ++c) bad |= !finite(load1(row + c));
   }
-#pragma unroll
-  for (int s = 0; s < 2; ++s)
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      bf16x8 y = tr_op<RS>(p + 16 * s * RS + 32 * c);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = finite((float)y[e]) ? y[e] : (__bf16)0.f;
-      acc[c] = mfma16(y, as_op(x[s]), acc[c]);
-    }
-  add_bad<D, RS>(acc, t, lane, see);
-}
-template <int D, int RS, int NC, class See>
-__device__ __forceinline__ void mul_rows(f32x16 (&acc)[NC], const float *t, const float (&w)[16],
-                                         int lane, bool bad, See see) {
-  const float *p = t + 4 * (lane >> 5) * RS + (lane & 31) % D;
-  if (!__builtin_expect(bad, 0)) {
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-#pragma unroll
-      for (int c = 0; c < NC; ++c) acc[c] = mfma32(p[krel0(r) * RS + 32 * c], w[r], acc[c]);
-    return;
-  }
-#pragma unroll
-  for (int r = 0; r < 16; ++r)
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const float v = p[krel0(r) * RS + 32 * c];
-      acc[c] = mfma32(finite(v) ? v : 0.f, w[r], acc[c]);
-    }
-  add_bad<D, RS>(acc, t, lane, see);
+  const uint64_t x = __ballot(bad);
+  return (uint32_t)x | (uint32_t)(x >> 32);
 }
 
 // One lane's row from accumulators (register r of block c: channel
@@ -292,10 +297,11 @@ template <int KT> struct KeyTiles {
   __device__ __forceinline__ int at(int n) const { return (n < sink ? n : low + n - sink) * KT; }
 };
 
-template <typename TI, int D, int NW> struct FwdCfg {
-  static constexpr int KT = is_f32<TI> ? 32 : 64, NT = 64 * NW;
-  using R = Rows<TI, D, KT, NT>;
-};
+// Keys of a step, and waves per SIMD that the registers are kept to: with 64 keys a step
+// the forward needs 256 at d = 128 in bf16, with 32 its 168 leave room for a third wave.
+constexpr int KT = 32;
+template <typename TI, int D> constexpr int fwd_occ = is_f32<TI> ? (D == 128 ? 2 : 3) : D == 128 ? 3 : 4;
+template <typename TI, int D> constexpr int dq_occ = D == 128 || (is_f32<TI> && D == 64) ? 2 : 3;
 
 // One workgroup: NW groups of 32 queries of one head, over the key tiles that any of
 // them sees. Keys and values of the next tile are fetched into registers while a tile
@@ -303,10 +309,9 @@ template <typename TI, int D, int NW> struct FwdCfg {
 // The running maximum of a row moves (and its sums are scaled) only when a score
 // passes it by 2^8: sums of weights up to 2^8 lose nothing in fp32.
 template <typename TI, int D, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void win_fwd_kernel(WinArgs a) {
-  using C = FwdCfg<TI, D, NW>;
-  using R = typename C::R;
-  constexpr int KT = C::KT, NT = C::NT, SUB = KT / 32, NC = D >= 32 ? D / 32 : 1, RS = R::RS;
+__global__ __launch_bounds__(64 * NW, (fwd_occ<TI, D>)) void win_fwd_kernel(WinArgs a) {
+  using R = Rows<TI, D, KT, 64 * NW>;
+  constexpr int NC = D >= 32 ? D / 32 : 1, RS = R::RS;
   __shared__ __attribute__((aligned(16))) TI smem[4 * R::SIZE + 32];
   __shared__ int flag[2][NW];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
@@ -318,8 +323,6 @@ __global__ __launch_bounds__(64 * NW, 2) void win_fwd_kernel(WinArgs a) {
   const int i0 = (nqb - 1 - (int)(blockIdx.x / (kvs * G))) * 32 * NW;
   const int n = length_of(a, b);
   const int iw = i0 + 32 * wave, row = iw + l32;
-  TI *orow = slice_of<TI>(a.o, b, h) + row * a.o.st;
-  float *lse = a.lse + ((int64_t)b * a.H + h) * a.T;
   f32x16 acc[NC];
   clear(acc);
   float m = -INFINITY, l = 0.f;
@@ -330,40 +333,36 @@ __global__ __launch_bounds__(64 * NW, 2) void win_fwd_kernel(WinArgs a) {
     const KeyTiles<KT> tiles(a, i0, min(i0 + 32 * NW, n));
     const TI *ks = slice_of<TI>(a.k, b, hk), *vs = slice_of<TI>(a.v, b, hk);
     R fk, fv;
-    fk.fetch(ks, a.k.st, tiles.at(0), n, tid);
-    fv.fetch(vs, a.v.st, tiles.at(0), n, tid);
-    for (int p = 0; p < tiles.count; ++p) {
-      const int j = tiles.at(p);
-      TI *kb = smem + (p & 1) * 2 * R::SIZE, *vb = kb + R::SIZE;
-      fk.stash(kb, tid);
-      fv.stash(vb, tid);
-      const bool part = !sees_all(a, i0, 32 * NW, j, KT);
+    auto fetch = [&](int p) {
+      fk.fetch(ks, a.k.st, tiles.at(p), n, tid);
+      fv.fetch(vs, a.v.st, tiles.at(p), n, tid);
+    };
+    auto stage = [&](int p) {
+      TI *kb = smem + (p & 1) * 2 * R::SIZE;
+      const bool part = !sees_all(a, i0, 32 * NW, tiles.at(p), KT);
       if (part) {
         const bool bad = __any(fv.bad());
+        if (__builtin_expect(bad, 0)) fv.clean();
         if (lane == 0) flag[p & 1][wave] = bad;
       }
-      if (p + 1 < tiles.count) {
-        fk.fetch(ks, a.k.st, tiles.at(p + 1), n, tid);
-        fv.fetch(vs, a.v.st, tiles.at(p + 1), n, tid);
-      }
+      fk.stash(kb, tid);
+      fv.stash(kb + R::SIZE, tid);
+      if (p + 1 < tiles.count) fetch(p + 1);
       lds_barrier();
-      if (iw >= n || !sees_some(a, iw, 32, j, KT)) continue;
-      const bool bad = part && any_flag<NW>(flag[p & 1]);
-      f32x16 S[SUB];
-#pragma unroll
-      for (int u = 0; u < SUB; ++u) S[u] = dots<D, RS>(kb + 32 * u * RS, q, lane);
+      return part && any_flag<NW>(flag[p & 1]);
+    };
+    auto compute = [&](int p, bool bad) {
+      const int j = tiles.at(p);
+      const TI *kb = smem + (p & 1) * 2 * R::SIZE, *vb = kb + R::SIZE;
+      if (iw >= n || !sees_some(a, iw, 32, j, KT)) return;
+      f32x16 S = dots<D, RS>(kb, q, lane);
       if (!sees_all(a, iw, 32, j, KT)) {
 #pragma unroll
-        for (int u = 0; u < SUB; ++u)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            S[u][r] = sees(a, row, j + 32 * u + krel(r, half)) ? S[u][r] : -INFINITY;
+        for (int r = 0; r < 16; ++r) S[r] = sees(a, row, j + krel(r, half)) ? S[r] : -INFINITY;
       }
-      float top = S[0][0];
+      float top = S[0];
 #pragma unroll
-      for (int u = 0; u < SUB; ++u)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, S[u][r]);
+      for (int r = 1; r < 16; ++r) top = fmaxf(top, S[r]);
       top = fmaxf(top, __shfl_xor(top, 32));
       // (row by row: no row's bits depend on another's)
       const bool up = (top - m) * c2 > 8.f;
@@ -377,36 +376,40 @@ __global__ __launch_bounds__(64 * NW, 2) void win_fwd_kernel(WinArgs a) {
           for (int r = 0; r < 16; ++r) acc[c][r] *= f;
       }
       const float mm = m == -INFINITY ? 0.f : m;
+      float w[16], sum = 0.f;
 #pragma unroll
-      for (int u = 0; u < SUB; ++u) {
-        float w[16], sum = 0.f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          // (fp32: the difference first, so that the error is its own and not the score's)
-          if constexpr (is_f32<TI>) w[r] = __builtin_amdgcn_exp2f((S[u][r] - mm) * c2);
-          else w[r] = __builtin_amdgcn_exp2f(fmaf(S[u][r], c2, -mm * c2));
-          sum += w[r];
-        }
-        l += sum;
-        mul_rows<D, RS, NC>(acc, vb + 32 * u * RS, w, lane, bad,
-                            [&](int i) { return sees(a, row, j + 32 * u + i); });
+      for (int r = 0; r < 16; ++r) {
+        // (fp32: the difference first, so that the error is its own and not the score's)
+        if constexpr (is_f32<TI>) w[r] = __builtin_amdgcn_exp2f((S[r] - mm) * c2);
+        else w[r] = __builtin_amdgcn_exp2f(fmaf(S[r], c2, -mm * c2));
+        sum += w[r];
       }
+      l += sum;
+      mul_rows<D, RS>(acc, vb, w, lane);
+      if (__builtin_expect(bad, 0))
+        add_bad<D>(acc, vs + j * a.v.st, a.v.st, n - j, lane,
+                   [&](int i) { return sees(a, row, j + i); });
+    };
+    fetch(0);
+    for (int p = 0; p < tiles.count; ++p) {
+      const bool bad = stage(p);
+      compute(p, bad);
     }
   }
   if (row >= a.T) return;
   l += __shfl_xor(l, 32);
   const bool none = l == 0.f || row >= n;
-  store_row<D, NC>(orow, acc, half, none ? 0.f : 1.f / l);
-  if (half == 0) lse[row] = none ? -INFINITY : fmaf(m, a.scale, logf(l));
+  store_row<D, NC>(slice_of<TI>(a.o, b, h) + row * a.o.st, acc, half, none ? 0.f : 1.f / l);
+  if (half == 0)
+    a.lse[((int64_t)b * a.H + h) * a.T + row] = none ? -INFINITY : fmaf(m, a.scale, logf(l));
 }
 
 // dQ, and D for the key gradients. The same walk as the forward's, with the scores
 // formed again and p from lse.
 template <typename TI, int D, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void win_dq_kernel(WinArgs a) {
-  using C = FwdCfg<TI, D, NW>;
-  using R = typename C::R;
-  constexpr int KT = C::KT, SUB = KT / 32, NC = D >= 32 ? D / 32 : 1, RS = R::RS;
+__global__ __launch_bounds__(64 * NW, (dq_occ<TI, D>)) void win_dq_kernel(WinArgs a) {
+  using R = Rows<TI, D, KT, 64 * NW>;
+  constexpr int NC = D >= 32 ? D / 32 : 1, RS = R::RS;
   __shared__ __attribute__((aligned(16))) TI smem[4 * R::SIZE + 32];
   __shared__ int flag[2][NW];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
@@ -418,7 +421,6 @@ __global__ __launch_bounds__(64 * NW, 2) void win_dq_kernel(WinArgs a) {
   const int i0 = (nqb - 1 - (int)(blockIdx.x / (kvs * G))) * 32 * NW;
   const int n = length_of(a, b);
   const int iw = i0 + 32 * wave, row = iw + l32;
-  TI *dqrow = slice_of<TI>(a.dq, b, h) + row * a.dq.st;
   f32x16 acc[NC];
   clear(acc);
   if (i0 < n) {
@@ -441,47 +443,55 @@ __global__ __launch_bounds__(64 * NW, 2) void win_dq_kernel(WinArgs a) {
     const KeyTiles<KT> tiles(a, i0, min(i0 + 32 * NW, n));
     const TI *ks = slice_of<TI>(a.k, b, hk), *vs = slice_of<TI>(a.v, b, hk);
     R fk, fv;
-    fk.fetch(ks, a.k.st, tiles.at(0), n, tid);
-    fv.fetch(vs, a.v.st, tiles.at(0), n, tid);
-    for (int p = 0; p < tiles.count; ++p) {
-      const int j = tiles.at(p);
-      TI *kb = smem + (p & 1) * 2 * R::SIZE, *vb = kb + R::SIZE;
-      fk.stash(kb, tid);
-      fv.stash(vb, tid);
-      const bool part = !sees_all(a, i0, 32 * NW, j, KT);
+    auto fetch = [&](int p) {
+      fk.fetch(ks, a.k.st, tiles.at(p), n, tid);
+      fv.fetch(vs, a.v.st, tiles.at(p), n, tid);
+    };
+    auto stage = [&](int p) {
+      TI *kb = smem + (p & 1) * 2 * R::SIZE;
+      const bool part = !sees_all(a, i0, 32 * NW, tiles.at(p), KT);
       if (part) {
         const bool bad = __any(fk.bad());
+        if (__builtin_expect(bad, 0)) fk.clean();
         if (lane == 0) flag[p & 1][wave] = bad;
       }
-      if (p + 1 < tiles.count) {
-        fk.fetch(ks, a.k.st, tiles.at(p + 1), n, tid);
-        fv.fetch(vs, a.v.st, tiles.at(p + 1), n, tid);
-      }
+      fk.stash(kb, tid);
+      fv.stash(kb + R::SIZE, tid);
+      if (p + 1 < tiles.count) fetch(p + 1);
       lds_barrier();
-      if (iw >= n || !sees_some(a, iw, 32, j, KT)) continue;
-      const bool bad = part && any_flag<NW>(flag[p & 1]);
-      const bool all = sees_all(a, iw, 32, j, KT);
+      return part && any_flag<NW>(flag[p & 1]);
+    };
+    auto compute = [&](int p, bool bad) {
+      const int j = tiles.at(p);
+      const TI *kb = smem + (p & 1) * 2 * R::SIZE, *vb = kb + R::SIZE;
+      if (iw >= n || !sees_some(a, iw, 32, j, KT)) return;
+      const f32x16 S = dots<D, RS>(kb, q, lane);
+      const f32x16 P = dots<D, RS>(vb, g, lane);
+      float w[16];
 #pragma unroll
-      for (int u = 0; u < SUB; ++u) {
-        const f32x16 S = dots<D, RS>(kb + 32 * u * RS, q, lane);
-        const f32x16 P = dots<D, RS>(vb + 32 * u * RS, g, lane);
-        float w[16];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float e = is_f32<TI> ? fmaf(S[r], a.scale, -lse) * LOG2E_F : fmaf(S[r], c2, -lse2);
-          w[r] = __builtin_amdgcn_exp2f(e) * (P[r] - delta);
-        }
-        if (!all) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            w[r] = sees(a, row, j + 32 * u + krel(r, half)) ? w[r] : 0.f;
-        }
-        mul_rows<D, RS, NC>(acc, kb + 32 * u * RS, w, lane, bad,
-                            [&](int i) { return sees(a, row, j + 32 * u + i); });
+      for (int r = 0; r < 16; ++r) {
+        const float e = is_f32<TI> ? fmaf(S[r], a.scale, -lse) * LOG2E_F : fmaf(S[r], c2, -lse2);
+        w[r] = __builtin_amdgcn_exp2f(e) * (P[r] - delta);
       }
+      if (__builtin_expect(bad, 0)) {  // (a query that sees such a key has no score there)
+        const uint32_t rows = bad_rows<D>(ks + j * a.k.st, a.k.st, n - j, lane);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) w[r] = rows >> krel(r, half) & 1 ? NAN : w[r];
+      }
+      if (!sees_all(a, iw, 32, j, KT)) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) w[r] = sees(a, row, j + krel(r, half)) ? w[r] : 0.f;
+      }
+      mul_rows<D, RS>(acc, kb, w, lane);
+    };
+    fetch(0);
+    for (int p = 0; p < tiles.count; ++p) {
+      const bool bad = stage(p);
+      compute(p, bad);
     }
   }
-  if (row < a.T) store_row<D, NC>(dqrow, acc, half, row < n ? a.scale : 0.f);
+  if (row < a.T)
+    store_row<D, NC>(slice_of<TI>(a.dq, b, h) + row * a.dq.st, acc, half, row < n ? a.scale : 0.f);
 }
 
 // The key block, the part of its query range and the number of parts of a workgroup.
@@ -513,10 +523,10 @@ __global__ __launch_bounds__(256, is_f32<TI> && D == 128 ? 1 : 2) void win_dkv_k
   using R = Rows<TI, D, WIN_QT, NT>;
   constexpr int RS = R::RS;
   // queries and dO (and keys and values); then the second half's sums
-  constexpr int SMEM = (KV ? 4 : 2) * R::SIZE * sizeof(TI) + 64;
+  constexpr int ROWS = (KV ? 4 : 2) * R::SIZE * sizeof(TI) + 64;
   constexpr int RED = 2 * 64 * 2 * NC * 16 * 4;
-  __shared__ __attribute__((aligned(16))) char smem[SMEM > RED ? SMEM : RED];
-  __shared__ __attribute__((aligned(16))) float stat[2][WIN_QT];
+  __shared__ __attribute__((aligned(16))) char smem[ROWS > RED ? ROWS : RED];
+  __shared__ __attribute__((aligned(16))) float stat[2][WIN_QT];  // lse and D of the tile's rows
   __shared__ int flag[4];
   TI *qb = reinterpret_cast<TI *>(smem), *gb = qb + R::SIZE, *kb = gb + R::SIZE, *vb = kb + R::SIZE;
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
@@ -563,23 +573,26 @@ __global__ __launch_bounds__(256, is_f32<TI> && D == 128 ? 1 : 2) void win_dkv_k
         if (!wave && !is_f32<TI>) st *= LOG2E_F;
       }
     };
-    fetch(it0);
-    for (int it = it0; it < it1; ++it) {
-      const int i = j0 + it % per * WIN_QT, iw = i + 32 * qg;
+    auto stage = [&](int it) {
+      const int i = j0 + it % per * WIN_QT;
+      const bool part = !sees_all(a, i, WIN_QT, j0, WIN_KB);
+      bool bad = false;
+      if (part) {
+        bad = __any(fq.bad() | fg.bad());
+        if (__builtin_expect(bad, 0)) fq.clean(), fg.clean();
+      }
       if (it > it0) lds_barrier();
       fq.stash(qb, tid);
       fg.stash(gb, tid);
       if (wave < 2) stat[wave][lane] = st;
-      const bool part = !sees_all(a, i, WIN_QT, j0, WIN_KB);
-      if (part) {
-        const bool bad = __any(fq.bad() | fg.bad());
-        if (lane == 0) flag[wave] = bad;
-      }
+      if (part && lane == 0) flag[wave] = bad;
       if (it + 1 < it1) fetch(it + 1);
       lds_barrier();
-      if (jw >= n || iw >= n || !sees_some(a, iw, 32, jw, 32)) continue;
-      const bool bad = part && any_flag<4>(flag);
-      const bool all = sees_all(a, iw, 32, jw, 32);
+      return part && any_flag<4>(flag);
+    };
+    auto compute = [&](int it, bool bad) {
+      const int iw = j0 + it % per * WIN_QT + 32 * qg;
+      if (jw >= n || iw >= n || !sees_some(a, iw, 32, jw, 32)) return;
       const TI *qt = qb + 32 * qg * RS, *gt = gb + 32 * qg * RS;
       f32x16 S, P;
       if constexpr (KV) {
@@ -603,7 +616,7 @@ __global__ __launch_bounds__(256, is_f32<TI> && D == 128 ? 1 : 2) void win_dkv_k
           ds[r] = w[r] * (P[r] - E[e]);
         }
       }
-      if (!all) {
+      if (!sees_all(a, iw, 32, jw, 32)) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const bool ok = sees(a, iw + krel(r, half), key);
@@ -611,9 +624,17 @@ __global__ __launch_bounds__(256, is_f32<TI> && D == 128 ? 1 : 2) void win_dkv_k
           ds[r] = ok ? ds[r] : 0.f;
         }
       }
-      auto see = [&](int r) { return sees(a, iw + r, key); };
-      mul_rows<D, RS, NC>(dv, gt, w, lane, bad, see);
-      mul_rows<D, RS, NC>(dk, qt, ds, lane, bad, see);
+      mul_rows<D, RS>(dv, gt, w, lane);
+      mul_rows<D, RS>(dk, qt, ds, lane);
+      // (a query with such a value has lse or D that makes its weights NaN)
+      if (__builtin_expect(bad, 0))
+        add_bad<D>(dv, slice_of<TI>(a.dO, b, hk * G + it / per) + iw * a.dO.st, a.dO.st, n - iw,
+                   lane, [&](int r) { return sees(a, iw + r, key); });
+    };
+    fetch(it0);
+    for (int it = it0; it < it1; ++it) {
+      const bool bad = stage(it);
+      compute(it, bad);
     }
   }
   // the halves of the queries: the second hands its sums over
