@@ -24,7 +24,6 @@
 // infinities or NaNs go to LDS with zeros in their place, and what they do to the rows
 // that see them is done apart (add_bad, bad_rows): a branch that few calls ever take,
 // kept small because its registers count for the loop it stands in.
-#include <type_traits>
 
 #include "kia_around.hpp"
 #include "kia_host.hpp"
@@ -297,32 +296,71 @@ template <int KT> struct KeyTiles {
   __device__ __forceinline__ int at(int n) const { return (n < sink ? n : low + n - sink) * KT; }
 };
 
-// Keys of a step, and waves per SIMD that the registers are kept to: with 64 keys a step
-// the forward needs 256 at d = 128 in bf16, with 32 its 168 leave room for a third wave.
-constexpr int KT = 32;
-template <typename TI, int D> constexpr int fwd_occ = is_f32<TI> ? (D == 128 ? 2 : 3) : D == 128 ? 3 : 4;
-template <typename TI, int D> constexpr int dq_occ = D == 128 || (is_f32<TI> && D == 64) ? 2 : 3;
+// Launch shapes of the forward and dQ: a workgroup's four waves are RG groups of 32
+// queries times KP parts of each step's 32 KP keys. Large grids take 4 x 1: every staged
+// tile serves 128 queries, and registers that leave room for a third wave a SIMD in bf16
+// at d = 128 (168; with 64 keys a step 256). Grids too small to fill the chip give up
+// row groups for key parts, whose sums are joined in order through LDS.
+template <typename TI, int D, int RG> struct Shape {
+  static constexpr int KP = 4 / RG, KT = 32 * KP;
+  using R = Rows<TI, D, KT, 256>;
+  static constexpr int NC = D >= 32 ? D / 32 : 1;
+  static constexpr int BUF = 2 * R::SIZE * (int)sizeof(TI);  // keys and values of a step
+  static constexpr int NBUF = 2 * BUF <= 140 * 1024 ? 2 : 1;
+  static constexpr int JOIN = KP > 1 ? RG * (KP - 1) * 64 * (NC * 16 + 2) * 4 : 0;
+  static constexpr int SMEM = (NBUF * BUF > JOIN ? NBUF * BUF : JOIN) + 64;
+  static constexpr int WGS = 160 * 1024 / (SMEM + 64);  // that fit a CU's LDS
+  static constexpr int FWD = RG < 4 ? 2 : is_f32<TI> ? (D == 128 ? 2 : 3) : D == 128 ? 3 : 4;
+  static constexpr int DQ = RG < 4 || D == 128 || (is_f32<TI> && D == 64) ? 2 : 3;
+  static constexpr int FWD_OCC = FWD < WGS ? FWD : WGS, DQ_OCC = DQ < WGS ? DQ : WGS;
+};
 
-// One workgroup: NW groups of 32 queries of one head, over the key tiles that any of
+// Key parts 1 .. hand their sums (and x, y of each lane) to part 0, through LDS.
+template <int RG, int KP, int NC, class Take>
+__device__ __forceinline__ void join_parts(char *smem, const f32x16 (&acc)[NC], float x, float y,
+                                           int rg, int kp, int lane, Take take) {
+  constexpr int W = NC * 16 + 2;
+  __syncthreads();
+  float *mine = reinterpret_cast<float *>(smem) + lane;
+  if (kp > 0) {
+    float *p = mine + (rg * (KP - 1) + kp - 1) * W * 64;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p[(16 * c + r) * 64] = acc[c][r];
+    p[(W - 2) * 64] = x;
+    p[(W - 1) * 64] = y;
+  }
+  __syncthreads();
+  if (kp > 0) return;
+#pragma unroll
+  for (int k = 1; k < KP; ++k) {
+    const float *p = mine + (rg * (KP - 1) + k - 1) * W * 64;
+    take(p[(W - 2) * 64], p[(W - 1) * 64], [&](int c, int r) { return p[(16 * c + r) * 64]; });
+  }
+}
+
+// One workgroup: RG groups of 32 queries of one head, over the key tiles that any of
 // them sees. Keys and values of the next tile are fetched into registers while a tile
 // is worked on, and stored to the other of two buffers: one barrier a tile.
 // The running maximum of a row moves (and its sums are scaled) only when a score
 // passes it by 2^8: sums of weights up to 2^8 lose nothing in fp32.
-template <typename TI, int D, int NW>
-__global__ __launch_bounds__(64 * NW, (fwd_occ<TI, D>)) void win_fwd_kernel(WinArgs a) {
-  using R = Rows<TI, D, KT, 64 * NW>;
-  constexpr int NC = D >= 32 ? D / 32 : 1, RS = R::RS;
-  __shared__ __attribute__((aligned(16))) TI smem[4 * R::SIZE + 32];
-  __shared__ int flag[2][NW];
+template <typename TI, int D, int RG>
+__global__ __launch_bounds__(256, (Shape<TI, D, RG>::FWD_OCC)) void win_fwd_kernel(WinArgs a) {
+  using C = Shape<TI, D, RG>;
+  using R = typename C::R;
+  constexpr int KP = C::KP, KT = C::KT, NBUF = C::NBUF, NC = C::NC, RS = R::RS;
+  __shared__ __attribute__((aligned(16))) char smem[C::SMEM];
+  __shared__ int flag[2][4];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), rg = wave % RG, kp = wave / RG;
   const int G = a.H / a.Hkv, kvs = a.B * a.Hkv;
   const int s = blockIdx.x % kvs, b = s / a.Hkv, hk = s % a.Hkv;
   const int h = hk * G + (int)(blockIdx.x / kvs) % G;
-  const int nqb = (a.T + 32 * NW - 1) / (32 * NW);
-  const int i0 = (nqb - 1 - (int)(blockIdx.x / (kvs * G))) * 32 * NW;
+  const int nqb = (a.T + 32 * RG - 1) / (32 * RG);
+  const int i0 = (nqb - 1 - (int)(blockIdx.x / (kvs * G))) * 32 * RG;
   const int n = length_of(a, b);
-  const int iw = i0 + 32 * wave, row = iw + l32;
+  const int iw = i0 + 32 * rg, row = iw + l32;
   f32x16 acc[NC];
   clear(acc);
   float m = -INFINITY, l = 0.f;
@@ -330,16 +368,20 @@ __global__ __launch_bounds__(64 * NW, (fwd_occ<TI, D>)) void win_fwd_kernel(WinA
   if (i0 < n) {
     RowReg<TI, D> q;
     q.load(slice_of<TI>(a.q, b, h) + min(row, n - 1) * a.q.st, half, row < n);
-    const KeyTiles<KT> tiles(a, i0, min(i0 + 32 * NW, n));
+    const KeyTiles<KT> tiles(a, i0, min(i0 + 32 * RG, n));
     const TI *ks = slice_of<TI>(a.k, b, hk), *vs = slice_of<TI>(a.v, b, hk);
     R fk, fv;
+    auto buf = [&](int p) {
+      return reinterpret_cast<TI *>(smem) + (NBUF == 2 ? p & 1 : 0) * 2 * R::SIZE;
+    };
     auto fetch = [&](int p) {
       fk.fetch(ks, a.k.st, tiles.at(p), n, tid);
       fv.fetch(vs, a.v.st, tiles.at(p), n, tid);
     };
     auto stage = [&](int p) {
-      TI *kb = smem + (p & 1) * 2 * R::SIZE;
-      const bool part = !sees_all(a, i0, 32 * NW, tiles.at(p), KT);
+      TI *kb = buf(p);
+      if (NBUF == 1 && p > 0) lds_barrier();
+      const bool part = !sees_all(a, i0, 32 * RG, tiles.at(p), KT);
       if (part) {
         const bool bad = __any(fv.bad());
         if (__builtin_expect(bad, 0)) fv.clean();
@@ -349,14 +391,14 @@ __global__ __launch_bounds__(64 * NW, (fwd_occ<TI, D>)) void win_fwd_kernel(WinA
       fv.stash(kb + R::SIZE, tid);
       if (p + 1 < tiles.count) fetch(p + 1);
       lds_barrier();
-      return part && any_flag<NW>(flag[p & 1]);
+      return part && any_flag<4>(flag[p & 1]);
     };
     auto compute = [&](int p, bool bad) {
-      const int j = tiles.at(p);
-      const TI *kb = smem + (p & 1) * 2 * R::SIZE, *vb = kb + R::SIZE;
-      if (iw >= n || !sees_some(a, iw, 32, j, KT)) return;
+      const int j = tiles.at(p) + 32 * kp;
+      const TI *kb = buf(p) + 32 * kp * RS, *vb = kb + R::SIZE;
+      if (iw >= n || !sees_some(a, iw, 32, j, 32)) return;
       f32x16 S = dots<D, RS>(kb, q, lane);
-      if (!sees_all(a, iw, 32, j, KT)) {
+      if (!sees_all(a, iw, 32, j, 32)) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) S[r] = sees(a, row, j + krel(r, half)) ? S[r] : -INFINITY;
       }
@@ -396,6 +438,20 @@ __global__ __launch_bounds__(64 * NW, (fwd_occ<TI, D>)) void win_fwd_kernel(WinA
       compute(p, bad);
     }
   }
+  if constexpr (KP > 1) {
+    join_parts<RG, KP>(smem, acc, m, l, rg, kp, lane, [&](float pm, float pl, auto part) {
+      const float to = fmaxf(m, pm);
+      const float f = m == to ? 1.f : __builtin_amdgcn_exp2f((m - to) * c2);
+      const float g = pm == to ? 1.f : __builtin_amdgcn_exp2f((pm - to) * c2);
+      m = to;
+      l = l * f + pl * g;
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[c][r] = acc[c][r] * f + part(c, r) * g;
+    });
+    if (kp > 0) return;
+  }
   if (row >= a.T) return;
   l += __shfl_xor(l, 32);
   const bool none = l == 0.f || row >= n;
@@ -406,21 +462,22 @@ __global__ __launch_bounds__(64 * NW, (fwd_occ<TI, D>)) void win_fwd_kernel(WinA
 
 // dQ, and D for the key gradients. The same walk as the forward's, with the scores
 // formed again and p from lse.
-template <typename TI, int D, int NW>
-__global__ __launch_bounds__(64 * NW, (dq_occ<TI, D>)) void win_dq_kernel(WinArgs a) {
-  using R = Rows<TI, D, KT, 64 * NW>;
-  constexpr int NC = D >= 32 ? D / 32 : 1, RS = R::RS;
-  __shared__ __attribute__((aligned(16))) TI smem[4 * R::SIZE + 32];
-  __shared__ int flag[2][NW];
+template <typename TI, int D, int RG>
+__global__ __launch_bounds__(256, (Shape<TI, D, RG>::DQ_OCC)) void win_dq_kernel(WinArgs a) {
+  using C = Shape<TI, D, RG>;
+  using R = typename C::R;
+  constexpr int KP = C::KP, KT = C::KT, NBUF = C::NBUF, NC = C::NC, RS = R::RS;
+  __shared__ __attribute__((aligned(16))) char smem[C::SMEM];
+  __shared__ int flag[2][4];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), rg = wave % RG, kp = wave / RG;
   const int G = a.H / a.Hkv, kvs = a.B * a.Hkv;
   const int s = blockIdx.x % kvs, b = s / a.Hkv, hk = s % a.Hkv;
   const int h = hk * G + (int)(blockIdx.x / kvs) % G;
-  const int nqb = (a.T + 32 * NW - 1) / (32 * NW);
-  const int i0 = (nqb - 1 - (int)(blockIdx.x / (kvs * G))) * 32 * NW;
+  const int nqb = (a.T + 32 * RG - 1) / (32 * RG);
+  const int i0 = (nqb - 1 - (int)(blockIdx.x / (kvs * G))) * 32 * RG;
   const int n = length_of(a, b);
-  const int iw = i0 + 32 * wave, row = iw + l32;
+  const int iw = i0 + 32 * rg, row = iw + l32;
   f32x16 acc[NC];
   clear(acc);
   if (i0 < n) {
@@ -437,19 +494,23 @@ __global__ __launch_bounds__(64 * NW, (dq_occ<TI, D>)) void win_dq_kernel(WinArg
       const int64_t r = ((int64_t)b * a.H + h) * a.T;
       lse = row < n ? a.lse[r + row] : INFINITY;
       if (lse == -INFINITY) lse = INFINITY;  // a row of nothing: no weight anywhere
-      if (half == 0 && row < n) a.delta[r + row] = delta;
+      if (half == 0 && kp == 0 && row < n) a.delta[r + row] = delta;
     }
     const float c2 = a.scale * LOG2E_F, lse2 = lse * LOG2E_F;
-    const KeyTiles<KT> tiles(a, i0, min(i0 + 32 * NW, n));
+    const KeyTiles<KT> tiles(a, i0, min(i0 + 32 * RG, n));
     const TI *ks = slice_of<TI>(a.k, b, hk), *vs = slice_of<TI>(a.v, b, hk);
     R fk, fv;
+    auto buf = [&](int p) {
+      return reinterpret_cast<TI *>(smem) + (NBUF == 2 ? p & 1 : 0) * 2 * R::SIZE;
+    };
     auto fetch = [&](int p) {
       fk.fetch(ks, a.k.st, tiles.at(p), n, tid);
       fv.fetch(vs, a.v.st, tiles.at(p), n, tid);
     };
     auto stage = [&](int p) {
-      TI *kb = smem + (p & 1) * 2 * R::SIZE;
-      const bool part = !sees_all(a, i0, 32 * NW, tiles.at(p), KT);
+      TI *kb = buf(p);
+      if (NBUF == 1 && p > 0) lds_barrier();
+      const bool part = !sees_all(a, i0, 32 * RG, tiles.at(p), KT);
       if (part) {
         const bool bad = __any(fk.bad());
         if (__builtin_expect(bad, 0)) fk.clean();
@@ -459,12 +520,12 @@ __global__ __launch_bounds__(64 * NW, (dq_occ<TI, D>)) void win_dq_kernel(WinArg
       fv.stash(kb + R::SIZE, tid);
       if (p + 1 < tiles.count) fetch(p + 1);
       lds_barrier();
-      return part && any_flag<NW>(flag[p & 1]);
+      return part && any_flag<4>(flag[p & 1]);
     };
     auto compute = [&](int p, bool bad) {
-      const int j = tiles.at(p);
-      const TI *kb = smem + (p & 1) * 2 * R::SIZE, *vb = kb + R::SIZE;
-      if (iw >= n || !sees_some(a, iw, 32, j, KT)) return;
+      const int j = tiles.at(p) + 32 * kp;
+      const TI *kb = buf(p) + 32 * kp * RS, *vb = kb + R::SIZE;
+      if (iw >= n || !sees_some(a, iw, 32, j, 32)) return;
       const f32x16 S = dots<D, RS>(kb, q, lane);
       const f32x16 P = dots<D, RS>(vb, g, lane);
       float w[16];
@@ -478,7 +539,7 @@ __global__ __launch_bounds__(64 * NW, (dq_occ<TI, D>)) void win_dq_kernel(WinArg
 #pragma unroll
         for (int r = 0; r < 16; ++r) w[r] = rows >> krel(r, half) & 1 ? NAN : w[r];
       }
-      if (!sees_all(a, iw, 32, j, KT)) {
+      if (!sees_all(a, iw, 32, j, 32)) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) w[r] = sees(a, row, j + krel(r, half)) ? w[r] : 0.f;
       }
@@ -489,6 +550,15 @@ __global__ __launch_bounds__(64 * NW, (dq_occ<TI, D>)) void win_dq_kernel(WinArg
       const bool bad = stage(p);
       compute(p, bad);
     }
+  }
+  if constexpr (KP > 1) {
+    join_parts<RG, KP>(smem, acc, 0.f, 0.f, rg, kp, lane, [&](float, float, auto part) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[c][r] += part(c, r);
+    });
+    if (kp > 0) return;
   }
   if (row < a.T)
     store_row<D, NC>(slice_of<TI>(a.dq, b, h) + row * a.dq.st, acc, half, row < n ? a.scale : 0.f);
@@ -698,19 +768,39 @@ template <typename TI, int D> __global__ __launch_bounds__(256) void win_sum_ker
   else *reinterpret_cast<u32x2 *>(dst) = u32x2{cvt_bf16x2(x[0], x[1]), cvt_bf16x2(x[2], x[3])};
 }
 
-template <typename TI, int D> void fwd(const WinArgs &a, hipStream_t s) {
-  constexpr int NW = 4;
-  const unsigned grid = (unsigned)(a.B * a.H) * ((a.T + 32 * NW - 1) / (32 * NW));
+template <typename TI, int D, int RG> void launch_fwd(const WinArgs &a, hipStream_t s) {
+  const unsigned grid = (unsigned)(a.B * a.H) * ((a.T + 32 * RG - 1) / (32 * RG));
+  hipLaunchKernelGGL((win_fwd_kernel<TI, D, RG>), dim3(grid), dim3(256), 0, s, a);
+}
+template <typename TI, int D, int RG> void launch_dq(const WinArgs &a, hipStream_t s) {
+  const unsigned grid = (unsigned)(a.B * a.H) * ((a.T + 32 * RG - 1) / (32 * RG));
+  hipLaunchKernelGGL((win_dq_kernel<TI, D, RG>), dim3(grid), dim3(256), 0, s, a);
+}
+// Two row groups times two key parts up to a number of 128-query blocks, four row groups
+// above. Measured, forward and dQ (us, 2 x 2 / 4 x 1; sinks of 4):
+//   bf16 d = 64, T = 1024, window 256   96 blocks 12.7 / 18.9, 14.0 / 20.9; 384 17.6 / 21.3,
+//                                       20.8 / 24.5; 768 27.5 / 26.6, 33.1 / 32.3
+//   bf16 d = 128, T = 2048, window 512  256 blocks 27.6 / 33.5, 33.5 / 36.4; 512 44.7 / 40.9,
+//                                       53.6 / 49.5
+//   fp32 d = 64, T = 1024, window 256   96 blocks 24 / 42, 30 / 53; 768 90 / 91, 123 / 134
+//   fp32 d = 128, T = 1024, window 256  128 blocks 43 / 69, 57 / 115; 256 82 / 71, 111 / 118
+// (1 x 4, with 128 keys a step, gains 1 us on grids of a few blocks and loses above.)
+template <typename TI, int D> bool two_groups(const WinArgs &a, int cus) {
+  const int64_t blocks = (int64_t)a.B * a.H * ((a.T + 127) / 128);
+  return blocks <= (D == 128 ? (is_f32<TI> ? cus / 2 : cus) : is_f32<TI> ? 3 * cus : 2 * cus);
+}
+
+template <typename TI, int D> void fwd(const WinArgs &a, int cus, hipStream_t s) {
   timed_call("kia_window_fwd", s, [&] {
-    hipLaunchKernelGGL((win_fwd_kernel<TI, D, NW>), dim3(grid), dim3(64 * NW), 0, s, a);
+    if (two_groups<TI, D>(a, cus)) launch_fwd<TI, D, 2>(a, s);
+    else launch_fwd<TI, D, 4>(a, s);
   });
 }
 
-template <typename TI, int D> void bwd(const WinArgs &a, hipStream_t s) {
-  constexpr int NW = 4;
-  const unsigned grid = (unsigned)(a.B * a.H) * ((a.T + 32 * NW - 1) / (32 * NW));
+template <typename TI, int D> void bwd(const WinArgs &a, int cus, hipStream_t s) {
   timed_call("kia_window_dq", s, [&] {
-    hipLaunchKernelGGL((win_dq_kernel<TI, D, NW>), dim3(grid), dim3(64 * NW), 0, s, a);
+    if (two_groups<TI, D>(a, cus)) launch_dq<TI, D, 2>(a, s);
+    else launch_dq<TI, D, 4>(a, s);
   });
   const int nkb = (a.T + WIN_KB - 1) / WIN_KB, sb = a.sink_blocks;
   const unsigned kvs = a.B * a.Hkv;
@@ -730,13 +820,13 @@ template <typename TI, int D> void bwd(const WinArgs &a, hipStream_t s) {
 
 }  // namespace
 
-template <> void launch_win_fwd<KIA_HEAD>(const WinArgs &a, int dtype, int, hipStream_t s) {
-  if (dtype == KIA_F32) fwd<float, KIA_HEAD>(a, s);
-  else fwd<uint16_t, KIA_HEAD>(a, s);
+template <> void launch_win_fwd<KIA_HEAD>(const WinArgs &a, int dtype, int cus, hipStream_t s) {
+  if (dtype == KIA_F32) fwd<float, KIA_HEAD>(a, cus, s);
+  else fwd<uint16_t, KIA_HEAD>(a, cus, s);
 }
-template <> void launch_win_bwd<KIA_HEAD>(const WinArgs &a, int dtype, int, hipStream_t s) {
-  if (dtype == KIA_F32) bwd<float, KIA_HEAD>(a, s);
-  else bwd<uint16_t, KIA_HEAD>(a, s);
+template <> void launch_win_bwd<KIA_HEAD>(const WinArgs &a, int dtype, int cus, hipStream_t s) {
+  if (dtype == KIA_F32) bwd<float, KIA_HEAD>(a, cus, s);
+  else bwd<uint16_t, KIA_HEAD>(a, cus, s);
 }
 
 }  // namespace kia
