@@ -793,7 +793,9 @@ template <typename TI, int D> __global__ __launch_bounds__(256) void win_sum_ker
   const float *p = a.part + ((int64_t)s * win_slots(nkb, a.sink_blocks, a.parts_a, a.parts_b) + slot)
                               * 2 * WIN_KB * D + 4 * z;
   f32x4 x = *reinterpret_cast<const f32x4 *>(p);
-  for (int i = 1; i < parts; ++i) x += *reinterpret_cast<const f32x4 *>(p + (int64_t)i * 2 * WIN_KB * D);
+#pragma unroll 8
+  for (int i = 1; i < parts; ++i)
+    x += *reinterpret_cast<const f32x4 *>(p + (int64_t)i * 2 * WIN_KB * D);
   const int key = kb * WIN_KB + z % PER / (D / 4), c = z % (D / 4) * 4;
   if (key >= a.T) return;
   const View &out = z < PER ? a.dk : a.dv;
