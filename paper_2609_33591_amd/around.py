@@ -237,8 +237,9 @@ def _rotary_call(like, views, Hkv, plan, positions, back, stream=None):
     import torch
     B, H, T, d = like.shape
     freq = plan.freq
-    if freq.dim() != 1:
-        raise KiaError("a plan's frequencies must be one-dimensional")
+    if freq.dim() != 1 or not 2 <= 2 * freq.shape[0] <= d:
+        raise KiaError(f"a plan's frequencies must be one to {d // 2} in one dimension for heads of "
+                       f"{d} channels, got shape {tuple(freq.shape)}")
     fp = _buffer("the plan's frequencies", freq, torch.float64, 1, like.device, 8)
     first, ptr, sb = 0, None, 0
     if isinstance(positions, torch.Tensor):

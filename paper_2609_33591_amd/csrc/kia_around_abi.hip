@@ -107,8 +107,8 @@ WinArgs window_args(int B, int H, int Hkv, int T, int d, int window, int sinks) 
   a.scale = (float)(1.0 / sqrt((double)d));
   // The key blocks' lists of query tiles, in parts of at most a 512th of all tiles (two
   // workgroups a CU), and of four tiles at least (d = 128: eight; its sums cost more to
-  // add). Blocks of first tokens, which every query sees, are cut four times finer, so
-  // that they fill the gaps that the others leave. Measured, dK and dV with the sum (us):
+  // add). Blocks of first tokens, which every query sees, are cut up to four times finer,
+  // so that they fill the gaps that the others leave. Measured, dK and dV with the sum (us):
   // one sequence of 1024, 12 heads of 64, window 256: least 8 tiles 31, 4 tiles 26 (fp32 58 and
   // 49); 16 heads of 128 over 4 key heads, T = 2048, window 512: 56 and 65.
   const int G = H / Hkv, nkb = (T + WIN_KB - 1) / WIN_KB, least = d == 128 ? 8 : 4;
@@ -118,7 +118,7 @@ WinArgs window_args(int B, int H, int Hkv, int T, int d, int window, int sinks) 
   const int64_t total = (int64_t)B * Hkv * G * (a.sink_blocks * all + (nkb - a.sink_blocks) * near);
   const int64_t most = std::max<int64_t>(least, (total + 511) / 512);
   a.parts_b = nkb > a.sink_blocks ? (int)((G * near + most - 1) / most) : 1;
-  const int64_t fine = std::max<int64_t>(least, G * near / (4 * a.parts_b));
+  const int64_t fine = std::max<int64_t>({least, G * near / (4 * a.parts_b), most / 4});
   a.parts_a = a.sink_blocks ? (int)((G * all + fine - 1) / fine) : 1;
   return a;
 }
