@@ -1,4 +1,4 @@
-"""Build libkia.so (gfx950) from csrc/ with hipcc, in-tree.
+"""Build libkia.so (gfx950) from csrc/ with hipcc, and the binding's C module, in-tree.
 
 Every HIP source is compiled for gfx950 only, with packed-fp32 instruction
 selection disabled and hardware float atomics enabled (device buffers are
@@ -11,12 +11,14 @@ import concurrent.futures as cf
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libkia.so")
+HOST = os.path.join(HERE, "_host.so")  # csrc/kia_host.c, the calls of around.py in C
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 HEADS = (16, 32, 64, 128)
 # object -> its compilations (source, extra flags): the kernels that are
@@ -52,6 +54,14 @@ def _compile(unit) -> None:
          f"hipcc {src} {flags}")
 
 
+def build_host() -> None:
+    tmp = HOST + ".tmp"
+    _run([os.environ.get("CC", "gcc"), "-O2", "-shared", "-fPIC",
+          "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(ROOT, "include"),
+          os.path.join(CSRC, "kia_host.c"), "-o", tmp], "gcc kia_host.c")
+    os.replace(tmp, HOST)
+
+
 def link() -> None:
     for obj, parts in OBJECTS.items():
         if len(parts) > 1:
@@ -68,6 +78,7 @@ def build(verbose: bool = False) -> str:
     with cf.ThreadPoolExecutor(max_workers=min(len(UNITS), os.cpu_count() or 1)) as ex:
         list(ex.map(_compile, UNITS))
     link()
+    build_host()
     if verbose:
         print("built", LIB)
     return LIB
