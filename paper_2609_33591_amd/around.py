@@ -186,7 +186,7 @@ def _int(name, x, low):
 
 
 # The allocating calls go through csrc/kia_host.c where every argument is as the kernels
-# take it (a call for one token 8 us instead of 14); it returns None where one is not, and
+# take it (a call for one token 9 us instead of 14); it returns None where one is not, and
 # the code below then copies what needs copying, or says what is wrong.
 @functools.lru_cache(maxsize=1)
 def _fast():

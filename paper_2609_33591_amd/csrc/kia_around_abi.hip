@@ -252,7 +252,9 @@ int cache_copy(bool write, const kia_view *k, const kia_view *v, void *cache, in
 // resident at once: three workgroups a CU in bf16, two in fp32 (registers). More parts
 // cost more joining than the balance gains (32 sequences of 16 000 keys, softmax, bf16:
 // 67 / 59 / 69 us with two / three / six a CU; fp32, 16 sequences: 42 / 48 with two /
-// three). A part has 128 keys at least, 32 for each wave.
+// three). A part has 128 keys at least, 32 for each wave; up to 256 keys one part, and no
+// join (a call alone of 200 keys: bf16 24 us, 28 in two parts, fp32 32 and 34; of 400: 25
+// and 28, 35 and 34).
 void cached_shape(CachedArgs &a, int dtype, int cus) {
   a.tiles = (a.T * (a.H / a.Hkv) + 15) / 16;
   const int64_t keys = (int64_t)a.width << a.lpage;
@@ -261,7 +263,7 @@ void cached_shape(CachedArgs &a, int dtype, int cus) {
                            : std::min(keys, (int64_t)a.window + a.T + a.sinks + 64);
   const int64_t groups = (int64_t)a.Hkv * a.tiles, parts = (most + 127) / 128;
   const int64_t want = std::max<int64_t>(1, (dtype == KIA_F32 ? 2 : 3) * cus / groups);
-  a.shares = parts == 1 ? 1 : (int)std::min<int64_t>({want, parts * a.B, 255});
+  a.shares = most <= 256 ? 1 : (int)std::min<int64_t>({want, parts * a.B, 255});
 }
 
 int check_cached(int H, int Hkv, int K, int calib, float tau, int recon, int window, int sinks) {

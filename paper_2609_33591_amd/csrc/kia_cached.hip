@@ -35,7 +35,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // 32 keys at a time: two tiles of 16 and the next two on their way leave room for three
 // workgroups a CU in bf16 (162 registers; with 64 keys 217, two workgroups, and the
-// interval weights of 32 x 16 500 keys took 101 us, now 88).
+// interval weights of 32 x 16 500 keys took 101 us against 88).
 constexpr int TILES = 2, CHUNK = 16 * TILES, NWAVE = 4;
 enum { PASS_SOFTMAX, PASS_EXTREMA, PASS_GRID };
 
@@ -78,6 +78,26 @@ template <int N> __device__ __forceinline__ void load_words(const uint8_t *p, ui
   } else {
     w[0] = *reinterpret_cast<const uint32_t *>(p);
   }
+}
+
+// A row's value over the lanes that share it, in a fixed order (with FEW the columns 8 and 4
+// on, by rotations of the 16; then 16 and 32 lanes on).
+template <bool FEW, class F> __device__ __forceinline__ float across(float x, F f) {
+  if constexpr (FEW) {
+    x = f(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x128, 0xf, 0xf, true)));
+    x = f(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x124, 0xf, 0xf, true)));
+  }
+  x = f(x, __shfl_xor(x, 16));
+  return f(x, __shfl_xor(x, 32));
+}
+// The value of the lane 4 e on (in columns 0 .. 3; the others' results are not used).
+__device__ __forceinline__ float from_column(float x, int e) {
+  const int v = __float_as_int(x);
+  const int y = e == 0   ? v
+                : e == 1 ? __builtin_amdgcn_mov_dpp(v, 0x104, 0xf, 0xf, true)   // row_shl:4
+                : e == 2 ? __builtin_amdgcn_mov_dpp(v, 0x108, 0xf, 0xf, true)   // row_shl:8
+                         : __builtin_amdgcn_mov_dpp(v, 0x10c, 0xf, 0xf, true);  // row_shl:12
+  return __int_as_float(y);
 }
 
 // The chunks of keys that rows at positions lo .. hi see: the first tokens', then the
@@ -153,13 +173,22 @@ __device__ __forceinline__ int64_t slot_of(const CachedArgs &a, int hk, int tile
   return (((int64_t)hk * a.tiles + tile) * (a.shares + a.B) + w) * 16;
 }
 
-template <typename TI, int D, int PASS, int CALIB, int RECON>
+// FEW: a key head has at most four rows. The 16 columns then hold them four times over, and
+// of the four keys that a lane has scores of it takes one's weight, the (l / 4)-th: a
+// quarter of the work on weights. The interval weights are bound by that work: LERP over
+// the 32 sequences below 86 -> 76 us, Nearest with MinMax over 16 000 keys each 124 -> 107
+// and its extrema 73 -> 65. The softmax, whose maximum then crosses more lanes, is not
+// (118 and 119 us), nor are extrema without the minimum (fp32: 40 -> 45 us).
+template <typename TI, int D, int PASS, int CALIB, int RECON, bool FEW>
 __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
-  constexpr int NP = Pieces<TI>::N, N = D / 32, NT = D / 16;
+  constexpr int NP = Pieces<TI>::N, N = D / 32, NT = D / 16, NE = FEW ? 1 : 4;
   constexpr bool VALUES = PASS != PASS_EXTREMA;
   __shared__ float red[NWAVE][16][2];
   __shared__ __attribute__((aligned(16))) float rows[VALUES ? NWAVE * 16 * (D + 4) : 4];
-  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, kb = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, kb = lane >> 4;
+  const int slot = lane & 15;               // its key of a tile, its channels of the values
+  const int col = FEW ? slot & 3 : slot;    // its row
+  const int own = FEW ? slot >> 2 : 0;      // of its four scores a tile, the one it weighs
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hk = blockIdx.x % a.Hkv, tile = (int)(blockIdx.x / a.Hkv) % a.tiles;
   const int w = blockIdx.x / (a.Hkv * a.tiles);
@@ -211,13 +240,13 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
       x.ok |= ok << i;
       const uint8_t *kp = a.cache + cache_block<D>(ok ? page : 0, 0, hk, a.Hkv, a.lpage);
       const int tok = key & ((1 << a.lpage) - 1);
-      load_words<N>(kp + (tok + col) * (D / 2) + kb * (D / 8), x.k[i]);
-      x.ks[i] = kp[codes + (tok + col) * (D / 32) + kb * (D / 4) / 32];
+      load_words<N>(kp + (tok + slot) * (D / 2) + kb * (D / 8), x.k[i]);
+      x.ks[i] = kp[codes + (tok + slot) * (D / 32) + kb * (D / 4) / 32];
       if constexpr (VALUES) {
         const uint8_t *vp = kp + a.Hkv * block;
         load_words<N>(vp + tok * (D / 2) + lane * (D / 8), x.v[i]);
         x.vs[i] = *reinterpret_cast<const uint32_t *>(vp + codes + tok * (D / 32) + kb * (D / 8) +
-                                                      col * (D / 16) / 32 * 4);
+                                                      slot * (D / 16) / 32 * 4);
       }
     }
   };
@@ -269,7 +298,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
       }
     }
     bad = __any(bad);
-    float S[TILES][4];
+    float Q[TILES][4];
 #pragma unroll
     for (int i = 0; i < TILES; ++i) {
       const float f = scale_of(cur.ks[i]);
@@ -284,7 +313,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
 #pragma unroll
         for (int x = 0; x < N; ++x) acc = mma16(as_op(w[x]), q[p][x], acc);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) S[i][e] = acc[e];
+      for (int e = 0; e < 4; ++e) Q[i][e] = acc[e];
     }
     if (__builtin_expect(bad, 0)) {
 #pragma unroll
@@ -293,35 +322,44 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
         y |= y >> 32;
         y |= y >> 16;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) S[i][e] = y >> (4 * kb + e) & 1 ? NAN : S[i][e];
+        for (int e = 0; e < 4; ++e) Q[i][e] = y >> (4 * kb + e) & 1 ? NAN : Q[i][e];
       }
     }
+    // the scores of the keys that the lane weighs: key j + 16 i + 4 kb + own + e
+    float S[TILES][NE];
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+      if constexpr (FEW)
+        S[i][0] = own < 2 ? (own ? Q[i][1] : Q[i][0]) : own == 2 ? Q[i][2] : Q[i][3];
+      else
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[i][e] = Q[i][e];
+    }
+    auto counts = [&](int i, int e) { return sees(j + 16 * i + 4 * kb + own + e, i); };
     if (!all) {
 #pragma unroll
       for (int i = 0; i < TILES; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          S[i][e] = sees(j + 16 * i + 4 * kb + e, i) ? S[i][e] : -INFINITY;
+        for (int e = 0; e < NE; ++e) S[i][e] = counts(i, e) ? S[i][e] : -INFINITY;
     }
     if constexpr (PASS == PASS_EXTREMA) {
 #pragma unroll
       for (int i = 0; i < TILES; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < NE; ++e) {
           m = fmaxf(m, S[i][e]);
-          const bool in = all || sees(j + 16 * i + 4 * kb + e, i);
+          const bool in = all || counts(i, e);
           if constexpr (CALIB != CAL_FWM) low = in ? fminf(low, S[i][e]) : low;
         }
     } else {
-      float w[TILES][4];
+      float w[TILES][NE];
       if constexpr (PASS == PASS_SOFTMAX) {
         float top = S[0][0];
 #pragma unroll
         for (int i = 0; i < TILES; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) top = fmaxf(top, S[i][e]);
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
+          for (int e = 0; e < NE; ++e) top = fmaxf(top, S[i][e]);
+        top = across<FEW>(top, [](float x, float y) { return fmaxf(x, y); });
         // (moved, and the sums scaled, only when passed by 2^8, row by row: no row's bits
         // depend on another's)
         const bool up = (top - m) * c2 > 8.f;
@@ -336,13 +374,13 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
 #pragma unroll
         for (int i = 0; i < TILES; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) w[i][e] = __builtin_amdgcn_exp2f((S[i][e] - mm) * c2);
+          for (int e = 0; e < NE; ++e) w[i][e] = __builtin_amdgcn_exp2f((S[i][e] - mm) * c2);
       } else {
         bool any = false;
 #pragma unroll
         for (int i = 0; i < TILES; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
+          for (int e = 0; e < NE; ++e) {
             w[i][e] = fmaf(S[i][e], rc.alpha, rc.beta);
             any |= is_ambiguous<CALIB>(w[i][e], rc.margin2, edge);
           }
@@ -351,7 +389,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
 #pragma unroll
           for (int i = 0; i < TILES; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int e = 0; e < NE; ++e) {
               const bool amb = is_ambiguous<CALIB>(w[i][e], rc.margin2, edge);
               if (!__any(amb)) continue;
               const float x = 0.5f * exact_v2<CALIB>(S[i][e] * a.scale, 2.f * w[i][e], Mx, Mn, a.K, a.tau);
@@ -361,7 +399,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
 #pragma unroll
         for (int i = 0; i < TILES; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
+          for (int e = 0; e < NE; ++e) {
             const KeyDec k = key_of<CALIB>(w[i][e], Kf);
             const float up = grid_upper(k.rf, rc);
             float x;
@@ -376,8 +414,8 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
 #pragma unroll
           for (int i = 0; i < TILES; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              w[i][e] = sees(j + 16 * i + 4 * kb + e, i) ? w[i][e] : 0.f;
+            for (int e = 0; e < NE; ++e)
+              w[i][e] = counts(i, e) ? w[i][e] : 0.f;
         }
       }
       if (!all) {
@@ -400,7 +438,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
             is[i / 2][i % 2 * 4 + e] = (__bf16)(nan ? 1.f : 0.f);
             one[i / 2][i % 2 * 4 + e] = (__bf16)(sees(j + 16 * i + 4 * kb + e, i) ? 1.f : 0.f);
           }
-        // (column `col` of the values here is row 4 kb + e of the sums)
+        // (column `slot` of the values here is row 4 kb + e of the sums)
         f32x4 k = {};
 #pragma unroll
         for (int u = 0; u < TILES / 2; ++u) k = mma16(is[u], one[u], k);
@@ -410,13 +448,19 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
           for (int x = 0; x < NT; ++x) o[x][e] = k[e] > 0.f ? NAN : o[x][e];
       }
 #pragma unroll
-      for (int i = 0; i < TILES; ++i) l += (w[i][0] + w[i][1]) + (w[i][2] + w[i][3]);
+      for (int i = 0; i < TILES; ++i) {
+        if constexpr (FEW) l += w[i][0];
+        else l += (w[i][0] + w[i][1]) + (w[i][2] + w[i][3]);
+      }
 #pragma unroll
       for (int u = 0; u < TILES / 2; ++u) {
         // the weights of the lane's eight keys of 32, and those keys' values
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = w[2 * u + e / 4][e % 4];
+        for (int e = 0; e < 8; ++e) {
+          if constexpr (FEW) x[e] = from_column(w[2 * u + e / 4][0], e % 4);
+          else x[e] = w[2 * u + e / 4][e % 4];
+        }
         bf16x8 p[NP];
         to_pieces<NP>(x, p);
         float f[8];
@@ -450,13 +494,11 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
 
   const int64_t out = slot_of(a, hk, tile, w);
   if constexpr (PASS == PASS_EXTREMA) {
-    m = fmaxf(m, __shfl_xor(m, 16));
-    m = fmaxf(m, __shfl_xor(m, 32));
-    low = fminf(low, __shfl_xor(low, 16));
-    low = fminf(low, __shfl_xor(low, 32));
+    m = across<FEW>(m, [](float x, float y) { return fmaxf(x, y); });
+    low = across<FEW>(low, [](float x, float y) { return fminf(x, y); });
     if (kb == 0) red[wave][col][0] = m, red[wave][col][1] = low;
     __syncthreads();
-    if (tid < 16) {
+    if (tid < (FEW ? 4 : 16)) {
 #pragma unroll
       for (int i = 1; i < NWAVE; ++i) {
         m = fmaxf(m, red[i][col][0]);
@@ -466,15 +508,16 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
       a.ext[(out + col) * 2 + 1] = low;
     }
   } else {
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
+    l = across<FEW>(l, [](float x, float y) { return x + y; });
     if (kb == 0) red[wave][col][0] = m, red[wave][col][1] = l;
     // channel (4 kb + e) NT + x of row `col`
-    float *mine = rows + (wave * 16 + col) * (D + 4);
+    if (!FEW || own == 0) {
+      float *mine = rows + (wave * 16 + col) * (D + 4);
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+      for (int e = 0; e < 4; ++e)
 #pragma unroll
-      for (int x = 0; x < NT; ++x) mine[(4 * kb + e) * NT + x] = o[x][e];
+        for (int x = 0; x < NT; ++x) mine[(4 * kb + e) * NT + x] = o[x][e];
+    }
     __syncthreads();
     // joined in wave order: 256 threads, 16 rows, D / 16 channels each
     const int row = tid / 16, part = tid % 16;
@@ -565,32 +608,39 @@ template <typename TI, int D> __global__ __launch_bounds__(256) void join_kernel
   else *reinterpret_cast<u32x2 *>(y) = u32x2{cvt_bf16x2(x[0], x[1]), cvt_bf16x2(x[2], x[3])};
 }
 
-template <typename TI, int D, int CALIB> void grid_passes(const CachedArgs &a, dim3 g, hipStream_t s) {
+template <typename TI, int D, bool FEW, int CALIB>
+void grid_passes(const CachedArgs &a, dim3 g, hipStream_t s) {
   const dim3 t(64 * NWAVE);
   timed_call("kia_cache4_extrema", s, [&] {
-    hipLaunchKernelGGL((cached_kernel<TI, D, PASS_EXTREMA, CALIB, REC_LERP>), g, t, 0, s, a);
+    hipLaunchKernelGGL((cached_kernel<TI, D, PASS_EXTREMA, CALIB, REC_LERP, FEW && CALIB != CAL_FWM>),
+                       g, t, 0, s, a);
   });
   timed_call("kia_cache4_attn", s, [&] {
     if (a.recon == REC_LERP)
-      hipLaunchKernelGGL((cached_kernel<TI, D, PASS_GRID, CALIB, REC_LERP>), g, t, 0, s, a);
+      hipLaunchKernelGGL((cached_kernel<TI, D, PASS_GRID, CALIB, REC_LERP, FEW>), g, t, 0, s, a);
     else
-      hipLaunchKernelGGL((cached_kernel<TI, D, PASS_GRID, CALIB, REC_NEAREST>), g, t, 0, s, a);
+      hipLaunchKernelGGL((cached_kernel<TI, D, PASS_GRID, CALIB, REC_NEAREST, FEW>), g, t, 0, s, a);
   });
+}
+
+template <typename TI, int D, int CALIB> void grid_rows(const CachedArgs &a, dim3 g, hipStream_t s) {
+  if (a.T * (a.H / a.Hkv) <= 4) grid_passes<TI, D, true, CALIB>(a, g, s);
+  else grid_passes<TI, D, false, CALIB>(a, g, s);
 }
 
 template <typename TI, int D> void run(const CachedArgs &a, hipStream_t s) {
   const dim3 g((unsigned)(a.shares + a.B) * a.Hkv * a.tiles);
   if (a.recon == REC_SOFTMAX) {
     timed_call("kia_cache4_attn", s, [&] {
-      hipLaunchKernelGGL((cached_kernel<TI, D, PASS_SOFTMAX, CAL_FWM, REC_SOFTMAX>), g,
+      hipLaunchKernelGGL((cached_kernel<TI, D, PASS_SOFTMAX, CAL_FWM, REC_SOFTMAX, false>), g,
                          dim3(64 * NWAVE), 0, s, a);
     });
   } else if (a.calib == CAL_MINMAX) {
-    grid_passes<TI, D, CAL_MINMAX>(a, g, s);
+    grid_rows<TI, D, CAL_MINMAX>(a, g, s);
   } else if (a.calib == CAL_FWM) {
-    grid_passes<TI, D, CAL_FWM>(a, g, s);
+    grid_rows<TI, D, CAL_FWM>(a, g, s);
   } else {
-    grid_passes<TI, D, CAL_RESOLVED>(a, g, s);
+    grid_rows<TI, D, CAL_RESOLVED>(a, g, s);
   }
   if (a.shares > 1) {
     timed_call("kia_cache4_join", s, [&] {

@@ -31,7 +31,7 @@
 namespace kia {
 namespace {
 
-constexpr float LOG2E_F = 1.44269504f, LN2_F = 0.69314718f;
+constexpr float LOG2E_F = 1.44269504f;
 
 template <typename TI> constexpr bool is_f32 = sizeof(TI) == 4;
 
