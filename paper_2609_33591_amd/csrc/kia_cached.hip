@@ -595,7 +595,7 @@ template <typename TI, int D> __global__ __launch_bounds__(256) void join_kernel
   f32x4 x = {};
 #pragma unroll 4
   for (int i = grp; i < share.parts; i += NG)
-    if (f[i] != 0.f) x += p[(int64_t)i * 16 * W] * f[i];
+    x += p[(int64_t)i * 16 * W] * f[i];  // (a NaN stays one, however small its part's weight)
   sums[grp][at] = x;
   __syncthreads();
   if (grp) return;
