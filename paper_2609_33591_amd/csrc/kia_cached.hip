@@ -107,7 +107,8 @@ struct Chunks {
   __device__ __forceinline__ Chunks(const CachedArgs &a, int lo, int hi) {
     const int from = max(0, lo - a.window + 1);  // (window INT_MAX: 0)
     low = from / CHUNK;
-    sink = min((min(a.sinks, from) + CHUNK - 1) / CHUNK, low);
+    const int first = min(a.sinks, from);
+    sink = min(first / CHUNK + (first % CHUNK != 0), low);  // (up to 2^31 - 2 keys)
     count = hi < 0 ? 0 : sink + hi / CHUNK + 1 - low;
   }
   __device__ __forceinline__ int at(int n) const { return (n < sink ? n : low + n - sink) * CHUNK; }
