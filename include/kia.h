@@ -516,7 +516,10 @@ int kia_set_deterministic(int on);
  *     device and read when the kernels run: values that the caller may not
  *     pass (a page that the cache does not have, a position past the table)
  *     are skipped as each call says and never followed;
- *   - B*H*T*d may pass 2^31; T is at most 2^24;
+ *   - B*H*T*d may pass 2^31; T is at most 2^24; a call that would take 2^24
+ *     workgroups or more (about B*H*T of 2^30 for the attention and the cache,
+ *     B*T of 2^27 for the positions; 2^24 sequences of a token for each) is
+ *     KIA_ERR_SHAPE;
  *   - every call is bitwise repeatable, and keeps no state.
  * The kernels are timed as "kia_rotary", "kia_window_fwd", "kia_window_dq",
  * "kia_window_dkv", "kia_window_sum", "kia_cache4_write", "kia_cache4_read",
@@ -562,7 +565,8 @@ int kia_rotary(const kia_view *q, const kia_view *q_out, const kia_view *k,
  * `lengths` (int32 [B], or NULL), i < lengths[b]. window >= 1 (T or more:
  * every earlier key), sinks >= 0. s = q.k / sqrt(d).
  *   o = sum_j e^{s_j - lse} v_j, lse = ln sum_j e^{s_j} ([B,H,T] fp32,
- *   contiguous); a query past its sequence has o = 0 and lse = -infinity.
+ *   contiguous); a query past its sequence, or whose every score is -infinity,
+ *   has o = 0 and lse = -infinity, and no gradient.
  * Rows at or past lengths[b] (clamped to [0, T]) of q, k, v and dO are never
  * read as values, and what a query does not see has no influence on it,
  * infinities and NaNs included.
@@ -609,7 +613,8 @@ int kia_window_bwd(const kia_view *q, const kia_view *k, const kia_view *v,
 int kia_cache4_bytes(int pages, int page, int Hkv, int d, size_t *bytes);
 /* Writes token t of k, v [B, Hkv, T, d], t < counts[b] (NULL: every t), to
  * position starts[b] + t; positions below 0 or past the table are dropped.
- * Nothing else in the cache changes. */
+ * Nothing else in the cache changes. No two tokens of a call may go to one
+ * place: what it then holds is not defined. */
 int kia_cache4_write(const kia_view *k, const kia_view *v, void *cache,
                      int pages, int page, const int32_t *table, int width,
                      const int32_t *starts, const int32_t *counts, int B,
@@ -627,7 +632,8 @@ int kia_cache4_read(const void *cache, int pages, int page,
  * clamped to [0, width*page]): keys of sequence b, the new tokens' own among
  * them; query t of T is at position i = lengths[b] - T + t and sees key
  * j <= i, with window > 0 only if i - j < window or j < sinks (window 0: all).
- * A query that sees nothing (i < 0, no pages) has o = 0.
+ * A query that sees nothing (i < 0, no pages) has o = 0, and so has one whose
+ * every score is -infinity under softmax.
  * Weights by recon: KIA_RECON_SOFTMAX, or LERP / Nearest over the grid of
  * calib, K and tau as in kia_attn_fwd (softmax looks at none of them), with
  * the row's extrema over the keys that it sees. s = q.k / sqrt(d) from the

@@ -31,6 +31,17 @@ struct RotArgs {
   int first, layout, back, B, H, Hkv, T, d, rot;
   int tokens, per;  // tokens of a workgroup, rounds of heads of a share (the launcher's)
 };
+// Tokens of a workgroup, and the channels of an access (vw): the widest whose pairs fill
+// whole chunks (16 bytes for most plans; a rotated part of 2 mod 4 channels takes
+// single values).
+constexpr int ROT_NT = 256;
+inline int rotary_tokens(int T, int d, int rot, int dtype, int &vw) {
+  vw = dtype == KIA_F32 ? 4 : 8;
+  while (rot / 2 % vw) vw /= 2;
+  int tokens = 1;
+  while (2 * tokens <= T && tokens < 8 && 2 * tokens * (d / (2 * vw)) <= ROT_NT) tokens *= 2;
+  return tokens;
+}
 void launch_rotary(RotArgs a, int dtype, int cus, hipStream_t s);
 
 // ---- attention with a sliding window (kia_window.hip) ---------------------------
@@ -61,6 +72,12 @@ struct CacheArgs {
   View k, v;                           // the tokens to hold, or where to read them to
   int pages, lpage, width, B, Hkv, T;  // lpage: log2 of the tokens of a page
 };
+// Tokens of a head that a workgroup writes or reads: four a thread where that still leaves
+// eight workgroups a CU.
+inline int cache_tokens(int B, int Hkv, int T, int d, int cus) {
+  const int one = 256 * 8 / d;
+  return 2.0 * B * Hkv * T / (4 * one) >= 8.0 * cus ? 4 * one : one;
+}
 void launch_cache_write(const CacheArgs &a, int d, int dtype, int cus, hipStream_t s);
 void launch_cache_read(const CacheArgs &a, int d, int dtype, int cus, hipStream_t s);
 

@@ -16,6 +16,8 @@ using namespace kia;
 bool al16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 int launched() { return hipGetLastError() == hipSuccess ? KIA_OK : KIA_ERR_HIP; }
 int bytes_of(int dtype) { return dtype == KIA_F32 ? 4 : 2; }
+// A launch counts its threads, 256 a workgroup, in 32 bits.
+bool too_many(double groups) { return groups >= 1 << 24; }
 
 int check_common(int B, int H, int Hkv, int T, int d, int dtype, bool small_heads) {
   if (B < 1 || H < 1 || Hkv < 1 || T < 1) return KIA_ERR_SHAPE;
@@ -61,6 +63,9 @@ extern "C" int kia_rotary(const kia_view *q, const kia_view *q_out, const kia_vi
   if ((uintptr_t)freq & 7u || (uintptr_t)positions & 3u) return KIA_ERR_ALIGN;
   if (positions_sb < 0 || (int64_t)first + T > INT_MAX) return KIA_ERR_SHAPE;
   if ((int64_t)B * T > INT_MAX || (int64_t)H + Hkv > 65535) return KIA_ERR_SHAPE;
+  int vw = 0;
+  const int tokens = rotary_tokens(T, d, rot, dtype, vw);
+  if (too_many((double)B * ((T + tokens - 1) / tokens))) return KIA_ERR_SHAPE;
   const kia_view *v[4] = {q, q_out, k, k_out};
   for (int i = 0; i < (keys ? 4 : 2); ++i) {
     rc = check_view(v[i], B, i < 2 ? H : Hkv, T, d, dtype);
@@ -97,6 +102,10 @@ int check_window(int B, int H, int Hkv, int T, int d, int window, int sinks, int
   if ((double)B * H * ((T + 31) / 32) > 1 << 27) return KIA_ERR_SHAPE;
   return KIA_OK;
 }
+
+// (The key blocks' parts are less than 2560 more than the blocks, and their sums' workgroups
+// less than 40960 in all.)
+bool window_too_many(int B, int H, int T) { return too_many((double)B * H * ((T + 63) / 64) + 4096); }
 
 WinArgs window_args(int B, int H, int Hkv, int T, int d, int window, int sinks) {
   WinArgs a{};
@@ -148,6 +157,7 @@ extern "C" int kia_window_fwd(const kia_view *q, const kia_view *k, const kia_vi
                               void *stream) {
   int rc = check_window(B, H, Hkv, T, d, window, sinks, dtype);
   if (rc) return rc;
+  if (window_too_many(B, H, T)) return KIA_ERR_SHAPE;
   const kia_view *x[4] = {q, k, v, o};
   for (int i = 0; i < 4; ++i) {
     rc = check_view(x[i], B, i == 1 || i == 2 ? Hkv : H, T, d, dtype);
@@ -177,6 +187,7 @@ extern "C" int kia_window_bwd(const kia_view *q, const kia_view *k, const kia_vi
                               int d, int window, int sinks, int dtype, void *stream) {
   int rc = check_window(B, H, Hkv, T, d, window, sinks, dtype);
   if (rc) return rc;
+  if (window_too_many(B, H, T)) return KIA_ERR_SHAPE;
   const kia_view *x[8] = {q, o, dO, dq, k, v, dk, dv};
   for (int i = 0; i < 8; ++i) {
     rc = check_view(x[i], B, i < 4 ? H : Hkv, T, d, dtype);
@@ -234,7 +245,8 @@ int cache_copy(bool write, const kia_view *k, const kia_view *v, void *cache, in
   }
   if (!starts) return KIA_ERR_NULL;
   if ((uintptr_t)starts & 3u || (uintptr_t)counts & 3u) return KIA_ERR_ALIGN;
-  if (2.0 * B * Hkv * (T / 16 + 1) >= 2147483648.0) return KIA_ERR_SHAPE;
+  const int cus = host_cus(), per = cache_tokens(B, Hkv, T, d, cus);
+  if (too_many(2.0 * B * Hkv * ((T + per - 1) / per))) return KIA_ERR_SHAPE;
   CacheArgs a{};
   a.cache = static_cast<uint8_t *>(cache);
   a.table = table, a.starts = starts, a.counts = counts;
@@ -242,7 +254,6 @@ int cache_copy(bool write, const kia_view *k, const kia_view *v, void *cache, in
   a.pages = pages, a.lpage = page_log(page), a.width = width;
   a.B = B, a.Hkv = Hkv, a.T = T;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const int cus = host_cus();
   if (write) timed_call("kia_cache4_write", s, [&] { launch_cache_write(a, d, dtype, cus, s); });
   else timed_call("kia_cache4_read", s, [&] { launch_cache_read(a, d, dtype, cus, s); });
   return launched();
@@ -286,7 +297,8 @@ int cached_args(CachedArgs &a, int pages, int page, int width, int B, int H, int
   a.sinks = window > 0 ? sinks : 0;
   if ((double)T * (H / Hkv) >= 1 << 24) return KIA_ERR_SHAPE;
   cached_shape(a, dtype, host_cus());
-  if ((double)(a.shares + B) * Hkv * a.tiles >= 2147483648.0) return KIA_ERR_SHAPE;
+  if (too_many((double)(a.shares + B) * Hkv * a.tiles)) return KIA_ERR_SHAPE;
+  if (a.shares > 1 && too_many((double)B * H * T)) return KIA_ERR_SHAPE;  // (the join's)
   return KIA_OK;
 }
 

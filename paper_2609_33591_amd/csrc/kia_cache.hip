@@ -197,10 +197,8 @@ template <typename TI, int D, int REP> void launch_as(const CacheArgs &a, bool w
   else hipLaunchKernelGGL((read_kernel<TI, D, REP>), grid, block, 0, s, a);
 }
 
-// Four tokens a thread where that still leaves eight workgroups a CU.
 template <typename TI, int D> void launch_t(const CacheArgs &a, bool write, int cus, hipStream_t s) {
-  const double wgs = 2.0 * a.B * a.Hkv * a.T / (4 * Place<D, 4>::TOKENS);
-  if (wgs >= 8.0 * cus) launch_as<TI, D, 4>(a, write, s);
+  if (cache_tokens(a.B, a.Hkv, a.T, D, cus) > Place<D, 1>::TOKENS) launch_as<TI, D, 4>(a, write, s);
   else launch_as<TI, D, 1>(a, write, s);
 }
 template <int D> void launch(const CacheArgs &a, bool write, int dtype, int cus, hipStream_t s) {

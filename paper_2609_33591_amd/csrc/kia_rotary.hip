@@ -14,7 +14,6 @@
 
 namespace kia {
 
-constexpr int ROT_NT = 256;
 
 template <typename TI, int VW> struct RotVec {
   typedef TI vec __attribute__((ext_vector_type(VW)));
@@ -113,16 +112,12 @@ template <typename TI, int VW> static void launch(const RotArgs &a, dim3 grid, h
                      a.tokens * (a.rot / 2) * sizeof(float2), s, a);
 }
 
-// The widest access whose pairs fill whole chunks (16 bytes for most plans; a rotated
-// part of 2 mod 4 channels takes single values), and the grid: tokens of a
-// workgroup, and the heads in as many shares as it takes to reach four workgroups
-// per CU.
+// The grid: workgroups of `tokens` tokens, and the heads in as many shares as it takes to
+// reach four workgroups per CU.
 void launch_rotary(RotArgs a, int dtype, int cus, hipStream_t s) {
-  int vw = dtype == KIA_F32 ? 4 : 8;
-  while (a.rot / 2 % vw) vw /= 2;
+  int vw;
+  a.tokens = rotary_tokens(a.T, a.d, a.rot, dtype, vw);
   const int chunks = a.d / (2 * vw);
-  a.tokens = 1;
-  while (2 * a.tokens <= a.T && a.tokens < 8 && 2 * a.tokens * chunks <= ROT_NT) a.tokens *= 2;
   const int slots = ROT_NT / (chunks * a.tokens);
   const int rounds = (a.H + a.Hkv + slots - 1) / slots;
   const unsigned nb = (unsigned)a.B * ((a.T + a.tokens - 1) / a.tokens);
