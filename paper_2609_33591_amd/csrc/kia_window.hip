@@ -178,21 +178,30 @@ __device__ __forceinline__ f32x16 dots(const uint16_t *t, const uint16_t *b, int
 
 // acc[c][channel][row of b's side] += sum over the 32 streamed rows of their
 // channels 32 c .. times the weights w (register r: streamed row krel(r, half)).
-template <int D, int RS, int NC>
+// REST: bf16 weights in two pieces, what the rounding leaves multiplied too.
+template <int D, int RS, bool REST = false, int NC>
 __device__ __forceinline__ void mul_rows(f32x16 (&acc)[NC], const uint16_t *t, const float (&w)[16],
                                          int lane) {
   const uint16_t *p = t + tr_base<D, RS>(lane);
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
-    u32x4 x;
+    u32x4 x, y;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = cvt_bf16x2(w[8 * s + 2 * e], w[8 * s + 2 * e + 1]);
+    for (int e = 0; e < 4; ++e) {
+      const float a = w[8 * s + 2 * e], b = w[8 * s + 2 * e + 1];
+      x[e] = cvt_bf16x2(a, b);
+      if constexpr (REST)
+        y[e] = cvt_bf16x2(a - __uint_as_float(x[e] << 16), b - __uint_as_float(x[e] & 0xffff0000u));
+    }
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-      acc[c] = mfma16(tr_op<RS>(p + 16 * s * RS + 32 * c), as_op(x), acc[c]);
+    for (int c = 0; c < NC; ++c) {
+      const bf16x8 r = tr_op<RS>(p + 16 * s * RS + 32 * c);
+      if constexpr (REST) acc[c] = mfma16(r, as_op(y), acc[c]);
+      acc[c] = mfma16(r, as_op(x), acc[c]);
+    }
   }
 }
-template <int D, int RS, int NC>
+template <int D, int RS, bool REST = false, int NC>
 __device__ __forceinline__ void mul_rows(f32x16 (&acc)[NC], const float *t, const float (&w)[16],
                                          int lane) {
   const float *p = t + 4 * (lane >> 5) * RS + (lane & 31) % D;
@@ -469,12 +478,17 @@ __global__ __launch_bounds__(256, (Shape<TI, D, RG>::FWD_OCC)) void win_fwd_kern
 // their keys once before for that sum alone. (2-norm errors of dQ and dK against 64 bits at
 // d = 128: window 2 4.5e-3 -> 2.4e-3, window 512 2.6e-3 -> 2.4e-3; the output's rounding
 // alone is 1.65e-3. Beside rows of over 128 keys the error is lost in the others.)
+// In small heads a score has a large share of each key (q / sqrt(d) of it on average), and
+// the roundings of a row's dS, which add up to 0 without them, carry that share into dQ:
+// up to 32 channels dS goes in two bf16 pieces (window 217, 100 first tokens, T = 4531: d =
+// 16 2.51e-3 -> 1.76e-3 for 111 -> 127 us with 128 heads, d = 32 2.42e-3 -> 1.71e-3 for 117
+// -> 134; d = 64 has 2.37e-3 and would pay 163 -> 191).
 template <typename TI, int D, int RG>
 __global__ __launch_bounds__(256, (Shape<TI, D, RG>::DQ_OCC)) void win_dq_kernel(WinArgs a) {
   using C = Shape<TI, D, RG>;
   using R = typename C::R;
   constexpr int KP = C::KP, KT = C::KT, NBUF = C::NBUF, NC = C::NC, RS = R::RS;
-  constexpr bool FIX = !is_f32<TI>;
+  constexpr bool FIX = !is_f32<TI>, REST = FIX && D <= 32;
   __shared__ __attribute__((aligned(16))) char smem[C::SMEM];
   __shared__ float offs[4][64];
   __shared__ int flag[2][4];
@@ -557,7 +571,7 @@ __global__ __launch_bounds__(256, (Shape<TI, D, RG>::DQ_OCC)) void win_dq_kernel
         off += sum;
         if (only_sum) return;
       }
-      mul_rows<D, RS>(acc, kb, w, lane);
+      mul_rows<D, RS, REST>(acc, kb, w, lane);
     };
     auto all_tiles = [&](bool only_sum) {
       fetch(0);
