@@ -107,25 +107,30 @@ int check_window(int B, int H, int Hkv, int T, int d, int window, int sinks, int
 // less than 40960 in all.)
 bool window_too_many(int B, int H, int T) { return too_many((double)B * H * ((T + 63) / 64) + 4096); }
 
-WinArgs window_args(int B, int H, int Hkv, int T, int d, int window, int sinks) {
+WinArgs window_args(int B, int H, int Hkv, int T, int d, int window, int sinks, int dtype) {
   WinArgs a{};
   a.B = B, a.H = H, a.Hkv = Hkv, a.T = T;
   a.window = std::min(window, T);
   // (first tokens that the window holds everywhere change nothing)
   a.sinks = a.window == T ? 0 : std::min(sinks, T);
   a.scale = (float)(1.0 / sqrt((double)d));
-  // The key blocks' lists of query tiles, in parts of at most a 512th of all tiles (two
-  // workgroups a CU), and of four tiles at least (d = 128: eight; its sums cost more to
-  // add). Blocks of first tokens, which every query sees, are cut up to four times finer,
-  // so that they fill the gaps that the others leave. Measured, dK and dV with the sum (us):
-  // one sequence of 1024, 12 heads of 64, window 256: least 8 tiles 31, 4 tiles 26 (fp32 58 and
-  // 49); 16 heads of 128 over 4 key heads, T = 2048, window 512: 56 and 65.
-  const int G = H / Hkv, nkb = (T + WIN_KB - 1) / WIN_KB, least = d == 128 ? 8 : 4;
+  // The key blocks' lists of query tiles, in parts of at most all tiles over the workgroups
+  // that the chip holds (two a CU, of d = 128 in fp32 one), and of two tiles at least (four
+  // of d = 128 in bf16; its sums cost as much to add). Blocks of first tokens, which every
+  // query sees, are cut up to four times finer, so that they fill the gaps that the others
+  // leave. Measured, dK and dV and the sum (us) with 8 / 4 / 2 tiles at least, windows of 256:
+  //   d = 64, T = 1024, 12 heads, fp32            53 + 6 / 43 + 7 / 35 + 8
+  //   d = 64, T = 500, 16 heads over 4, bf16      24 + 6 / 16 + 6 / 13 + 6
+  //   d = 128, T = 1024, 16 heads over 4, bf16    34 + 7 / 27 + 8 / 29 + 10
+  //   d = 128, T = 685, 21 heads over 3, window 7, fp32   129 + 6 / 87 + 6 / 63 + 7
+  const int G = H / Hkv, nkb = (T + WIN_KB - 1) / WIN_KB;
+  const int least = d == 128 && dtype == KIA_BF16 ? 4 : 2;
+  const int slots = d == 128 && dtype == KIA_F32 ? 256 : 512;
   a.sink_blocks = (a.sinks + WIN_KB - 1) / WIN_KB;
   const int64_t all = (T + WIN_QT - 1) / WIN_QT;
   const int64_t near = std::min<int64_t>(all, (WIN_KB - 1 + (int64_t)a.window + WIN_QT - 1) / WIN_QT);
   const int64_t total = (int64_t)B * Hkv * G * (a.sink_blocks * all + (nkb - a.sink_blocks) * near);
-  const int64_t most = std::max<int64_t>(least, (total + 511) / 512);
+  const int64_t most = std::max<int64_t>(least, (total + slots - 1) / slots);
   a.parts_b = nkb > a.sink_blocks ? (int)((G * near + most - 1) / most) : 1;
   const int64_t fine = std::max<int64_t>({least, G * near / (4 * a.parts_b), most / 4});
   a.parts_a = a.sink_blocks ? (int)((G * all + fine - 1) / fine) : 1;
@@ -147,7 +152,9 @@ extern "C" int kia_window_ws_bytes(int B, int H, int Hkv, int T, int d, int wind
   *bytes = 0;
   const int rc = check_window(B, H, Hkv, T, d, window, sinks, KIA_F32);
   if (rc) return rc;
-  *bytes = window_ws(window_args(B, H, Hkv, T, d, window, sinks), d);
+  // (for either type)
+  for (int dtype : {KIA_F32, KIA_BF16})
+    *bytes = std::max(*bytes, window_ws(window_args(B, H, Hkv, T, d, window, sinks, dtype), d));
   return KIA_OK;
 }
 
@@ -165,7 +172,7 @@ extern "C" int kia_window_fwd(const kia_view *q, const kia_view *k, const kia_vi
   }
   if (!lse) return KIA_ERR_NULL;
   if (!al16(lse) || (uintptr_t)lengths & 3u) return KIA_ERR_ALIGN;
-  WinArgs a = window_args(B, H, Hkv, T, d, window, sinks);
+  WinArgs a = window_args(B, H, Hkv, T, d, window, sinks, dtype);
   a.q = view_of(q, B, H, T), a.o = view_of(o, B, H, T);
   a.k = view_of(k, B, Hkv, T), a.v = view_of(v, B, Hkv, T);
   a.lse = lse;
@@ -195,7 +202,7 @@ extern "C" int kia_window_bwd(const kia_view *q, const kia_view *k, const kia_vi
   }
   if (!lse || !ws) return KIA_ERR_NULL;
   if (!al16(lse) || (uintptr_t)lengths & 3u || (uintptr_t)ws & 255u) return KIA_ERR_ALIGN;
-  WinArgs a = window_args(B, H, Hkv, T, d, window, sinks);
+  WinArgs a = window_args(B, H, Hkv, T, d, window, sinks, dtype);
   a.q = view_of(q, B, H, T), a.o = view_of(o, B, H, T), a.dO = view_of(dO, B, H, T);
   a.dq = view_of(dq, B, H, T);
   a.k = view_of(k, B, Hkv, T), a.v = view_of(v, B, Hkv, T);
