@@ -575,7 +575,8 @@ int kia_rotary(const kia_view *q, const kia_view *q_out, const kia_view *k,
  * past their sequence. `ws`: kia_window_ws_bytes bytes, 256-byte aligned,
  * uninitialized.
  * bf16: the weights and the score gradients enter their products rounded to
- * bf16 (2^-8 of each). fp32: every product is an fp32 product.
+ * bf16 (2^-8 of each; for dq with d <= 32 in two such pieces). fp32: every
+ * product is an fp32 product.
  */
 int kia_window_fwd(const kia_view *q, const kia_view *k, const kia_view *v,
                    const kia_view *o, float *lse, const int32_t *lengths,

@@ -18,6 +18,8 @@
 // Softmax runs in one pass with a running maximum. The interval weights' grid
 // depends on the row's extrema, so a first pass over the keys alone (a third of the
 // bytes) finds them; the weights are absolute then and the parts' sums just add.
+// 32 sequences of up to 32 000 keys, 16 heads of 128 over 4, LERP: extrema 35 us (144 MB,
+// 4.2 TB/s), weights 74 us (289 MB, 3.9 TB/s), join 6.
 //
 // bf16 queries: scores are sums of exact products, weights are rounded to bf16 (2^-8
 // of each) for the product with V. fp32 queries and weights go as three bf16 pieces
