@@ -176,6 +176,20 @@ __device__ __forceinline__ f32x16 dots(const uint16_t *t, const uint16_t *b, int
   return c;
 }
 
+template <int D, int RS>
+__device__ __forceinline__ f32x16 dots(const float *t, const float *b, int lane) {
+  f32x16 c = {};
+  const int at = (lane & 31) * RS + 4 * (lane >> 5);
+#pragma unroll
+  for (int s = 0; s < D / 8; ++s) {
+    const f32x4 x = *reinterpret_cast<const f32x4 *>(t + at + 8 * s);
+    const f32x4 y = *reinterpret_cast<const f32x4 *>(b + at + 8 * s);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = mfma32(x[e], y[e], c);
+  }
+  return c;
+}
+
 // acc[c][channel][row of b's side] += sum over the 32 streamed rows of their
 // channels 32 c .. times the weights w (register r: streamed row krel(r, half)).
 // REST: bf16 weights in two pieces, what the rounding leaves multiplied too.
@@ -320,7 +334,10 @@ template <typename TI, int D, int RG> struct Shape {
   static constexpr int SMEM = (NBUF * BUF > JOIN ? NBUF * BUF : JOIN) + 64;
   static constexpr int WGS = 160 * 1024 / (SMEM + 64);  // that fit a CU's LDS
   static constexpr int FWD = RG < 4 ? 2 : is_f32<TI> ? (D == 128 ? 2 : 3) : D == 128 ? 3 : 4;
-  static constexpr int DQ = RG < 4 || D == 128 || (is_f32<TI> && D == 64) ? 2 : 3;
+  // (fp32, d = 128: two waves a SIMD spill 45 registers, 595 us against 559 with one)
+  static constexpr int DQ = is_f32<TI> && D == 128                              ? 1
+                            : RG < 4 || D == 128 || (is_f32<TI> && D == 64) ? 2
+                                                                            : 3;
   static constexpr int FWD_OCC = FWD < WGS ? FWD : WGS;
   static constexpr int DQ_OCC = DQ < WGS ? DQ : WGS;
 };
@@ -636,14 +653,14 @@ struct KeyPart {
 // added at the end through LDS. Blocks whose tiles are many (those of the first
 // tokens, which every query sees) are cut into parts, whose sums win_sum_kernel adds in
 // order: no atomics, so that the gradients repeat bit for bit.
-// At d = 128 in bf16 the keys and values stay in LDS: with them in registers the sums
-// (128) leave too few. The training step above: 150 us, 400 TFLOP/s, bound by two
+// At d = 128 the keys and values stay in LDS: with them in registers the sums (128) leave
+// too few (fp32, 16 heads, T = 2048, window 512: 76 spilled, 350 us against 212). The training step above: 150 us, 400 TFLOP/s, bound by two
 // workgroups a CU that wait for LDS and for each other (matrix unit busy 18%, vector
 // unit 22%, LDS 36% of the time).
 template <typename TI, int D>
 __global__ __launch_bounds__(256, is_f32<TI> && D == 128 ? 1 : 2) void win_dkv_kernel(WinArgs a) {
   constexpr int NT = 256, NC = D >= 32 ? D / 32 : 1;
-  constexpr bool KV = !is_f32<TI> && D == 128;
+  constexpr bool KV = D == 128;
   using R = Rows<TI, D, WIN_QT, NT>;
   constexpr int RS = R::RS;
   // queries and dO (and keys and values); then the second half's sums
