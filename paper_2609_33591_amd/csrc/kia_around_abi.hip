@@ -122,7 +122,7 @@ WinArgs window_args(int B, int H, int Hkv, int T, int d, int window, int sinks, 
   //   d = 64, T = 1024, 12 heads, fp32            53 + 6 / 43 + 7 / 35 + 8
   //   d = 64, T = 500, 16 heads over 4, bf16      24 + 6 / 16 + 6 / 13 + 6
   //   d = 128, T = 1024, 16 heads over 4, bf16    34 + 7 / 27 + 8 / 29 + 10
-  //   d = 128, T = 685, 21 heads over 3, window 7, fp32   129 + 6 / 87 + 6 / 63 + 7
+  //   d = 128, T = 685, 21 heads over 3, window 7, fp32   86 + 6 / 54 + 6 / 35 + 7
   const int G = H / Hkv, nkb = (T + WIN_KB - 1) / WIN_KB;
   const int least = d == 128 && dtype == KIA_BF16 ? 4 : 2;
   const int slots = d == 128 && dtype == KIA_F32 ? 256 : 512;

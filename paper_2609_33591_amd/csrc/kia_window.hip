@@ -654,7 +654,8 @@ struct KeyPart {
 // tokens, which every query sees) are cut into parts, whose sums win_sum_kernel adds in
 // order: no atomics, so that the gradients repeat bit for bit.
 // At d = 128 the keys and values stay in LDS: with them in registers the sums (128) leave
-// too few (fp32, 16 heads, T = 2048, window 512: 76 spilled, 350 us against 212). The training step above: 150 us, 400 TFLOP/s, bound by two
+// too few (fp32, 16 heads, T = 2048, window 512: 76 spilled, 350 us against 212; in bf16
+// one wave a SIMD, with room for all, takes 271 us where two take 151). The training step above: 150 us, 400 TFLOP/s, bound by two
 // workgroups a CU that wait for LDS and for each other (matrix unit busy 18%, vector
 // unit 22%, LDS 36% of the time).
 template <typename TI, int D>
@@ -856,7 +857,7 @@ template <typename TI, int D, int RG> void launch_dq(const WinArgs &a, hipStream
 //   bf16 d = 128, T = 2048, window 512  256 blocks 27.6 / 33.5, 33.5 / 36.4; 512 44.7 / 40.9,
 //                                       53.6 / 49.5
 //   fp32 d = 64, T = 1024, window 256   96 blocks 24 / 42, 30 / 53; 768 90 / 91, 123 / 134
-//   fp32 d = 128, T = 1024, window 256  128 blocks 43 / 69, 57 / 115; 256 82 / 71, 111 / 118
+//   fp32 d = 128, T = 1024, window 256  128 blocks 44 / 69, 58 / 98; 256 82 / 71, 111 / 102
 // (1 x 4, with 128 keys a step, gains 1 us on grids of a few blocks and loses above.)
 template <typename TI, int D> bool two_groups(const WinArgs &a, int cus) {
   const int64_t blocks = (int64_t)a.B * a.H * ((a.T + 127) / 128);
