@@ -179,7 +179,7 @@ __device__ __forceinline__ int64_t slot_of(const CachedArgs &a, int hk, int tile
 // FEW: a key head has at most four rows. The 16 columns then hold them four times over, and
 // of the four keys that a lane has scores of it takes one's weight, the (l / 4)-th: a
 // quarter of the work on weights. The interval weights are bound by that work: LERP over
-// the 32 sequences below 86 -> 76 us, Nearest with MinMax over 16 000 keys each 124 -> 107
+// the 32 sequences above 86 -> 76 us, Nearest with MinMax over 16 000 keys each 124 -> 107
 // and its extrema 73 -> 65. The softmax, whose maximum then crosses more lanes, is not
 // (118 and 119 us), nor are extrema without the minimum (fp32: 40 -> 45 us).
 template <typename TI, int D, int PASS, int CALIB, int RECON, bool FEW>
