@@ -485,6 +485,8 @@ __global__ __launch_bounds__(256, (Shape<TI, D, RG>::FWD_OCC)) void win_fwd_kern
   if (row >= a.T) return;
   l += __shfl_xor(l, 32);
   const bool none = l == 0.f || row >= n;
+  // (not by a factor of 0: what such a row met on its way may be infinite or NaN)
+  if (none) clear(acc);
   store_row<D, NC>(slice_of<TI>(a.o, b, h) + row * a.o.st, acc, half, none ? 0.f : 1.f / l);
   if (half == 0)
     a.lse[((int64_t)b * a.H + h) * a.T + row] = none ? -INFINITY : fmaf(m, a.scale, logf(l));
@@ -526,6 +528,7 @@ __global__ __launch_bounds__(256, (Shape<TI, D, RG>::DQ_OCC)) void win_dq_kernel
   f32x16 acc[NC];
   clear(acc);
   float off = 0.f, delta = 0.f;  // off: sum of the row's weights
+  float lse = INFINITY;          // (of a row of nothing too: no weight anywhere)
   if (i0 < n) {
     RowReg<TI, D> q, g;
     const int at = min(row, n - 1);
@@ -537,8 +540,8 @@ __global__ __launch_bounds__(256, (Shape<TI, D, RG>::DQ_OCC)) void win_dq_kernel
       delta = g.dot(o);
       delta += __shfl_xor(delta, 32);
     }
-    float lse = row < n ? a.lse[srow] : INFINITY;
-    if (lse == -INFINITY) lse = INFINITY;  // a row of nothing: no weight anywhere
+    if (row < n) lse = a.lse[srow];
+    if (lse == -INFINITY) lse = INFINITY;
     const float c2 = a.scale * LOG2E_F, lse2 = lse * LOG2E_F;
     const KeyTiles<KT> tiles(a, i0, min(i0 + 32 * RG, n));
     const TI *ks = slice_of<TI>(a.k, b, hk), *vs = slice_of<TI>(a.v, b, hk);
@@ -630,7 +633,8 @@ __global__ __launch_bounds__(256, (Shape<TI, D, RG>::DQ_OCC)) void win_dq_kernel
   }
   if (row >= a.T) return;
   if (half == 0 && row < n) a.delta[srow] = delta;
-  store_row<D, NC>(slice_of<TI>(a.dq, b, h) + row * a.dq.st, acc, half, row < n ? a.scale : 0.f);
+  if (lse == INFINITY) clear(acc);
+  store_row<D, NC>(slice_of<TI>(a.dq, b, h) + row * a.dq.st, acc, half, a.scale);
 }
 
 // The key block, the part of its query range and the number of parts of a workgroup.

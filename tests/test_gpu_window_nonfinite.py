@@ -1,0 +1,61 @@
+"""Windowed attention on the device where infinities and NaNs stand in rows that are
+seen: what they reach goes by the definition, not by the tile that a row or the end of
+a sequence falls in. Everything else is compared bit for bit with a call of finite
+values in their place that has the same weights."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2609_33591_amd as kia  # noqa: E402
+from tests.test_gpu_window import inputs  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+TYPES = (torch.float32, torch.bfloat16)
+# grids of two and of four groups of rows in a workgroup
+GRIDS = ((1, 2, 1), (2, 208, 8))
+
+
+def both(q, k, v, g, window, sinks, lengths=None):
+    o, lse = kia.window_forward(q, k, v, window, sinks, lengths)
+    return (o, lse, *kia.window_backward(q, k, v, o, g, lse, window, sinks, lengths))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", (16, 64, 128))
+@pytest.mark.parametrize("grid", GRIDS)
+@pytest.mark.parametrize("bad", (math.nan, math.inf, -math.inf))
+def test_rows_behind_a_sequence_stay_zero(dtype, d, grid, bad):
+    """The last token of a sequence in the middle of a tile is not finite: what is behind
+    the end is 0 all the same."""
+    B, H, Hkv = grid
+    T, n = 150, 77
+    lengths = torch.full((B,), n, dtype=torch.int32, device="cuda")
+    for which in range(4):
+        x = inputs(B, H, Hkv, T, d, dtype, seed=200)
+        x[which][:, :, n - 1, 3] = bad
+        o, lse, *grads = both(*x, 40, 2, lengths)
+        for y in (o, *grads):
+            assert bool((y[:, :, n:] == 0).all()), which
+        assert bool((lse[:, :, n:] == -math.inf).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", (16, 64, 128))
+@pytest.mark.parametrize("grid", GRIDS)
+def test_rows_of_no_weight_are_zero(dtype, d, grid):
+    """A query whose every score is -infinity has o = 0, lse = -infinity and dq = 0,
+    whatever the values that it sees hold."""
+    B, H, Hkv = grid
+    T = 150
+    q, k, v, g = inputs(B, H, Hkv, T, d, dtype, seed=230)
+    k[..., 3] = k[..., 3].abs() + 0.5
+    q[:, :, 100, 3] = -math.inf
+    for window, sinks in ((T, 0), (40, 2)):
+        for bad in (math.inf, math.nan):
+            y = v.clone()
+            y[:, :, 80, 1] = bad
+            o, lse, dq, *_ = both(q, k, y, g, window, sinks)
+            assert bool((o[:, :, 100] == 0).all()) and bool((dq[:, :, 100] == 0).all())
+            assert bool((lse[:, :, 100] == -math.inf).all())
