@@ -706,22 +706,24 @@ __global__ __launch_bounds__(256, is_f32<TI> && D == 128 ? 1 : 2) void win_dkv_k
       v.load(vs + at * a.v.st, half, key < n);
     }
     const float c2 = a.scale * LOG2E_F;
-    float st = 0.f;  // threads 0..63: lse, 64..127: D of the tile's rows
+    float lse = 0.f, dd = 0.f;  // of the tile's rows, a lane each (D: the second wave's)
     auto fetch = [&](int it) {
       const int h = hk * G + it / per, i = j0 + it % per * WIN_QT;
       fq.fetch(slice_of<TI>(a.q, b, h), a.q.st, i, n, tid);
       fg.fetch(slice_of<TI>(a.dO, b, h), a.dO.st, i, n, tid);
-      if (wave < 2) {
-        const int64_t r = ((int64_t)b * a.H + h) * a.T + i + lane;
-        const bool ok = i + lane < n;
-        st = ok ? (wave ? a.delta : a.lse)[r] : wave ? 0.f : INFINITY;
-        if (!wave && st == -INFINITY) st = INFINITY;
-        if (!wave && !is_f32<TI>) st *= LOG2E_F;
-      }
+      const int64_t r = ((int64_t)b * a.H + h) * a.T + i + lane;
+      const bool ok = i + lane < n;
+      lse = ok ? a.lse[r] : INFINITY;
+      if (lse == -INFINITY) lse = INFINITY;
+      if (wave == 1) dd = ok ? a.delta[r] : 0.f;
     };
+    bool none = false;
     auto stage = [&](int it) {
       const int i = j0 + it % per * WIN_QT;
-      const bool part = !sees_all(a, i, WIN_QT, j0, WIN_KB);
+      // rows of no weight, past the end or of no finite score, add nothing: their own
+      // infinities and NaNs are zeros in LDS too, and what a key's make of them is masked
+      none = __any(lse == INFINITY);
+      const bool part = none || !sees_all(a, i, WIN_QT, j0, WIN_KB);
       bool bad = false;
       if (part) {
         bad = __any(fq.bad() | fg.bad());
@@ -730,7 +732,8 @@ __global__ __launch_bounds__(256, is_f32<TI> && D == 128 ? 1 : 2) void win_dkv_k
       if (it > it0) lds_barrier();
       fq.stash(qb, tid);
       fg.stash(gb, tid);
-      if (wave < 2) stat[wave][lane] = st;
+      if (wave == 0) stat[0][lane] = is_f32<TI> ? lse : lse * LOG2E_F;
+      if (wave == 1) stat[1][lane] = dd;
       if (part && lane == 0) flag[wave] = bad;
       if (it + 1 < it1) fetch(it + 1);
       lds_barrier();
@@ -770,12 +773,22 @@ __global__ __launch_bounds__(256, is_f32<TI> && D == 128 ? 1 : 2) void win_dkv_k
           ds[r] = ok ? ds[r] : 0.f;
         }
       }
+      if (__builtin_expect(none, 0)) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const bool ok = stat[0][32 * qg + krel(r, half)] != INFINITY;
+          w[r] = ok ? w[r] : 0.f;
+          ds[r] = ok ? ds[r] : 0.f;
+        }
+      }
       mul_rows<D, RS>(dv, gt, w, lane);
       mul_rows<D, RS>(dk, qt, ds, lane);
       // (a query with such a value has lse or D that makes its weights NaN)
       if (__builtin_expect(bad, 0))
         add_bad<D>(dv, slice_of<TI>(a.dO, b, hk * G + it / per) + iw * a.dO.st, a.dO.st, n - iw,
-                   lane, [&](int r) { return sees(a, iw + r, key); });
+                   lane, [&](int r) {
+                     return sees(a, iw + r, key) && stat[0][32 * qg + r] != INFINITY;
+                   });
     };
     fetch(it0);
     for (int it = it0; it < it1; ++it) {

@@ -59,3 +59,50 @@ def test_rows_of_no_weight_are_zero(dtype, d, grid):
             o, lse, dq, *_ = both(q, k, y, g, window, sinks)
             assert bool((o[:, :, 100] == 0).all()) and bool((dq[:, :, 100] == 0).all())
             assert bool((lse[:, :, 100] == -math.inf).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", (16, 64, 128))
+@pytest.mark.parametrize("grid", GRIDS)
+def test_rows_of_no_weight_add_nothing(dtype, d, grid):
+    """A query whose every score is -infinity adds nothing to dk and dv, whatever its dO
+    holds, and changes no other row."""
+    B, H, Hkv = grid
+    T = 150
+    q, k, v, g = inputs(B, H, Hkv, T, d, dtype, seed=210)
+    k[..., 3] = k[..., 3].abs() + 0.5
+    for at in (0, 31, 70, 149):
+        for window, sinks in ((T, 0), (40, 2)):
+            # a row with dO = 0 adds nothing to dk and dv either
+            g0 = g.clone()
+            g0[:, :, at] = 0
+            want = both(q, k, v, g0, window, sinks)
+            x, bad = q.clone(), g.clone()
+            x[:, :, at, 3] = -math.inf
+            for value in (1.0, math.nan, math.inf):
+                bad[:, :, at, 1] = value
+                o, lse, dq, dk, dv = both(x, k, v, bad, window, sinks)
+                rest = torch.arange(T, device="cuda") != at
+                assert bool((o[:, :, at] == 0).all()) and bool((dq[:, :, at] == 0).all())
+                assert bool((lse[:, :, at] == -math.inf).all())
+                for got, to in zip((o, lse, dq), want):
+                    assert torch.equal(got[:, :, rest], to[:, :, rest])
+                assert torch.equal(dk, want[3]) and torch.equal(dv, want[4])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", (16, 64, 128))
+@pytest.mark.parametrize("n", (65, 77, 97, 150))
+def test_keys_of_no_weight_beside_the_end(dtype, d, n):
+    """A key whose scores are all -infinity has no gradient, also where rows behind the
+    end of its sequence share its tile."""
+    T = 150
+    q, k, v, g = inputs(2, 2, 1, T, d, dtype, seed=240)
+    q[..., 3] = q[..., 3].abs() + 0.5
+    k[:, :, 40, 3] = -math.inf
+    lengths = torch.full((2,), n, dtype=torch.int32, device="cuda")
+    for window, sinks in ((T, 0), (70, 0), (30, 2)):
+        *_, dk, dv = both(q, k, v, g, window, sinks, lengths)
+        assert bool((dv[:, :, 40] == 0).all())
+        if dtype == torch.float32:
+            assert bool((dk[:, :, 40] == 0).all())
