@@ -228,10 +228,10 @@ __device__ __forceinline__ void mul_rows(f32x16 (&acc)[NC], const float *t, cons
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
 // The infinities and NaNs of the 32 streamed rows at `rows` (stride st, only the first
 // `count`), which mul_rows took as zeros: added to the lane's row where see(i) says
-// that streamed row i counts for it.
+// that streamed row i counts for it, times f (0: as NaN).
 template <int D, int NC, typename TI, class See>
 __device__ __forceinline__ void add_bad(f32x16 (&acc)[NC], const TI *rows, int64_t st, int count,
-                                        int lane, See see) {
+                                        int lane, float f, See see) {
 #pragma unroll 1
   for (int i = 0; i < min(32, count); ++i) {
     const bool ok = see(i);
@@ -242,7 +242,7 @@ __device__ __forceinline__ void add_bad(f32x16 (&acc)[NC], const TI *rows, int64
       for (int g = 0; g < (D < 32 ? D / 8 : 4); ++g) {
         const f32x4 x = load4(row + 32 * c + 8 * g);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[c][4 * g + e] += ok && !finite(x[e]) ? x[e] : 0.f;
+        for (int e = 0; e < 4; ++e) acc[c][4 * g + e] += ok && !finite(x[e]) ? x[e] * f : 0.f;
       }
   }
 }
@@ -459,7 +459,7 @@ __global__ __launch_bounds__(256, (Shape<TI, D, RG>::FWD_OCC)) void win_fwd_kern
       l += sum;
       mul_rows<D, RS>(acc, vb, w, lane);
       if (__builtin_expect(bad, 0))
-        add_bad<D>(acc, vs + j * a.v.st, a.v.st, n - j, lane,
+        add_bad<D>(acc, vs + j * a.v.st, a.v.st, n - j, lane, 1.f,
                    [&](int i) { return sees(a, row, j + i); });
     };
     fetch(0);
@@ -580,10 +580,12 @@ __global__ __launch_bounds__(256, (Shape<TI, D, RG>::DQ_OCC)) void win_dq_kernel
         const float e = is_f32<TI> ? fmaf(S[r], a.scale, -lse) * LOG2E_F : fmaf(S[r], c2, -lse2);
         w[r] = __builtin_amdgcn_exp2f(e) * (P[r] - delta);
       }
-      if (__builtin_expect(bad, 0)) {  // (a query that sees such a key has no score there)
+      if (__builtin_expect(bad, 0)) {
+        // (a score of -infinity, weight 0, or a row of NaN, D among it)
         const uint32_t rows = bad_rows<D>(ks + j * a.k.st, a.k.st, n - j, lane);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) w[r] = rows >> krel(r, half) & 1 ? NAN : w[r];
+        for (int r = 0; r < 16; ++r)
+          w[r] = rows >> krel(r, half) & 1 ? 0.f * (P[r] - delta) : w[r];
       }
       if (!sees_all(a, iw, 32, j, 32)) {
 #pragma unroll
@@ -596,6 +598,9 @@ __global__ __launch_bounds__(256, (Shape<TI, D, RG>::DQ_OCC)) void win_dq_kernel
         if (only_sum) return;
       }
       mul_rows<D, RS, REST>(acc, kb, w, lane);
+      if (__builtin_expect(bad, 0))
+        add_bad<D>(acc, ks + j * a.k.st, a.k.st, n - j, lane, 0.f,
+                   [&](int i) { return sees(a, row, j + i); });
     };
     auto all_tiles = [&](bool only_sum) {
       fetch(0);
@@ -786,7 +791,7 @@ __global__ __launch_bounds__(256, is_f32<TI> && D == 128 ? 1 : 2) void win_dkv_k
       // (a query with such a value has lse or D that makes its weights NaN)
       if (__builtin_expect(bad, 0))
         add_bad<D>(dv, slice_of<TI>(a.dO, b, hk * G + it / per) + iw * a.dO.st, a.dO.st, n - iw,
-                   lane, [&](int r) {
+                   lane, 1.f, [&](int r) {
                      return sees(a, iw + r, key) && stat[0][32 * qg + r] != INFINITY;
                    });
     };

@@ -2,6 +2,7 @@
 seen: what they reach goes by the definition, not by the tile that a row or the end of
 a sequence falls in. Everything else is compared bit for bit with a call of finite
 values in their place that has the same weights."""
+import itertools
 import math
 
 import pytest
@@ -103,6 +104,44 @@ def test_keys_of_no_weight_beside_the_end(dtype, d, n):
     lengths = torch.full((2,), n, dtype=torch.int32, device="cuda")
     for window, sinks in ((T, 0), (70, 0), (30, 2)):
         *_, dk, dv = both(q, k, v, g, window, sinks, lengths)
-        assert bool((dv[:, :, 40] == 0).all())
-        if dtype == torch.float32:
-            assert bool((dk[:, :, 40] == 0).all())
+        assert bool((dk[:, :, 40] == 0).all()) and bool((dv[:, :, 40] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", (16, 64, 128))
+@pytest.mark.parametrize("grid", GRIDS)
+def test_keys_of_scores_of_minus_infinity(dtype, d, grid):
+    """A key whose scores are all -infinity has weight 0 as one whose scores are far below
+    the others': the same outputs and gradients, but for dq, which is NaN in the channel
+    where 0 meets the infinity; in every kind of tile, and beside the end of a sequence."""
+    B, H, Hkv = grid
+    T = 150
+    q, k, v, g = inputs(B, H, Hkv, T, d, dtype, seed=220)
+    q[..., 3] = q[..., 3].abs() + 0.5
+    i = torch.arange(T, device="cuda")
+    for at, n, (window, sinks) in itertools.product((0, 5, 40, 63, 64), (65, 77, 96, 97, 128, T),
+                                                    ((T, 0), (70, 0), (30, 2))):
+        lengths = torch.full((B,), n, dtype=torch.int32, device="cuda")
+        low, none = k.clone(), k.clone()
+        low[:, :, at, 3] = -2.0 ** 15  # (scores below -2^10: weight 0 in fp32)
+        none[:, :, at, 3] = -math.inf
+        want, got = (both(q, x, v, g, window, sinks, lengths) for x in (low, none))
+        see = (i >= at) & ((i - at < window) | (at < sinks)) & (i < n)
+        # the first row sees no other key than the first: no weight, where the finite
+        # score has all of it
+        alone = (i == 0) & (at == 0)
+        what = f"key {at}, {n} tokens, window {window}"
+        for a, b in zip(got[:2], want[:2]):
+            assert torch.equal(a[:, :, ~alone], b[:, :, ~alone]), what
+        dq, see = got[2], see & ~alone
+        assert bool((got[0][:, :, alone] == 0).all()) and bool((dq[:, :, alone] == 0).all()), what
+        assert bool(torch.isnan(dq[:, :, see][..., 3]).all()), what
+        dq[..., 3] = torch.where(see, want[2][..., 3], dq[..., 3])
+        assert torch.equal(dq[:, :, ~alone], want[2][:, :, ~alone]), what
+        if at == 0:
+            g0 = g.clone()
+            g0[:, :, 0] = 0
+            want = both(q, low, v, g0, window, sinks, lengths)
+        assert torch.equal(got[3], want[3]), what
+        assert torch.equal(got[4], want[4]), what
+        assert bool((got[3][:, :, at] == 0).all()) and bool((got[4][:, :, at] == 0).all()), what
