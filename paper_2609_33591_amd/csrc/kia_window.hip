@@ -717,16 +717,18 @@ __global__ __launch_bounds__(256, is_f32<TI> && D == 128 ? 1 : 2) void win_dkv_k
       fq.fetch(slice_of<TI>(a.q, b, h), a.q.st, i, n, tid);
       fg.fetch(slice_of<TI>(a.dO, b, h), a.dO.st, i, n, tid);
       const int64_t r = ((int64_t)b * a.H + h) * a.T + i + lane;
-      const bool ok = i + lane < n;
-      lse = ok ? a.lse[r] : INFINITY;
-      if (lse == -INFINITY) lse = INFINITY;
-      if (wave == 1) dd = ok ? a.delta[r] : 0.f;
+      lse = INFINITY, dd = 0.f;
+      if (i + lane < n) {
+        lse = a.lse[r];
+        if (wave == 1) dd = a.delta[r];
+      }
     };
     bool none = false;
     auto stage = [&](int it) {
       const int i = j0 + it % per * WIN_QT;
       // rows of no weight, past the end or of no finite score, add nothing: their own
-      // infinities and NaNs are zeros in LDS too, and what a key's make of them is masked
+      // infinities and NaNs are zeros in LDS too, and what they make of a key's is masked
+      if (lse == -INFINITY) lse = INFINITY;
       none = __any(lse == INFINITY);
       const bool part = none || !sees_all(a, i, WIN_QT, j0, WIN_KB);
       bool bad = false;
