@@ -185,6 +185,19 @@ def _int(name, x, low):
     return x
 
 
+def _eager(*tensors):
+    """Refuses what a call would leave out without a word, since the kernels see data
+    alone: forward-mode derivatives of its inputs (their tangents), and its place in a
+    trace."""
+    import torch
+    ad = torch.autograd.forward_ad
+    if ad._current_level >= 0 and any(isinstance(x, torch.Tensor) and ad.unpack_dual(x).tangent is not None
+                                      for x in tensors):
+        raise KiaError("libkia has no forward-mode derivatives: an input has a tangent")
+    if torch.jit.is_tracing():
+        raise KiaError("libkia's calls cannot be traced")
+
+
 # The allocating calls go through csrc/kia_host.c where every argument is as the kernels
 # take it (a call for one token 9 us instead of 14); it returns None where one is not, and
 # the code below then copies what needs copying, or says what is wrong.
@@ -337,6 +350,7 @@ def rotary(q, k, plan, positions=None, back=False):
     """q and k (or None) with their positions' rotation, as new tensors; see
     kia_rotary. Differentiable."""
     import torch
+    _eager(q, k)
     if torch.is_grad_enabled() and (q.requires_grad or (k is not None and k.requires_grad)):
         return _rotary_function().apply(q, k, plan, positions, back)
     return _rotated(q, k, plan, positions, back)
@@ -406,6 +420,7 @@ def kia_window_bwd(q, k, v, o, dO, lse, ws, dq, dk, dv, window, sinks=0, lengths
 
 def window_forward(q, k, v, window, sinks=0, lengths=None):
     """Allocates o and lse and runs kia_window_fwd; returns (o, lse)."""
+    _eager(q, k, v)
     made = _fast().window_forward(q, k, v, window, sinks, lengths)
     if made is not None:
         return made
@@ -423,6 +438,7 @@ def window_forward(q, k, v, window, sinks=0, lengths=None):
 
 def window_backward(q, k, v, o, dO, lse, window, sinks=0, lengths=None):
     """Allocates dq, dk, dv and runs kia_window_bwd; returns (dq, dk, dv)."""
+    _eager(q, k, v, o, dO, lse)
     made = _fast().window_backward(q, k, v, window, sinks, lengths, o, dO, lse)
     if made is not None:
         return made
@@ -478,6 +494,7 @@ def window_attention(q, k, v, window, sinks=0, lengths=None, rotary=None, positi
         q, k = _rotate(q, k, rotary, positions)
     elif positions is not None:
         raise KiaError("positions without a rotary plan")
+    _eager(q, k, v)
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
         return _window_function().apply(q, k, v, window, sinks, lengths)
     return window_forward(q, k, v, window, sinks, lengths)[0]
@@ -578,6 +595,7 @@ def kia_cache4_read(cache, table, starts, k, v, counts=None, stream=None):
 
 def cache4_write(k, v, cache, table, starts, counts=None):
     """kia_cache4_write, for tensors of any layout."""
+    _eager(k, v)
     if _fast().cache4_write(k, v, cache.data, cache.page, cache.d, table, starts, counts):
         return
     like = _Like("k", k)
@@ -589,6 +607,7 @@ def cache4_write(k, v, cache, table, starts, counts=None):
 def cache4_read(cache, table, starts, T, dtype, counts=None):
     """Allocates k and v [B, heads, T, d] of `dtype` and runs kia_cache4_read."""
     import torch
+    _eager()
     if not isinstance(table, torch.Tensor) or table.dim() != 2:
         raise KiaError("table must be an int32 tensor [B, width]")
     k = torch.empty(table.shape[0], cache.heads, _int("T", T, 1), cache.d, dtype=dtype,
@@ -654,6 +673,7 @@ def cache4_attention(q, cache, table, lengths, K=4, calib="fwm", tau=8.0, recon=
     import torch
     if q.requires_grad and torch.is_grad_enabled():
         raise KiaError("attention over a 4-bit cache is forward only: call it under torch.no_grad")
+    _eager(q)
     op = _kia._op(K, calib, tau, recon, 0, 0, 0)
     made = _fast().cache4_attention(q, cache.data, cache.page, cache.d, table, lengths, *op[:4],
                                     window, sinks)
