@@ -615,6 +615,7 @@ def k_interval_attention(q, k, v, K=4, calib="fwm", tau=8.0, recon="nearest", st
     forward runs forward-only (gradient mode "none") and o is returned as
     is. rotary: a RotaryPlan that turns q and k by `positions` first."""
     import torch
+    around._eager(q, k, v)
     if rotary is not None:
         q, k = around.rotary(q, k, rotary, positions)
     elif positions is not None:

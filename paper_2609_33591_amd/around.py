@@ -490,11 +490,11 @@ def window_attention(q, k, v, window, sinks=0, lengths=None, rotary=None, positi
     int32 [B], tokens of each sequence (rows past it get o = 0 and no gradient).
     rotary: a RotaryPlan that turns q and k by `positions` first."""
     import torch
+    _eager(q, k, v)
     if rotary is not None:
         q, k = _rotate(q, k, rotary, positions)
     elif positions is not None:
         raise KiaError("positions without a rotary plan")
-    _eager(q, k, v)
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
         return _window_function().apply(q, k, v, window, sinks, lengths)
     return window_forward(q, k, v, window, sinks, lengths)[0]

@@ -19,9 +19,11 @@ def calls():
     return {
         "rotary q": (lambda x: kia.rotary(x, k, plan)[0], q),
         "rotary k": (lambda x: kia.rotary(q, x, plan)[0], k),
+        "k_interval_attention q": (lambda x: kia.k_interval_attention(x, q, q), q),
+        "k_interval_attention v": (lambda x: kia.k_interval_attention(q, q, x, rotary=plan), q),
         "window_attention q": (lambda x: kia.window_attention(x, k, k, 4), q),
         "window_attention v": (lambda x: kia.window_attention(q, k, x, 4), k),
-        "window_attention rotary": (lambda x: kia.window_attention(q, x, k, 4, rotary=plan), k),
+        "window_attention rotary": (lambda x: kia.window_attention(q, k, x, 4, rotary=plan), k),
         "window_forward": (lambda x: kia.window_forward(q, x, k, 4)[0], k),
         "window_backward": (lambda x: kia.window_backward(q, k, k, q, x, lse, 4)[0], q),
         "cache4_write": (lambda x: kia.cache4_write(k, x, cache, table, one), k),
