@@ -375,6 +375,15 @@ def _window_checked(q, k, window, sinks, lengths):
         _ints("lengths", lengths, (like.shape[0],), like.device)
 
 
+def _lse(like, t):
+    """Device pointer of a call's lse, contiguous [B, heads, T] (it is read and written
+    flat: any other shape would be other rows)."""
+    import torch
+    if t.shape != like.shape[:3]:
+        raise KiaError(f"lse has shape {tuple(t.shape)}, expected {tuple(like.shape[:3])}")
+    return _buffer("lse", t, torch.float32, 0, like.device, 16)
+
+
 def _window_fwd(c, views, lse, stream=None):
     like, Hkv, window, sinks, n = c
     B, H, T, d = like.shape
@@ -383,23 +392,19 @@ def _window_fwd(c, views, lse, stream=None):
 
 
 def _window_bwd(c, views, lse, ws, grads, stream=None):
-    import torch
     like, Hkv, window, sinks, n = c
     B, H, T, d = like.shape
-    lse = _buffer("lse", lse, torch.float32, B * H * T, like.device, 16)
-    _call(_kia.load().kia_window_bwd, like.device, stream, *views, lse, n, ws, *grads, B, H, Hkv, T,
+    _call(_kia.load().kia_window_bwd, like.device, stream, *views, _lse(like, lse), n, ws, *grads, B, H, Hkv, T,
           d, window, sinks, like.code)
 
 
 def kia_window_fwd(q, k, v, o, lse, window, sinks=0, lengths=None, stream=None):
     """Forward into o (as q) and lse ([B, H, T] float32)."""
-    import torch
     c = _window_checked(q, k, window, sinks, lengths)
     like, Hkv = c[:2]
-    B, H, T, _ = q.shape
     views = (like.view("q", q), like.view("k", k, Hkv), like.view("v", v, Hkv),
              like.view("o", o, out=True))
-    _window_fwd(c, views, _buffer("lse", lse, torch.float32, B * H * T, q.device, 16), stream)
+    _window_fwd(c, views, _lse(like, lse), stream)
 
 
 def kia_window_bwd(q, k, v, o, dO, lse, ws, dq, dk, dv, window, sinks=0, lengths=None,
