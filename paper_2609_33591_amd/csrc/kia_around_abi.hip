@@ -62,7 +62,7 @@ extern "C" int kia_rotary(const kia_view *q, const kia_view *q_out, const kia_vi
   if (!freq) return KIA_ERR_NULL;
   if ((uintptr_t)freq & 7u || (uintptr_t)positions & 3u) return KIA_ERR_ALIGN;
   if (positions_sb < 0 || (int64_t)first + T > INT_MAX) return KIA_ERR_SHAPE;
-  if ((int64_t)B * T > INT_MAX || (int64_t)H + Hkv > 65535) return KIA_ERR_SHAPE;
+  if ((int64_t)B * T > INT_MAX || (int64_t)H + (keys ? Hkv : 0) > 65535) return KIA_ERR_SHAPE;
   int vw = 0;
   const int tokens = rotary_tokens(T, d, rot, dtype, vw);
   if (too_many((double)B * ((T + tokens - 1) / tokens))) return KIA_ERR_SHAPE;
