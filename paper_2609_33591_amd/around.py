@@ -276,6 +276,8 @@ def _rotary_call(like, views, Hkv, plan, positions, back, stream=None):
     if isinstance(positions, torch.Tensor):
         if positions.dim() == 1:
             ptr = _ints("positions", positions, (T,), like.device)
+        elif positions.dim() == 2 and positions.shape[0] == 1:
+            ptr = _ints("positions", positions, (1, T), like.device)
         else:
             ptr, sb = _ints("positions", positions, (B, T), like.device), T
     elif positions is not None:
@@ -291,8 +293,8 @@ def _rotary_call(like, views, Hkv, plan, positions, back, stream=None):
 
 def kia_rotary(q, k, q_out, k_out, plan, positions=None, back=False, stream=None):
     """Rotates q (and k; None: only q) into q_out (k_out), which may be q and k.
-    positions: int32 [B, T] or [T], the first position as an integer, or None
-    (0). back: by the negative angle, the gradient of the rotation."""
+    positions: int32 [B, T], or [1, T] or [T] for every sequence, the first position
+    as an integer, or None (0). back: by the negative angle, the gradient of the rotation."""
     like = _Like("q", q)
     views, Hkv = [like.view("q", q), like.view("q_out", q_out, out=True), None, None], 0
     if k is not None:

@@ -230,9 +230,9 @@ static PyObject *rotary(PyObject *self, PyObject *const *a, Py_ssize_t na) {
   if (PyLong_CheckExact(a[3])) {
     if (!an_int(a[3], INT32_MIN, &first)) NONE;
   } else if (!ints_of(a[3], &q, 1, &q.n[2], 1, &pos)) {
-    const long n[2] = {q.n[0], q.n[2]};
-    if (!ints_of(a[3], &q, 2, n, 0, &pos)) NONE;
-    sb = q.n[2];
+    const long n[2] = {q.n[0], q.n[2]}, one[2] = {1, q.n[2]}; /* [1, T]: for every sequence */
+    if (ints_of(a[3], &q, 2, n, 0, &pos)) sb = q.n[2];
+    else if (!ints_of(a[3], &q, 2, one, 0, &pos)) NONE;
   }
   const double factor = PyFloat_AsDouble(a[5]);
   if (PyErr_Occurred()) {
