@@ -103,8 +103,10 @@ int check_window(int B, int H, int Hkv, int T, int d, int window, int sinks, int
   return KIA_OK;
 }
 
-// (The key blocks' parts are less than 2560 more than the blocks, and their sums' workgroups
-// less than 40960 in all.)
+// (The key blocks' parts are less than 2816 more than the blocks: a part has `fine` tiles at
+// least, all blocks together at most 512 times `most`, and most / fine is at most 11 / 2, by
+// the division rounded down. So less than 2816 blocks have several parts, and their sums less
+// than 45056 workgroups.)
 bool window_too_many(int B, int H, int T) { return too_many((double)B * H * ((T + 63) / 64) + 4096); }
 
 WinArgs window_args(int B, int H, int Hkv, int T, int d, int window, int sinks, int dtype) {
@@ -117,8 +119,9 @@ WinArgs window_args(int B, int H, int Hkv, int T, int d, int window, int sinks, 
   // The key blocks' lists of query tiles, in parts of at most all tiles over the workgroups
   // that the chip holds (two a CU, of d = 128 in fp32 one), and of two tiles at least (four
   // of d = 128 in bf16; its sums cost as much to add). Blocks of first tokens, which every
-  // query sees, are cut up to four times finer, so that they fill the gaps that the others
-  // leave. Measured, dK and dV and the sum (us) with 8 / 4 / 2 tiles at least, windows of 256:
+  // query sees, are cut about four times finer (five and a half at most), so that they fill
+  // the gaps that the others leave. (The places are those of the whole chip and not of the
+  // device at hand: the workspace, whose size goes by the parts, is then the same on all.) Measured, dK and dV and the sum (us) with 8 / 4 / 2 tiles at least, windows of 256:
   //   d = 64, T = 1024, 12 heads, fp32            53 + 6 / 43 + 7 / 35 + 8
   //   d = 64, T = 500, 16 heads over 4, bf16      24 + 6 / 16 + 6 / 13 + 6
   //   d = 128, T = 1024, 16 heads over 4, bf16    34 + 7 / 27 + 8 / 29 + 10
