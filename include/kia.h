@@ -547,9 +547,9 @@ typedef struct kia_view {
  * turns by the angle a = p * freq[n] (radians; freq: rot/2 doubles on the
  * device): (x, y) -> factor * (x cos a - y sin a, y cos a + x sin a). The
  * other channels are copied. p is positions[b*positions_sb + t] (int32, any
- * sign) or, with positions NULL, first + t. back = 1 takes -a: the gradient.
- * Angles are taken in fp64. k and k_out may both be NULL (Hkv is then not
- * looked at). q_out and k_out may be q and k.
+ * sign; positions_sb 0: the same for all) or, with positions NULL, first + t.
+ * back = 1 takes -a: the gradient. Angles are taken in fp64. k and k_out may
+ * both be NULL (Hkv is then not looked at). q_out and k_out may be q and k.
  */
 #define KIA_ROTARY_HALF 0
 #define KIA_ROTARY_NEIGHBOURS 1
@@ -569,14 +569,21 @@ int kia_rotary(const kia_view *q, const kia_view *q_out, const kia_view *k,
  *   has o = 0 and lse = -infinity, and no gradient.
  * Rows at or past lengths[b] (clamped to [0, T]) of q, k, v and dO are never
  * read as values, and what a query does not see has no influence on it,
- * infinities and NaNs included.
+ * infinities and NaNs included. A key whose score is -infinity has weight 0
+ * for that query and no gradient from it; dq of the query is NaN in the
+ * channels where the key is not finite (0 times them). An infinite v or dO
+ * under a weight of 0 gives an infinity or a NaN where it counts.
  * Backward: dq, dk, dv of a loss with gradient dO at o, from the forward's o
  * and lse (dk and dv summed over the query heads of a key head); 0 in rows
  * past their sequence. `ws`: kia_window_ws_bytes bytes, 256-byte aligned,
  * uninitialized.
  * bf16: the weights and the score gradients enter their products rounded to
- * bf16 (2^-8 of each; for dq with d <= 32 in two such pieces). fp32: every
- * product is an fp32 product.
+ * bf16 (2^-8 of each; for dq with d <= 32 in two such pieces). The sum dO.o in
+ * the score gradients is taken from the rounded o; its error is corrected for
+ * dk, and for dq where window + sinks (or the query's position) is at most
+ * 128: in longer rows that few keys take, dq is off by up to 5 times its own
+ * rounding (2-norm; else at most 1.5 times). fp32: every product is an fp32
+ * product.
  */
 int kia_window_fwd(const kia_view *q, const kia_view *k, const kia_view *v,
                    const kia_view *o, float *lse, const int32_t *lengths,

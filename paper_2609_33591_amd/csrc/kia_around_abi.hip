@@ -271,9 +271,9 @@ int cache_copy(bool write, const kia_view *k, const kia_view *v, void *cache, in
 
 // The launch shape: row tiles of 16, and the parts that their keys are cut into, all
 // resident at once: three workgroups a CU in bf16, two in fp32 (registers). More parts
-// cost more joining than the balance gains (32 sequences of 16 000 keys, softmax, bf16:
-// 67 / 59 / 69 us with two / three / six a CU; fp32, 16 sequences: 42 / 48 with two /
-// three). A part has 128 keys at least, 32 for each wave; up to 256 keys one part, and no
+// cost more joining than the balance gains (32 sequences of 16 000 keys, 16 heads of 128
+// over 4, softmax, bf16: 67 / 59 / 69 us with two / three / six a CU; fp32, 16 sequences: 42
+// / 48 with two / three). A part has 128 keys at least, 32 for each wave; up to 256 keys one part, and no
 // join (a call alone of 200 keys: bf16 24 us, 28 in two parts, fp32 32 and 34; of 400: 25
 // and 28, 35 and 34).
 void cached_shape(CachedArgs &a, int dtype, int cus) {

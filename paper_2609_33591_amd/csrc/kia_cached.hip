@@ -19,12 +19,15 @@
 // depends on the row's extrema, so a first pass over the keys alone (a third of the
 // bytes) finds them; the weights are absolute then and the parts' sums just add.
 // 32 sequences of up to 32 000 keys, 16 heads of 128 over 4, LERP: extrema 35 us (144 MB,
-// 4.2 TB/s), weights 74 us (289 MB, 3.9 TB/s), join 6.
+// 4.2 TB/s), weights 74 us (289 MB, 3.9 TB/s), join 6; Nearest takes as long.
 //
 // bf16 queries: scores are sums of exact products, weights are rounded to bf16 (2^-8
-// of each) for the product with V. fp32 queries and weights go as three bf16 pieces
-// (exact for 2^-100 to 2^126; smaller ones lose less than 2^-133), which the idle matrix
-// unit takes for free. Sums, extrema and statistics are fp32.
+// of each) for the product with V: an output's error is up to 1.4 times that of its own
+// rounding (2-norm; with weights in two pieces 1.0 times, and their pass takes 6 to 8%
+// longer: 76 -> 81 us above, the softmax of kia_around_abi.hip's figures 59 -> 63). fp32
+// queries and weights go as three bf16 pieces (exact for 2^-100 to 2^126; smaller ones lose
+// less than 2^-133), which the idle matrix unit takes for free. Sums, extrema and
+// statistics are fp32.
 #include <limits.h>
 
 #include "kia_cache.hpp"
@@ -179,9 +182,10 @@ __device__ __forceinline__ int64_t slot_of(const CachedArgs &a, int hk, int tile
 // FEW: a key head has at most four rows. The 16 columns then hold them four times over, and
 // of the four keys that a lane has scores of it takes one's weight, the (l / 4)-th: a
 // quarter of the work on weights. The interval weights are bound by that work: LERP over
-// the 32 sequences above 86 -> 76 us, Nearest with MinMax over 16 000 keys each 124 -> 107
-// and its extrema 73 -> 65. The softmax, whose maximum then crosses more lanes, is not
-// (118 and 119 us), nor are extrema without the minimum (fp32: 40 -> 45 us).
+// the 32 sequences above 86 -> 76 us; 32 sequences of 16 000 keys, 32 heads of 128 over 8,
+// Nearest with MinMax 124 -> 107 and its extrema 73 -> 65. The softmax, whose maximum then
+// crosses more lanes, is not (118 and 119 us there), nor are extrema without the minimum
+// (16 of those sequences in fp32: 40 -> 45 us).
 template <typename TI, int D, int PASS, int CALIB, int RECON, bool FEW>
 __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
   constexpr int NP = Pieces<TI>::N, N = D / 32, NT = D / 16, NE = FEW ? 1 : 4;

@@ -4,8 +4,9 @@
  * take 10 to 25 us in Python, this module a third of that. Each function makes the call
  * if every argument is what the kernels take as it is (types, shapes, one device that
  * is the current one, layouts), and returns None otherwise: the caller then goes on in
- * Python, which copies what needs copying and says what is wrong. Only attributes and
- * methods of the tensors are used, no internals of torch.
+ * Python, which copies what needs copying and says what is wrong. Of the tensors only
+ * attributes and methods are used; the current device and stream come from torch._C
+ * (_cuda_getDevice, _cuda_getCurrentRawStream).
  */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>

@@ -17,13 +17,18 @@
 //
 // bf16 runs on v_mfma_f32_32x32x16_bf16; the weights p and dS, the products'
 // computed operands, are rounded to bf16 (2^-8 of each), all sums and statistics are
-// fp32. fp32 runs on v_mfma_f32_32x32x2_f32 throughout and rounds nothing.
+// fp32. Over random values such a rounding adds as much again as the output's own: errors
+// of sqrt(2) times that one in the 2-norm (1.3 to 1.45 measured), and the goal is 1.5 times.
+// With p and dS in two pieces it is 1.0 times, and the training step of win_fwd_kernel's
+// figures takes 16% longer, the prompt there 19%. fp32 runs on v_mfma_f32_32x32x2_f32
+// throughout: no operand is rounded, sums are fp32.
 //
 // A key that a query does not see has no influence on it, whatever it holds: its score
 // is replaced before it is used, and in tiles where some pair is masked, rows that hold
 // infinities or NaNs go to LDS with zeros in their place, and what they do to the rows
 // that see them is done apart (add_bad, bad_rows): a branch that few calls ever take,
-// kept small because its registers count for the loop it stands in.
+// kept small because its registers count for the loop it stands in. Rows of no weight
+// (past the end, or of no finite score) are masked and set to 0, never multiplied by it.
 
 #include "kia_around.hpp"
 #include "kia_host.hpp"
@@ -37,10 +42,11 @@ template <typename TI> constexpr bool is_f32 = sizeof(TI) == 4;
 
 // ---- rows in LDS ---------------------------------------------------------------
 // A [ROWS, D] block of rows of any stride, rows at or past `end` as zeros. The row
-// stride in LDS is D plus 32 bytes in bf16, so that both 16-byte reads of eight rows and
-// transposing reads of four fall in distinct banks (with D plus 16 the latter overlap:
-// the 8k prompt 135 against 130 us), and D plus 16 in fp32, whose columns are read one
-// by one.
+// stride in LDS is D plus 16 bytes in fp32, whose columns are read one by one, without
+// bank conflicts. In bf16, where 16-byte reads of rows and transposing reads meet, it is D
+// plus 32 bytes, by measurement: dK and dV at d = 128 take 152 us, with 16 / 48 / 64 bytes
+// 155 / 149 / 286, and the forward 4 to 6% more with 16 or 48. Conflicts are still 12 to 14%
+// of all cycles there.
 template <typename TI, int D, int ROWS, int NT> struct Rows {
   static constexpr int V = 16 / sizeof(TI), RS = D + (is_f32<TI> ? 4 : 16), SIZE = ROWS * RS;
   static constexpr int PER = ROWS * D / V, PF = (PER + NT - 1) / NT, RPP = NT * V / D;
@@ -499,7 +505,11 @@ __global__ __launch_bounds__(256, (Shape<TI, D, RG>::FWD_OCC)) void win_fwd_kern
 // query blocks whose rows see few keys, where the error would pass all others, walk
 // their keys once before for that sum alone. (2-norm errors of dQ and dK against 64 bits at
 // d = 128: window 2 4.5e-3 -> 2.4e-3, window 512 2.6e-3 -> 2.4e-3; the output's rounding
-// alone is 1.65e-3. Beside rows of over 128 keys the error is lost in the others.)
+// alone is 1.65e-3.) dQ of longer rows takes D as it is: with scores of a standard deviation
+// of 1 its error is lost in the others; where few keys take such a row, dS is small beside
+// D's error, and dQ is off by more (deviations of 2 / 4 / 9 / 25: at most 1.8 / 2.4 / 3.8 / 4.8
+// times the output's own rounding). Two walks for every row would hold that at 1.5, with 1.6
+// times the time of dQ.
 // In small heads a score has a large share of each key (q / sqrt(d) of it on average), and
 // the roundings of a row's dS, which add up to 0 without them, carry that share into dQ:
 // up to 32 channels dS goes in two bf16 pieces (window 217, 100 first tokens, T = 4531: d =
@@ -664,9 +674,9 @@ struct KeyPart {
 // order: no atomics, so that the gradients repeat bit for bit.
 // At d = 128 the keys and values stay in LDS: with them in registers the sums (128) leave
 // too few (fp32, 16 heads, T = 2048, window 512: 76 spilled, 350 us against 212; in bf16
-// one wave a SIMD, with room for all, takes 271 us where two take 151). The training step above: 150 us, 400 TFLOP/s, bound by two
-// workgroups a CU that wait for LDS and for each other (matrix unit busy 18%, vector
-// unit 22%, LDS 36% of the time).
+// one wave a SIMD, with room for all, takes 271 us where two take 151). The training step
+// above: 150 us, 400 TFLOP/s, bound by two workgroups a CU that wait for LDS and for each
+// other (matrix unit busy 18%, vector unit 23%, LDS 36% of the time).
 template <typename TI, int D>
 __global__ __launch_bounds__(256, is_f32<TI> && D == 128 ? 1 : 2) void win_dkv_kernel(WinArgs a) {
   constexpr int NT = 256, NC = D >= 32 ? D / 32 : 1;
