@@ -185,16 +185,22 @@ def _int(name, x, low):
     return x
 
 
+_modes = []  # torch.autograd.forward_ad and torch's tracing state, looked up once
+
+
 def _eager(*tensors):
     """Refuses what a call would leave out without a word, since the kernels see data
     alone: forward-mode derivatives of its inputs (their tangents), and its place in a
     trace."""
-    import torch
-    ad = torch.autograd.forward_ad
-    if ad._current_level >= 0 and any(isinstance(x, torch.Tensor) and ad.unpack_dual(x).tangent is not None
-                                      for x in tensors):
+    if not _modes:
+        import torch
+        _modes.extend((torch.autograd.forward_ad, torch._C._get_tracing_state))
+    ad, trace = _modes
+    if ad._current_level < 0 and trace() is None:
+        return
+    if any(hasattr(x, "requires_grad") and ad.unpack_dual(x).tangent is not None for x in tensors):
         raise KiaError("libkia has no forward-mode derivatives: an input has a tangent")
-    if torch.jit.is_tracing():
+    if trace() is not None:
         raise KiaError("libkia's calls cannot be traced")
 
 
