@@ -572,7 +572,9 @@ int kia_rotary(const kia_view *q, const kia_view *q_out, const kia_view *k,
  * infinities and NaNs included. A key whose score is -infinity has weight 0
  * for that query and no gradient from it; dq of the query is NaN in the
  * channels where the key is not finite (0 times them). An infinite v or dO
- * under a weight of 0 gives an infinity or a NaN where it counts.
+ * under a weight of 0 gives an infinity or a NaN where it counts. A row's sum
+ * is divided by the sum of its weights (up to 2^8 each) at the end: with |v|
+ * below 2^96 no sum overflows.
  * Backward: dq, dk, dv of a loss with gradient dO at o, from the forward's o
  * and lse (dk and dv summed over the query heads of a key head); 0 in rows
  * past their sequence. `ws`: kia_window_ws_bytes bytes, 256-byte aligned,
@@ -652,6 +654,7 @@ int kia_cache4_read(const void *cache, int pages, int page,
  * For few tokens: keys are read once for every 16 rows of (T x H / Hkv).
  * bf16: weights are rounded to bf16 (2^-8 of each). fp32: queries and weights
  * keep all bits (from 2^-100 to 2^126; an infinite query element gives NaN).
+ * (With |v| below 2^88 no sum overflows; see kia_window_fwd.)
  * `ws`: kia_cache4_ws_bytes bytes, 256-byte aligned, uninitialized.
  */
 int kia_cache4_ws_bytes(int page, int width, int B, int H, int Hkv, int T,
