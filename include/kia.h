@@ -665,6 +665,92 @@ int kia_cache4_attn(const kia_view *q, const kia_view *o, const void *cache,
                     int T, int d, int K, int calib, float tau, int recon,
                     int window, int sinks, int dtype, void *stream);
 
+/*
+ * ---- Many and long texts from the cache ------------------------------------
+ *
+ * Timed as "kia_cache4_append", "kia_cache4_bounds", "kia_cache4_score" and
+ * "kia_cache4_select"; the attention as above.
+ *
+ * The bounds of a page's keys: bounds[pages][Hkv][2][d], bf16, 16-byte aligned,
+ * of each channel the least (0) and the largest (1) of what the cache stands for
+ * at the page's tokens, exact; NaN where one of them is NaN.
+ *
+ * Appends new tokens: q [B, H, T, d] and k, v [B, Hkv, T, d], token t at position
+ * p = starts[b] + t of its sequence. q is turned by p as kia_rotary does, into
+ * q_out (every token; rows of their own); k is turned, and k and v of tokens t <
+ * counts[b] (NULL: every t) are held as kia_cache4_write does. The turned key is
+ * rounded once, to its 4 bits: what is held is that of the exact rotation. With
+ * `bounds` (or NULL), the bounds of every page that a token went to are those
+ * of its tokens up to the last one written. No two tokens of a call may go
+ * to one place and, with bounds, no two sequences' to one page. T <= 2^24.
+ */
+int kia_cache4_append(const kia_view *q, const kia_view *q_out,
+                      const kia_view *k, const kia_view *v, void *cache,
+                      void *bounds, int pages, int page, const int32_t *table,
+                      int width, const int32_t *starts, const int32_t *counts,
+                      const double *freq, float factor, int layout, int B,
+                      int H, int Hkv, int T, int d, int rot, int dtype,
+                      void *stream);
+/* Bounds of the pages that hold positions starts[b] .. ends[b] - 1 of a
+ * sequence (clamped to the table), over their tokens before ends[b]. */
+int kia_cache4_bounds(const void *cache, void *bounds, int pages, int page,
+                      const int32_t *table, int width, const int32_t *starts,
+                      const int32_t *ends, int B, int Hkv, int d,
+                      void *stream);
+
+/*
+ * Selects pages: for query t of T at position i = lengths[b] - T + t and each
+ * key head, `count` of the pages 0 .. i / page of its sequence, as their
+ * numbers in the table, ascending, into list [B, Hkv, T, count] (int32); all
+ * of them where there are no more, and -1 behind them. The first `first` (>= 0)
+ * and the last `last` (>= 1; first + last <= count) are taken in any case, the
+ * others by the largest of the group's heads'
+ *   sum_c max(q_c lo_c, q_c hi_c),
+ * which no score q.k of the page passes; the lower number first between equals.
+ * The sums are fp64; one that is NaN counts as infinite. Table entries that
+ * name no page are not taken. For few tokens, and at most 64 KB of a key head's
+ * queries of a token in fp32 (else KIA_ERR_SHAPE).
+ * `ws`: kia_cache4_select_ws_bytes bytes, 256-byte aligned, uninitialized.
+ */
+int kia_cache4_select_ws_bytes(int page, int width, int B, int H, int Hkv,
+                               int T, int d, size_t *bytes);
+int kia_cache4_select(const kia_view *q, const void *bounds, int pages,
+                      int page, const int32_t *table, int width,
+                      const int32_t *lengths, void *ws, int32_t *list,
+                      int count, int first, int last, int B, int H, int Hkv,
+                      int T, int d, int dtype, void *stream);
+
+/*
+ * kia_cache4_attn over listed pages: query t sees of the keys j <= i of its
+ * sequence those on the pages that list[b, h / (H / Hkv), t] names (int32
+ * [B, Hkv, T, count], in any order; below 0 or past the table: none; a page
+ * that stands there twice counts twice). count <= 200000, count * page < 2^31.
+ */
+int kia_cache4_pages_ws_bytes(int page, int width, int count, int B, int H,
+                              int Hkv, int T, int d, size_t *bytes);
+int kia_cache4_attn_pages(const kia_view *q, const kia_view *o,
+                          const void *cache, int pages, int page,
+                          const int32_t *table, int width,
+                          const int32_t *lengths, const int32_t *list,
+                          int count, void *ws, int B, int H, int Hkv, int T,
+                          int d, int K, int calib, float tau, int recon,
+                          int dtype, void *stream);
+
+/*
+ * kia_cache4_attn for sequences that share their first `shared` tokens (a
+ * multiple of the page and of 32, at most width*page): the first shared / page
+ * entries of every sequence's table are taken from the first one's, and their
+ * keys and values read once for all. No window.
+ */
+int kia_cache4_shared_ws_bytes(int page, int width, int shared, int B, int H,
+                               int Hkv, int T, int d, size_t *bytes);
+int kia_cache4_attn_shared(const kia_view *q, const kia_view *o,
+                           const void *cache, int pages, int page,
+                           const int32_t *table, int width,
+                           const int32_t *lengths, int shared, void *ws, int B,
+                           int H, int Hkv, int T, int d, int K, int calib,
+                           float tau, int recon, int dtype, void *stream);
+
 /* Human-readable text for a return code (static storage). */
 const char *kia_strerror(int code);
 

@@ -644,7 +644,9 @@ def _attention_out_dtype(q, k, v):
 # ------------------------------------------------- operators around the attention
 from . import around  # noqa: E402
 from .around import (  # noqa: E402,F401
-    Cache4, RotaryPlan, cache4_attention, cache4_read, cache4_write, kia_cache4_attn,
-    kia_cache4_bytes, kia_cache4_read, kia_cache4_write, kia_cache4_ws_bytes, kia_rotary,
-    kia_window_bwd, kia_window_fwd, kia_window_ws_bytes, new_cache4, rotary, rotary_plan,
-    window_attention, window_backward, window_forward)
+    Cache4, RotaryPlan, cache4_append, cache4_attention, cache4_bounds, cache4_read, cache4_select,
+    cache4_write, kia_cache4_append, kia_cache4_attn, kia_cache4_attn_pages, kia_cache4_attn_shared,
+    kia_cache4_bounds, kia_cache4_bytes, kia_cache4_pages_ws_bytes, kia_cache4_read, kia_cache4_select,
+    kia_cache4_select_ws_bytes, kia_cache4_shared_ws_bytes, kia_cache4_write, kia_cache4_ws_bytes,
+    kia_rotary, kia_window_bwd, kia_window_fwd, kia_window_ws_bytes, new_bounds4, new_cache4, rotary,
+    rotary_plan, window_attention, window_backward, window_forward)

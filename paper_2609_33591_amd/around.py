@@ -1,6 +1,7 @@
 """The operators around K-interval attention: rotary positions, softmax attention
 with a sliding window and visible first tokens, a paged key/value cache in 4
-bits, and attention of new tokens over it.
+bits, and attention of new tokens over it: over all of a text, over the pages that
+their bounds select, or behind tokens that a batch shares.
 
 The ``kia_*`` functions carry the names of the C-ABI entry points of
 ``include/kia.h`` and only marshal arguments, on buffers of the caller's; the
@@ -42,7 +43,15 @@ def declare(lib):
             ("kia_cache4_write", [V, V, P, I, I, P, I, P, P] + [I] * 5 + [P]),
             ("kia_cache4_read", [P, I, I, P, I, P, P, V, V] + [I] * 5 + [P]),
             ("kia_cache4_ws_bytes", [I] * 9 + [S]),
-            ("kia_cache4_attn", [V, V, P, I, I, P, I, P, P] + [I] * 7 + [F] + [I] * 4 + [P])):
+            ("kia_cache4_attn", [V, V, P, I, I, P, I, P, P] + [I] * 7 + [F] + [I] * 4 + [P]),
+            ("kia_cache4_append", [V] * 4 + [P, P, I, I, P, I, P, P, P, F] + [I] * 8 + [P]),
+            ("kia_cache4_bounds", [P, P, I, I, P, I, P, P, I, I, I, P]),
+            ("kia_cache4_select_ws_bytes", [I] * 7 + [S]),
+            ("kia_cache4_select", [V, P, I, I, P, I, P, P, P] + [I] * 9 + [P]),
+            ("kia_cache4_pages_ws_bytes", [I] * 8 + [S]),
+            ("kia_cache4_attn_pages", [V, V, P, I, I, P, I, P, P, I, P] + [I] * 7 + [F, I, I, P]),
+            ("kia_cache4_shared_ws_bytes", [I] * 8 + [S]),
+            ("kia_cache4_attn_shared", [V, V, P, I, I, P, I, P, I, P] + [I] * 7 + [F, I, I, P])):
         fn = getattr(lib, name)
         fn.argtypes, fn.restype = types, I
 
@@ -680,14 +689,19 @@ def kia_cache4_attn(q, o, cache, table, lengths, ws, K=4, calib="fwm", tau=8.0, 
 
 
 def cache4_attention(q, cache, table, lengths, K=4, calib="fwm", tau=8.0, recon="nearest",
-                     window=0, sinks=0):
+                     window=0, sinks=0, pages=None, shared=0):
     """Allocates the output (as q) and the workspace and runs kia_cache4_attn; the
-    operator's arguments are those of k_interval_attention. Forward only."""
+    operator's arguments are those of k_interval_attention. Forward only.
+    pages: only over these pages of each token and key head (cache4_select's, or any
+    int32 [B, heads, T, count] of their numbers in the table). shared: the first tokens
+    that all sequences have on the same pages, computed once for all."""
     import torch
     if q.requires_grad and torch.is_grad_enabled():
         raise KiaError("attention over a 4-bit cache is forward only: call it under torch.no_grad")
     _eager(q)
     op = _kia._op(K, calib, tau, recon, 0, 0, 0)
+    if pages is not None or shared:
+        return _served(q, cache, table, lengths, op, window, sinks, pages, shared)
     made = _fast().cache4_attention(q, cache.data, cache.page, cache.d, table, lengths, *op[:4],
                                     window, sinks)
     if made is not None:
@@ -698,4 +712,230 @@ def cache4_attention(q, cache, table, lengths, K=4, calib="fwm", tau=8.0, recon=
     ws = torch.empty(need, dtype=torch.uint8, device=like.device)
     _cache4_attn(like, args, vq, vo, ws.data_ptr(), cache.heads,
                  (K, calib, tau, recon), window, sinks)
+    return o
+
+
+# ---- many and long texts from the cache ----------------------------------------------
+def _bytes(name):
+    """The binding of a workspace size."""
+    def call(*args) -> int:
+        n = ctypes.c_size_t(0)
+        _kia._check(getattr(_kia.load(), name)(*args, ctypes.byref(n)))
+        return n.value
+    call.__name__ = name
+    return call
+
+
+kia_cache4_select_ws_bytes = _bytes("kia_cache4_select_ws_bytes")
+kia_cache4_pages_ws_bytes = _bytes("kia_cache4_pages_ws_bytes")
+kia_cache4_shared_ws_bytes = _bytes("kia_cache4_shared_ws_bytes")
+
+
+@functools.lru_cache(maxsize=1024)
+def _ws_on(device, size, *args) -> int:
+    import torch
+    if device.type != "cuda":
+        raise KiaError("libkia takes device tensors only")
+    with torch.cuda.device(device):  # (the size goes by the device's compute units)
+        return size(*args)
+
+
+def new_bounds4(cache):
+    """Bounds of a cache's pages, to be filled: bfloat16 [pages, heads, 2, d] (the least
+    and the largest key of each channel)."""
+    import torch
+    return torch.zeros((cache.pages, cache.heads, 2, cache.d), dtype=torch.bfloat16,
+                       device=cache.data.device)
+
+
+def _bounds(cache, bounds):
+    import torch
+    if not isinstance(bounds, torch.Tensor) or bounds.dtype != torch.bfloat16 or \
+            bounds.shape != (cache.pages, cache.heads, 2, cache.d):
+        raise KiaError(f"bounds must be a bfloat16 tensor [{cache.pages}, {cache.heads}, 2, {cache.d}]")
+    return _buffer("bounds", bounds, torch.bfloat16, 1, cache.data.device, 16)
+
+
+def _append(like, views, cache, table, starts, plan, counts, bounds, H, stream=None):
+    import torch
+    B, Hkv, T, d = like.shape
+    ptr, *rest = _cache_args(cache, table, like, Hkv)
+    freq = plan.freq
+    if freq.dim() != 1 or not 2 <= 2 * freq.shape[0] <= d:
+        raise KiaError(f"a plan's frequencies must be one to {d // 2} in one dimension for heads of "
+                       f"{d} channels, got shape {tuple(freq.shape)}")
+    if plan.layout not in LAYOUT:
+        raise KiaError(f"layout must be one of {sorted(LAYOUT)}, got {plan.layout!r}")
+    _call(_kia.load().kia_cache4_append, like.device, stream, *views, ptr,
+          None if bounds is None else _bounds(cache, bounds), *rest, _starts("starts", starts, like),
+          _ints("counts", counts, (B,), like.device),
+          _buffer("the plan's frequencies", freq, torch.float64, 1, like.device, 8), float(plan.factor),
+          LAYOUT[plan.layout], B, H, Hkv, T, d, 2 * freq.shape[0], like.code)
+
+
+def kia_cache4_append(q, q_out, k, v, cache, table, starts, plan, counts=None, bounds=None, stream=None):
+    """Appends tokens t < counts[b] (None: all) of k, v [B, heads, T, d] at positions
+    starts[b] + t of the sequences whose pages table [B, width] (int32) names, k turned
+    by its position, and q [B, H, T, d] turned into q_out. bounds (new_bounds4): those of
+    the pages that tokens went to are brought up to date."""
+    like, H = _Like("k", k), _heads(k, q)
+    _append(like, (like.view("q", q, H), like.view("q_out", q_out, H, True), like.view("k", k),
+                   like.view("v", v)), cache, table, starts, plan, counts, bounds, H, stream)
+
+
+def cache4_append(q, k, v, cache, table, starts, plan, counts=None, bounds=None):
+    """kia_cache4_append, for tensors of any layout; returns the turned q. Forward only."""
+    import torch
+    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
+        raise KiaError("appending to a 4-bit cache is forward only: call it under torch.no_grad")
+    _eager(q, k, v)
+    like, H = _Like("k", k), _heads(k, q)
+    q, vq = like.take("q", q, H)
+    k, vk = like.take("k", k)
+    v, vv = like.take("v", v)
+    out, vo = _new(q)
+    _append(like, (vq, vo, vk, vv), cache, table, starts, plan, counts, bounds, H)
+    return out
+
+
+def kia_cache4_bounds(cache, bounds, table, starts, ends, stream=None):
+    """Brings the bounds of the pages that hold positions starts[b] .. ends[b] - 1 up to
+    date, over their tokens before ends[b] (for tokens that kia_cache4_write held)."""
+    device = cache.data.device
+    if table.dim() != 2:
+        raise KiaError("table must be an int32 tensor [B, width]")
+    B, width = table.shape
+    if starts is None or ends is None:
+        raise KiaError("starts and ends must be int32 tensors")
+    if cache.data.data_ptr() % 16:
+        raise KiaError("the cache must be 16-byte aligned")
+    _call(_kia.load().kia_cache4_bounds, device, stream, cache.data.data_ptr(), _bounds(cache, bounds),
+          cache.pages, cache.page, _ints("table", table, (B, width), device), width,
+          _ints("starts", starts, (B,), device), _ints("ends", ends, (B,), device), B, cache.heads, cache.d)
+
+
+def cache4_bounds(cache, bounds, table, starts, ends):
+    """kia_cache4_bounds, on the current stream."""
+    _eager()
+    kia_cache4_bounds(cache, bounds, table, starts, ends)
+
+
+def _select(like, vq, cache, bounds, table, lengths, ws, pages, count, first, last, stream=None):
+    B, H, T, d = like.shape
+    _, *rest = _cache_args(cache, table, like)
+    if pages.shape != (B, cache.heads, T, count):
+        raise KiaError(f"pages has shape {tuple(pages.shape)}, expected {(B, cache.heads, T, count)}")
+    _call(_kia.load().kia_cache4_select, like.device, stream, vq, _bounds(cache, bounds), *rest,
+          _starts("lengths", lengths, like), ws, _ints("pages", pages, pages.shape, like.device), count,
+          first, last, B, H, cache.heads, T, d, like.code)
+
+
+def _select_checked(q, cache, table, count, first, last):
+    _int("count", count, 1), _int("first", first, 0), _int("last", last, 1)
+    if first + last > count:
+        raise KiaError(f"count must be at least first + last, got {count}")
+    like = _Like("q", q)
+    B, H, T, d = like.shape
+    width = _cache_args(cache, table, like)[4]
+    return like, _ws_on(like.device, kia_cache4_select_ws_bytes, cache.page, width, B, H, cache.heads, T, d)
+
+
+def kia_cache4_select(q, pages, cache, bounds, table, lengths, ws, first=1, last=1, stream=None):
+    """The pages that each of the last T tokens, q [B, H, T, d], reads of its sequence's
+    lengths[b] keys, into pages (int32 [B, heads, T, count]); ws: a uint8 device buffer of
+    kia_cache4_select_ws_bytes bytes, 256-byte aligned."""
+    import torch
+    if pages.dim() != 4:
+        raise KiaError(f"pages must be [B, heads, T, count], got shape {tuple(pages.shape)}")
+    count = pages.shape[3]
+    like, need = _select_checked(q, cache, table, count, first, last)
+    _select(like, like.view("q", q), cache, bounds, table, lengths,
+            _buffer("ws", ws, torch.uint8, need, like.device, 256), pages, count, first, last, stream)
+
+
+def cache4_select(q, cache, bounds, table, lengths, count, first=1, last=1):
+    """Allocates and returns the pages that kia_cache4_select takes: for each token and
+    key head `count` numbers of pages in the table, ascending, -1 behind them; the first and
+    the last ones and those whose bounds allow the highest score with any of the key
+    head's queries. For cache4_attention(..., pages=)."""
+    import torch
+    _eager(q)
+    like, need = _select_checked(q, cache, table, count, first, last)
+    q, vq = like.take("q", q)
+    B, H, T, d = like.shape
+    pages = torch.empty((B, cache.heads, T, count), dtype=torch.int32, device=like.device)
+    ws = torch.empty(need, dtype=torch.uint8, device=like.device)
+    _select(like, vq, cache, bounds, table, lengths, ws.data_ptr(), pages, count, first, last)
+    return pages
+
+
+def _pages_checked(q, cache, table, lengths, pages):
+    """(what the tensors have in common, arguments up to the workspace, its bytes)"""
+    import torch
+    if not isinstance(pages, torch.Tensor) or pages.dim() != 4:
+        raise KiaError("pages must be an int32 tensor [B, heads, T, count]")
+    like = _Like("q", q)
+    B, H, T, d = like.shape
+    args, count = _cache_args(cache, table, like), pages.shape[3]
+    n, ptr = _starts("lengths", lengths, like), _ints("pages", pages, (B, cache.heads, T, count), like.device)
+    need = _ws_on(like.device, kia_cache4_pages_ws_bytes, cache.page, args[4], count, B, H, cache.heads, T, d)
+    return like, (*args, n, ptr, count), need
+
+
+def _shared_checked(q, cache, table, lengths, shared):
+    like = _Like("q", q)
+    B, H, T, d = like.shape
+    args = _cache_args(cache, table, like)
+    if _int("shared", shared, 1) % max(32, cache.page):
+        raise KiaError(f"shared must be a multiple of {max(32, cache.page)} tokens, got {shared}")
+    if shared > args[4] * cache.page:
+        raise KiaError(f"shared passes the table's {args[4] * cache.page} tokens, got {shared}")
+    need = _ws_on(like.device, kia_cache4_shared_ws_bytes, cache.page, args[4], shared, B, H, cache.heads, T, d)
+    return like, (*args, _starts("lengths", lengths, like), shared), need
+
+
+def _served_call(name, like, args, vq, vo, ws, heads, op, stream=None):
+    B, H, T, d = like.shape
+    K, calib, tau, recon = op[:4]
+    _call(getattr(_kia.load(), name), like.device, stream, vq, vo, *args, ws, B, H, heads, T, d, K, calib,
+          tau, recon, like.code)
+
+
+def kia_cache4_attn_pages(q, o, cache, table, lengths, pages, ws, K=4, calib="fwm", tau=8.0, recon="nearest",
+                          stream=None):
+    """kia_cache4_attn of which token t and key head h see only the pages that
+    pages[b, h, t] names; ws: kia_cache4_pages_ws_bytes bytes."""
+    import torch
+    like, args, need = _pages_checked(q, cache, table, lengths, pages)
+    _served_call("kia_cache4_attn_pages", like, args, like.view("q", q), like.view("o", o, out=True),
+                 _buffer("ws", ws, torch.uint8, need, like.device, 256), cache.heads,
+                 _kia._op(K, calib, tau, recon, 0, 0, 0), stream)
+
+
+def kia_cache4_attn_shared(q, o, cache, table, lengths, shared, ws, K=4, calib="fwm", tau=8.0, recon="nearest",
+                           stream=None):
+    """kia_cache4_attn for sequences whose first `shared` tokens are on the same pages
+    (those of the table's first row); ws: kia_cache4_shared_ws_bytes bytes."""
+    import torch
+    like, args, need = _shared_checked(q, cache, table, lengths, shared)
+    _served_call("kia_cache4_attn_shared", like, args, like.view("q", q), like.view("o", o, out=True),
+                 _buffer("ws", ws, torch.uint8, need, like.device, 256), cache.heads,
+                 _kia._op(K, calib, tau, recon, 0, 0, 0), stream)
+
+
+def _served(q, cache, table, lengths, op, window, sinks, pages, shared):
+    """cache4_attention over listed pages or behind shared tokens."""
+    import torch
+    if pages is not None and shared:
+        raise KiaError("pages and shared tokens are not taken together")
+    if window != 0 or sinks != 0:
+        raise KiaError("a window is not taken with pages or shared tokens")
+    if pages is not None:
+        name, (like, args, need) = "kia_cache4_attn_pages", _pages_checked(q, cache, table, lengths, pages)
+    else:
+        name, (like, args, need) = "kia_cache4_attn_shared", _shared_checked(q, cache, table, lengths, shared)
+    q, vq = like.take("q", q)
+    o, vo = _new(q)
+    ws = torch.empty(need, dtype=torch.uint8, device=like.device)
+    _served_call(name, like, args, vq, vo, ws.data_ptr(), cache.heads, op)
     return o

@@ -30,8 +30,11 @@ OBJECTS = {
     "kia_bwd.o": [("kia_bwd.hip", [f"-DKIA_HEAD={d}"]) for d in HEADS],
     "kia_bf16.o": [("kia_bf16.hip", [])],
     "kia_around.o": [("kia_around_abi.hip", []), ("kia_rotary.hip", []), ("kia_cache.hip", [])],
+    "kia_serve.o": [("kia_serve_abi.hip", []), ("kia_append.hip", []), ("kia_select.hip", [])],
     "kia_window.o": [("kia_window.hip", [f"-DKIA_HEAD={d}"]) for d in HEADS],
     "kia_cached.o": [("kia_cached.hip", [f"-DKIA_HEAD={d}"]) for d in HEADS[1:]],
+    "kia_served.o": [("kia_cached.hip", [f"-DKIA_HEAD={d}", f"-DKIA_MODE={m}"]) for d in HEADS[1:] for m in (1, 2)]
+                    + [("kia_prefix.hip", [f"-DKIA_HEAD={d}"]) for d in HEADS[1:]],
 }
 # (source, flags, object file) of every compilation
 UNITS = [(src, flags, obj if len(parts) == 1 else f"{obj[:-2]}_{i}.o")

@@ -2,6 +2,8 @@
 // attention: rotary positions, attention with a sliding window, the 4-bit cache.
 #pragma once
 
+#include <algorithm>
+
 #include "kia.h"
 #include "kia_device.hpp"
 
@@ -31,6 +33,17 @@ struct RotArgs {
   int first, layout, back, B, H, Hkv, T, d, rot;
   int tokens, per;  // tokens of a workgroup, rounds of heads of a share (the launcher's)
 };
+// Sine and cosine of the angle p * freq, to a quarter turn in 64 bits and from there in 32.
+__device__ __forceinline__ void turn_of(double p, double freq, float &s, float &c) {
+  // quarter turns: q whole ones and a rest of at most a half
+  const double x = p * freq * 0.63661977236758134308;
+  const double q = rint(x);
+  sincospif(0.5f * (float)(x - q), &s, &c);
+  // (a large q is a multiple of 4 plus these bits whatever its size)
+  const int k = (int)(q - 4.0 * floor(q * 0.25));
+  if (k & 1) { const float y = s; s = c; c = -y; }
+  if (k & 2) { s = -s; c = -c; }
+}
 // Tokens of a workgroup, and the channels of an access (vw): the widest whose pairs fill
 // whole chunks (16 bytes for most plans; a rotated part of 2 mod 4 channels takes
 // single values).
@@ -81,6 +94,50 @@ inline int cache_tokens(int B, int Hkv, int T, int d, int cus) {
 void launch_cache_write(const CacheArgs &a, int d, int dtype, int cus, hipStream_t s);
 void launch_cache_read(const CacheArgs &a, int d, int dtype, int cus, hipStream_t s);
 
+// ---- appended tokens and the bounds of pages (kia_append.hip) -----------------------
+struct AppendArgs {
+  CacheArgs c;
+  View q, qo;
+  uint32_t *bounds;  // [pages][Hkv][2][d] bf16, or nullptr
+  const double *freq;
+  float factor;
+  int layout, rot, H;
+  int spans;  // of a sequence's new tokens: 64 positions or a page, whichever is more
+};
+inline int append_spans(int T, int lpage) {
+  const int l = lpage > 6 ? lpage : 6;
+  return ((T - 1 + (1 << l) - 1) >> l) + 1;
+}
+void launch_append(const AppendArgs &a, int d, int dtype, int cus, hipStream_t s);
+void launch_bounds(const AppendArgs &a, int d, hipStream_t s);
+
+// ---- selected pages (kia_select.hip) ------------------------------------------------
+struct SelectArgs {
+  const uint32_t *bounds;
+  const int *table, *lengths;
+  View q;
+  uint64_t *score;  // workspace [B][Hkv][T][width]
+  int *list;        // [B][Hkv][T][count]
+  int pages, lpage, width, B, H, Hkv, T;
+  int count, first, last;
+  int tokens;  // of a workgroup that scores: their rows of a key head are in its LDS
+};
+void launch_select(const SelectArgs &a, int d, int dtype, hipStream_t s);
+
+// ---- attention over the cache (kia_cached.hip) ----------------------------------------
+// The rows of all sequences over the tokens that they share: b T G + t G + g is the row of
+// token t and head g of the group, in 16-row tiles.
+struct Prefix {
+  float *ext, *stat, *part;  // as CachedArgs'
+  int tiles, parts;
+  __host__ __device__ int64_t slot(int hk, int64_t row) const {
+    return (((int64_t)hk * tiles + row / 16) * parts) * 16 + row % 16;
+  }
+};
+// Row tiles that a wave takes.
+inline int prefix_tiles(int tiles, int d, int dtype) {
+  return tiles == 1 || (d == 128 && dtype == KIA_F32) ? 1 : 2;
+}
 struct CachedArgs {
   const uint8_t *cache;
   const int *table, *lengths;
@@ -91,7 +148,16 @@ struct CachedArgs {
   int K, calib, recon;
   float tau, scale;
   int tiles, shares;  // 16-row tiles of a key head's rows, parts of its keys (< 256)
+  // Over listed pages, and over what lies behind shared tokens: `tiles` of a token's, or a
+  // sequence's, rows, `parts` for each, `shares` in all for a row tile.
+  int parts;
+  const int *list;  // [B][Hkv][T][count]
+  int count;
+  int shared;  // tokens
+  Prefix pre;
 };
+// Entries of a list that one part takes, at most.
+constexpr int LISTED_MOST = 1024;
 // Floats of the workspace: the parts' extrema, their maxima and sums, their rows.
 struct CachedLayout {
   size_t ext, stat, part, total;
@@ -106,5 +172,8 @@ inline CachedLayout cached_layout(const CachedArgs &a, int d) {
   return l;
 }
 template <int D> void launch_cached(const CachedArgs &a, int dtype, hipStream_t s);
+template <int D> void launch_listed(const CachedArgs &a, int dtype, hipStream_t s);
+template <int D> void launch_shared(const CachedArgs &a, int dtype, hipStream_t s);
+template <int D> void launch_prefix(const CachedArgs &a, int dtype, bool extrema, hipStream_t s);
 
 }  // namespace kia

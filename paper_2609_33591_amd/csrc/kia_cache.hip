@@ -19,27 +19,6 @@ namespace {
 
 constexpr int CACHE_NT = 256;
 
-template <typename TI> __device__ __forceinline__ void load8(const TI *p, float (&x)[8]) {
-#pragma unroll
-  for (int g = 0; g < 2; ++g) {
-    const f32x4 v = load4(p + 4 * g);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[4 * g + e] = v[e];
-  }
-}
-__device__ __forceinline__ void store8(float *p, const float (&x)[8]) {
-#pragma unroll
-  for (int g = 0; g < 2; ++g)
-    *reinterpret_cast<f32x4 *>(p + 4 * g) =
-        f32x4{x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]};
-}
-__device__ __forceinline__ void store8(uint16_t *p, const float (&x)[8]) {
-  u32x4 w;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) w[e] = cvt_bf16x2(x[2 * e], x[2 * e + 1]);
-  *reinterpret_cast<u32x4 *>(p) = w;
-}
-
 // The place of a thread: eight channels of REP tokens, TOKENS apart, of one head's keys or
 // values. What is the same for all of a workgroup is in scalar registers.
 template <int D, int REP> struct Place {
@@ -66,92 +45,6 @@ template <int D, int REP> struct Place {
   }
 };
 
-// Codes of eight values in units of their group's scale (to the nearest level, an even
-// one between two, at most 6), and the values of eight codes: an instruction a pair.
-__device__ __forceinline__ uint32_t codes_of(const float (&x)[8]) {
-  uint32_t w = 0;
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], 1.f, 0);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], 1.f, 1);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], 1.f, 2);
-  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], 1.f, 3);
-}
-template <int S> __device__ __forceinline__ void pair_of(uint32_t w, float f, float (&x)[8]) {
-  const auto v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, S);
-  x[2 * S] = v[0] * f;
-  x[2 * S + 1] = v[1] * f;
-}
-__device__ __forceinline__ void values_of(uint32_t w, float f, float (&x)[8]) {
-  pair_of<0>(w, f, x);
-  pair_of<1>(w, f, x);
-  pair_of<2>(w, f, x);
-  pair_of<3>(w, f, x);
-}
-
-// Eight channels of one token into its page's block c.
-template <int D>
-__device__ __forceinline__ void hold(const float (&x)[8], uint8_t *c, int tok, int which, int oct,
-                                     int lpage) {
-  // (as bits: NaN above infinity above every finite value)
-  uint32_t top = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
-  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-  if (!c) return;
-  // top = 1.m 2^k: at most 6 2^(k - 2) if 1.m <= 1.5, and 6 2^(k - 1) otherwise
-  int e = (int)(top >> 23) - 127 - ((top & 0x7fffffu) <= 0x400000u ? 2 : 1);
-  e = min(max(e, -126), 125);
-  const bool bad = top >= 0x7f800000u;
-  const float f = __uint_as_float((uint32_t)(127 - e) << 23);
-  float y[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = x[i] * f;
-  const uint32_t w = bad ? 0u : codes_of(y);
-  const uint8_t s = bad ? 255 : (uint8_t)(e + 127);
-  const int codes = D / 2 << lpage, g = oct / 4;
-  if (which == 0) {
-    *reinterpret_cast<uint32_t *>(c + tok * (D / 2) + 4 * oct) = w;
-    if (oct % 4 == 0) c[codes + tok * (D / 32) + g] = s;
-  } else {
-    // four tokens side by side: column r holds D / 16 channels, D / 32 bytes a token
-    uint8_t *d = c + tok / 4 * (2 * D) + tok % 4 * (D / 32);
-    if constexpr (D == 128) {
-      *reinterpret_cast<uint32_t *>(d + oct * 16) = w;
-    } else if constexpr (D == 64) {
-      *reinterpret_cast<uint16_t *>(d + 2 * oct * 8) = (uint16_t)w;
-      *reinterpret_cast<uint16_t *>(d + (2 * oct + 1) * 8) = (uint16_t)(w >> 16);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) d[(4 * oct + i) * 4] = (uint8_t)(w >> (8 * i));
-    }
-    if (oct % 4 == 0) c[codes + tok / 4 * (D / 8) + 4 * g + tok % 4] = s;
-  }
-}
-
-// The codes of eight channels of a token in block c, and their group's scale byte.
-template <int D>
-__device__ __forceinline__ void held_of(const uint8_t *c, int tok, int which, int oct, int lpage,
-                                         uint32_t &w, uint32_t &s) {
-  const int codes = D / 2 << lpage, g = oct / 4;
-  if (which == 0) {
-    w = *reinterpret_cast<const uint32_t *>(c + tok * (D / 2) + 4 * oct);
-    s = c[codes + tok * (D / 32) + g];
-    return;
-  }
-  const uint8_t *d = c + tok / 4 * (2 * D) + tok % 4 * (D / 32);
-  if constexpr (D == 128) {
-    w = *reinterpret_cast<const uint32_t *>(d + oct * 16);
-  } else if constexpr (D == 64) {
-    w = *reinterpret_cast<const uint16_t *>(d + 2 * oct * 8) |
-        (uint32_t)*reinterpret_cast<const uint16_t *>(d + (2 * oct + 1) * 8) << 16;
-  } else {
-    w = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w |= (uint32_t)d[(4 * oct + i) * 4] << (8 * i);
-  }
-  s = c[codes + tok / 4 * (D / 8) + 4 * g + tok % 4];
-}
-
 template <typename TI, int D, int REP>
 __global__ __launch_bounds__(CACHE_NT) void write_kernel(CacheArgs a) {
   const Place<D, REP> p(a);
@@ -166,7 +59,9 @@ __global__ __launch_bounds__(CACHE_NT) void write_kernel(CacheArgs a) {
   for (int i = 0; i < REP; ++i) {
     int tok = 0;
     uint8_t *c = p.held(a, p.token(i), tok);
-    hold<D>(x[i], c, tok, p.which, p.oct, a.lpage);
+    uint32_t w, sc;
+    quantise(x[i], w, sc);
+    if (c) put<D>(w, sc, c, tok, p.which, p.oct, a.lpage);
   }
 }
 

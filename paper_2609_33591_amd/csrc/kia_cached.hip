@@ -28,62 +28,21 @@
 // queries and weights go as three bf16 pieces (exact for 2^-100 to 2^126; smaller ones lose
 // less than 2^-133), which the idle matrix unit takes for free. Sums, extrema and
 // statistics are fp32.
-#include <limits.h>
-
-#include "kia_cache.hpp"
+#include "kia_cached.hpp"
 #include "kia_host.hpp"
+
+#ifndef KIA_MODE
+#define KIA_MODE 0
+#endif
 
 namespace kia {
 namespace {
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
-// 32 keys at a time: two tiles of 16 and the next two on their way leave room for three
-// workgroups a CU in bf16 (162 registers; with 64 keys 217, two workgroups, and the
-// interval weights of 32 x 16 500 keys took 101 us against 88).
-constexpr int TILES = 2, CHUNK = 16 * TILES, NWAVE = 4;
-enum { PASS_SOFTMAX, PASS_EXTREMA, PASS_GRID };
-
-__device__ __forceinline__ f32x4 mma16(bf16x8 a, bf16x8 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-
-// byte `s` of a word of codes as two bf16
-template <int S> __device__ __forceinline__ uint32_t pair(uint32_t w, float scale) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, S));
-}
-__device__ __forceinline__ uint32_t pair_at(int s, uint32_t w, float scale) {
-  return s == 0 ? pair<0>(w, scale) : s == 1 ? pair<1>(w, scale) : s == 2 ? pair<2>(w, scale)
-                                                                     : pair<3>(w, scale);
-}
-__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
-
-// One lane's share of a chunk: codes and scales of its keys and values.
-template <int D, bool VALUES> struct Stage4 {
-  static constexpr int N = D / 32;  // words of codes of a 16-key tile
-  uint32_t k[TILES][N], v[VALUES ? TILES : 1][N], vs[VALUES ? TILES : 1];
-  uint8_t ks[TILES];
-  int ok;  // bit t: the tile's page is one of the cache's
-  // the values of token e (of the lane's four) of tile i as zeros
-  __device__ __forceinline__ void clear(int i, int e) {
-    vs[i] &= ~(0xffu << (8 * e));
-    if constexpr (D == 128) v[i][e] = 0;
-    else if constexpr (D == 64) v[i][e / 2] &= ~(0xffffu << (16 * (e % 2)));
-    else v[i][0] &= ~(0xffu << (8 * e));
-  }
-};
-template <int N> __device__ __forceinline__ void load_words(const uint8_t *p, uint32_t (&w)[N]) {
-  if constexpr (N == 4) {
-    const u32x4 x = *reinterpret_cast<const u32x4 *>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = x[i];
-  } else if constexpr (N == 2) {
-    const u32x2 x = *reinterpret_cast<const u32x2 *>(p);
-    w[0] = x[0], w[1] = x[1];
-  } else {
-    w[0] = *reinterpret_cast<const uint32_t *>(p);
-  }
-}
+// Which keys a row sees: all of its sequence's up to its own (within a window, and the
+// first ones); those of the pages that a list names for its token and key head; or those
+// behind the tokens that the batch shares (kia_prefix.hip takes these).
+enum { SEQUENCE, LISTED, BEHIND };
+constexpr int MODE = KIA_MODE;
 
 // A row's value over the lanes that share it, in a fixed order (with FEW the columns 8 and 4
 // on, by rotations of the 16; then 16 and 32 lanes on).
@@ -108,7 +67,8 @@ __device__ __forceinline__ float from_column(float x, int e) {
 // The chunks of keys that rows at positions lo .. hi see: the first tokens', then the
 // window's.
 struct Chunks {
-  int sink, low, count;
+  int sink = 0, low = 0, count = 0;
+  Chunks() = default;
   __device__ __forceinline__ Chunks(const CachedArgs &a, int lo, int hi) {
     const int from = max(0, lo - a.window + 1);  // (window INT_MAX: 0)
     low = from / CHUNK;
@@ -176,8 +136,45 @@ struct Share {
 };
 // Of part w of a key head's row tile: its place in the workspace, in rows.
 __device__ __forceinline__ int64_t slot_of(const CachedArgs &a, int hk, int tile, int w) {
-  return (((int64_t)hk * a.tiles + tile) * (a.shares + a.B) + w) * 16;
+  const int slots = MODE == SEQUENCE ? a.shares + a.B : a.shares;
+  return (((int64_t)hk * a.tiles + tile) * slots + w) * 16;
 }
+
+// What a workgroup takes: rows of tokens t0 on of sequence b, at positions lo .. hi, and
+// chunks c0 .. c1 of their keys, as part w - first of `parts`.
+struct Work {
+  int b, t0, rows, n, lo, hi, first, parts, c0, c1;
+  Chunks chunks;
+  __device__ __forceinline__ Work(const CachedArgs &a, int tile, int w) {
+    const int G = a.H / a.Hkv;
+    if constexpr (MODE == SEQUENCE) {
+      const Share share(a, tile, w, false);
+      b = share.b, first = share.first, parts = share.parts;
+      if (b < 0) return;
+    } else {
+      // (as many parts for every sequence, or for every token of one)
+      parts = a.parts, first = w / parts * parts;
+      b = MODE == LISTED ? w / parts / a.T : w / parts;
+    }
+    const Rows16 rows16(a, b, tile);
+    n = rows16.n;
+    if constexpr (MODE == LISTED) {
+      t0 = w / parts % a.T, rows = G;
+      lo = hi = n - a.T + t0;
+      chunks.count = lo < 0 ? 0 : (int)((((int64_t)a.count << a.lpage) + CHUNK - 1) / CHUNK);
+    } else {
+      t0 = 0, rows = a.T * G;
+      lo = rows16.lo, hi = rows16.hi;
+      chunks = rows16.chunks(a);
+      if constexpr (MODE == BEHIND) {
+        chunks.low = a.shared / CHUNK;
+        chunks.count = max(0, chunks.count - chunks.low);
+      }
+    }
+    c0 = (int)((int64_t)chunks.count * (w - first) / parts);
+    c1 = (int)((int64_t)chunks.count * (w - first + 1) / parts);
+  }
+};
 
 // FEW: a key head has at most four rows. The 16 columns then hold them four times over, and
 // of the four keys that a lane has scores of it takes one's weight, the (l / 4)-th: a
@@ -191,6 +188,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
   constexpr int NP = Pieces<TI>::N, N = D / 32, NT = D / 16, NE = FEW ? 1 : 4;
   constexpr bool VALUES = PASS != PASS_EXTREMA;
   __shared__ float red[NWAVE][16][2];
+  __shared__ int2 listed[MODE == LISTED ? LISTED_MOST : 1];
   __shared__ __attribute__((aligned(16))) float rows[VALUES ? NWAVE * 16 * (D + 4) : 4];
   const int tid = threadIdx.x, lane = tid & 63, kb = lane >> 4;
   const int slot = lane & 15;               // its key of a tile, its channels of the values
@@ -199,62 +197,60 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hk = blockIdx.x % a.Hkv, tile = (int)(blockIdx.x / a.Hkv) % a.tiles;
   const int w = blockIdx.x / (a.Hkv * a.tiles);
-  const Share share(a, tile, w, false);
-  if (share.b < 0) return;
-  const int b = share.b, G = a.H / a.Hkv, total = a.T * G;
-  const Rows16 rows16(a, b, tile);
-  const int lo = rows16.lo, hi = rows16.hi;
+  const Work work(a, tile, w);
+  if (work.b < 0) return;
+  const int b = work.b, G = a.H / a.Hkv, total = work.rows, lo = work.lo, hi = work.hi;
   // this lane's row, and its position (-1 or less: before the text, sees nothing)
-  const int r = min(tile * 16 + col, total - 1), t = r / G, h = hk * G + r % G;
-  const int pos = rows16.n - a.T + t;
-  const Chunks chunks = rows16.chunks(a);
-  const int c0 = (int)((int64_t)chunks.count * (w - share.first) / share.parts);
-  const int c1 = (int)((int64_t)chunks.count * (w - share.first + 1) / share.parts);
+  const int r = min(tile * 16 + col, total - 1), t = work.t0 + r / G, h = hk * G + r % G;
+  const int pos = work.n - a.T + t;
+  const int c0 = work.c0, c1 = work.c1;
 
   bf16x8 q[NP][N];
   {
     const TI *p = slice_of<TI>(a.q, b, h) + t * a.q.st + kb * (D / 4);
 #pragma unroll
-    for (int c = 0; c < N; ++c) {
-      if constexpr (NP == 1) {
-        q[0][c] = as_op(*reinterpret_cast<const u32x4 *>(p + 8 * c));
-      } else {
-        float x[8];
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const f32x4 v = load4(p + 8 * c + 4 * g);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[4 * g + e] = v[e];
-        }
-        bf16x8 y[3];
-        to_pieces<3>(x, y);
-#pragma unroll
-        for (int i = 0; i < 3; ++i) q[i][c] = y[i];
-      }
+    for (int c = 0; c < N; ++c) load_query<TI>(p + 8 * c, q, c);
+  }
+
+  // the list's pages of this part, and where they stand in the text (-1: none)
+  const int per = a.lpage - 4;  // (a page is 2^per tiles)
+  const int e0 = (2 * c0) >> per;
+  if constexpr (MODE == LISTED) {
+    const int *list = a.list + (((int64_t)b * a.Hkv + hk) * a.T + work.t0) * a.count;
+    const int e1 = min(min(a.count, e0 + LISTED_MOST), ((2 * c1 - 1) >> per) + 1);
+    for (int e = e0 + tid; e < e1; e += 64 * NWAVE) {
+      const int at = list[e];
+      const int page = at >= 0 && at < a.width ? a.table[(int64_t)b * a.width + at] : -1;
+      listed[e - e0] = make_int2(page >= 0 && page < a.pages ? page : -1, at);
     }
+    __syncthreads();
   }
 
   const int codes = D / 2 << a.lpage;
   const int64_t block = (int64_t)codes + (D / 32 << a.lpage);  // bytes of a head's block
-  auto load = [&](int j, Stage4<D, VALUES> &x) {
+  auto load = [&](int c, Stage4<D, VALUES> &x) {
     x.ok = 0;
 #pragma unroll
     for (int i = 0; i < TILES; ++i) {
-      const int key = j + 16 * i, at = key >> a.lpage;
-      int page = at < a.width ? a.table[(int64_t)b * a.width + at] : -1;
-      page = __builtin_amdgcn_readfirstlane(page);
-      const bool ok = page >= 0 && page < a.pages;
-      x.ok |= ok << i;
-      const uint8_t *kp = a.cache + cache_block<D>(ok ? page : 0, 0, hk, a.Hkv, a.lpage);
-      const int tok = key & ((1 << a.lpage) - 1);
-      load_words<N>(kp + (tok + slot) * (D / 2) + kb * (D / 8), x.k[i]);
-      x.ks[i] = kp[codes + (tok + slot) * (D / 32) + kb * (D / 4) / 32];
-      if constexpr (VALUES) {
-        const uint8_t *vp = kp + a.Hkv * block;
-        load_words<N>(vp + tok * (D / 2) + lane * (D / 8), x.v[i]);
-        x.vs[i] = *reinterpret_cast<const uint32_t *>(vp + codes + tok * (D / 32) + kb * (D / 8) +
-                                                      slot * (D / 16) / 32 * 4);
+      int key, page;
+      if constexpr (MODE == LISTED) {
+        const int e = (2 * c + i) >> per;
+        const int2 y = e < a.count ? listed[e - e0] : make_int2(-1, -1);
+        page = __builtin_amdgcn_readfirstlane(y.x);
+        // (a page past the table has no number, so no product overflows)
+        key = page < 0 ? 0
+                       : (__builtin_amdgcn_readfirstlane(y.y) << a.lpage) + ((2 * c + i) & ((1 << per) - 1)) * 16;
+        if (key > pos) page = -1;
+      } else {
+        key = work.chunks.at(c) + 16 * i;
+        const int at = key >> a.lpage;
+        page = at < a.width ? a.table[(int64_t)b * a.width + at] : -1;
+        page = __builtin_amdgcn_readfirstlane(page);
       }
+      const bool ok = page >= 0 && page < a.pages;
+      x.at[i] = key;
+      x.ok |= ok << i;
+      load_tile<D, VALUES>(a, ok ? page : 0, hk, key & ((1 << a.lpage) - 1), codes, block, lane, i, x);
     }
   };
 
@@ -263,12 +259,21 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
   float Mx = -INFINITY, Mn = INFINITY;
   if constexpr (PASS == PASS_GRID) {
     const float2 *e = reinterpret_cast<const float2 *>(a.ext) +
-                      slot_of(a, hk, tile, share.first) + col;
+                      slot_of(a, hk, tile, work.first) + col;
 #pragma unroll 4
-    for (int i = kb; i < share.parts; i += 4) {
+    for (int i = kb; i < work.parts; i += 4) {
       const float2 x = e[16 * i];
       Mx = fmaxf(Mx, x.x);
       Mn = fminf(Mn, x.y);
+    }
+    if constexpr (MODE == BEHIND) {
+      // and over the shared tokens
+      e = reinterpret_cast<const float2 *>(a.pre.ext) + a.pre.slot(hk, b * total + r);
+      for (int i = kb; i < a.pre.parts; i += 4) {
+        const float2 x = e[16 * i];
+        Mx = fmaxf(Mx, x.x);
+        Mn = fminf(Mn, x.y);
+      }
     }
     Mx = fmaxf(Mx, __shfl_xor(Mx, 16));
     Mx = fmaxf(Mx, __shfl_xor(Mx, 32));
@@ -277,34 +282,26 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
     Mx *= a.scale, Mn *= a.scale;
     rc = row_const(Mx, Mn, a.K, CALIB, a.tau, a.scale);
   }
-  const float Kf = (float)a.K, edge = 2.f * Kf - 1.f, span = 1.f - rc.emh;
   const float c2 = a.scale * 1.44269504f;
 
   f32x4 o[VALUES ? NT : 1] = {};
   float m = -INFINITY, l = 0.f, low = INFINITY;  // (extrema: m and low)
   Stage4<D, VALUES> cur, nxt;
   int c = c0 + wave;
-  if (c < c1) load(chunks.at(c), cur);
+  if (c < c1) load(c, cur);
   for (; c < c1; c += NWAVE) {
-    const int j = chunks.at(c);
-    if (c + NWAVE < c1) load(chunks.at(c + NWAVE), nxt);
+    if (c + NWAVE < c1) load(c + NWAVE, nxt);
     // every row of the tile sees every key of the chunk
-    const bool all = j + CHUNK - 1 <= lo && cur.ok == (1 << TILES) - 1 &&
-                     ((int64_t)hi - j < a.window || j + CHUNK - 1 < a.sinks);
+    const int j = cur.at[0], end = (MODE == LISTED ? max(cur.at[0], cur.at[1]) + 16 : j + CHUNK) - 1;
+    const bool all = end <= lo && cur.ok == (1 << TILES) - 1 &&
+                     (MODE == LISTED || (int64_t)hi - j < a.window || end < a.sinks);
+    // tile i's key 4 kb + e
+    auto key_at = [&](int i, int e) { return (MODE == LISTED ? cur.at[i] : j + 16 * i) + 4 * kb + e; };
     auto sees = [&](int key, int i) {
       return key <= pos && ((int64_t)pos - key < a.window || key < a.sinks) && (cur.ok >> i & 1);
     };
     // groups that hold an infinity or NaN
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < TILES; ++i) {
-      bad |= cur.ks[i] == 255;
-      if constexpr (VALUES) {
-        const uint32_t y = ~cur.vs[i];
-        bad |= ((y - 0x01010101u) & ~y & 0x80808080u) != 0;
-      }
-    }
-    bad = __any(bad);
+    const bool bad = __any(holds_nan<D, VALUES>(cur));
     float Q[TILES][4];
 #pragma unroll
     for (int i = 0; i < TILES; ++i) {
@@ -332,7 +329,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
         for (int e = 0; e < 4; ++e) Q[i][e] = y >> (4 * kb + e) & 1 ? NAN : Q[i][e];
       }
     }
-    // the scores of the keys that the lane weighs: key j + 16 i + 4 kb + own + e
+    // the scores of the keys that the lane weighs: tile i's 4 kb + own + e
     float S[TILES][NE];
 #pragma unroll
     for (int i = 0; i < TILES; ++i) {
@@ -342,7 +339,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) S[i][e] = Q[i][e];
     }
-    auto counts = [&](int i, int e) { return sees(j + 16 * i + 4 * kb + own + e, i); };
+    auto counts = [&](int i, int e) { return sees(key_at(i, own + e), i); };
     if (!all) {
 #pragma unroll
       for (int i = 0; i < TILES; ++i)
@@ -383,40 +380,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
 #pragma unroll
           for (int e = 0; e < NE; ++e) w[i][e] = __builtin_amdgcn_exp2f((S[i][e] - mm) * c2);
       } else {
-        bool any = false;
-#pragma unroll
-        for (int i = 0; i < TILES; ++i)
-#pragma unroll
-          for (int e = 0; e < NE; ++e) {
-            w[i][e] = fmaf(S[i][e], rc.alpha, rc.beta);
-            any |= is_ambiguous<CALIB>(w[i][e], rc.margin2, edge);
-          }
-        if (__any(any)) {
-          // keys within rounding of a boundary: decided in 64 bits
-#pragma unroll
-          for (int i = 0; i < TILES; ++i)
-#pragma unroll
-            for (int e = 0; e < NE; ++e) {
-              const bool amb = is_ambiguous<CALIB>(w[i][e], rc.margin2, edge);
-              if (!__any(amb)) continue;
-              const float x = 0.5f * exact_v2<CALIB>(S[i][e] * a.scale, 2.f * w[i][e], Mx, Mn, a.K, a.tau);
-              w[i][e] = amb ? x : w[i][e];
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < TILES; ++i)
-#pragma unroll
-          for (int e = 0; e < NE; ++e) {
-            const KeyDec k = key_of<CALIB>(w[i][e], Kf);
-            const float up = grid_upper(k.rf, rc);
-            float x;
-            if constexpr (RECON == REC_NEAREST) x = k.up ? up : up * rc.emh;
-            else x = up * fmaf(k.t, span, rc.emh);
-            x = k.tail ? 0.f : x;
-            // an infinite or NaN score makes its row NaN
-            x = fabsf(S[i][e]) < INFINITY ? x : NAN;
-            w[i][e] = x;
-          }
+        grid_weights<CALIB, RECON, NE>(S, w, rc, Mx, Mn, a);
         if (!all) {
 #pragma unroll
           for (int i = 0; i < TILES; ++i)
@@ -431,7 +395,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
         for (int i = 0; i < TILES; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (j + 16 * i + 4 * kb + e > hi || !(cur.ok >> i & 1)) cur.clear(i, e);
+            if (key_at(i, e) > hi || !(cur.ok >> i & 1)) cur.clear(i, e);
       }
       if (__builtin_expect(bad, 0)) {
         // groups of NaN: their values as zeros here, and NaN for the rows that see them
@@ -443,7 +407,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
             const bool nan = (cur.vs[i] >> (8 * e) & 255) == 255;
             if (nan) cur.clear(i, e);
             is[i / 2][i % 2 * 4 + e] = (__bf16)(nan ? 1.f : 0.f);
-            one[i / 2][i % 2 * 4 + e] = (__bf16)(sees(j + 16 * i + 4 * kb + e, i) ? 1.f : 0.f);
+            one[i / 2][i % 2 * 4 + e] = (__bf16)(sees(key_at(i, e), i) ? 1.f : 0.f);
           }
         // (column `slot` of the values here is row 4 kb + e of the sums)
         f32x4 k = {};
@@ -475,19 +439,8 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
         for (int e = 0; e < 8; ++e) f[e] = scale_of(cur.vs[2 * u + e / 4] >> (8 * (e % 4)) & 255);
 #pragma unroll
         for (int y = 0; y < NT / 2; ++y) {
-          uint32_t z[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int i = 2 * u + e / 4, k = e % 4;
-            z[e] = pair_at(D == 128 ? y : D == 64 ? 2 * (k % 2) + y : k,
-                           cur.v[i][D == 128 ? k : D == 64 ? k / 2 : 0], f[e]);
-          }
           u32x4 even, odd;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            even[e] = __builtin_amdgcn_perm(z[2 * e + 1], z[2 * e], 0x05040100u);
-            odd[e] = __builtin_amdgcn_perm(z[2 * e + 1], z[2 * e], 0x07060302u);
-          }
+          value_ops<D>(cur, f, u, y, even, odd);
 #pragma unroll
           for (int i = NP - 1; i >= 0; --i) {
             o[2 * y] = mma16(as_op(even), p[i], o[2 * y]);
@@ -544,11 +497,11 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
       for (int e = 0; e < NT; ++e)
         x[e] = fmaf(rows[(i * 16 + row) * (D + 4) + part * NT + e], f, x[e]);
     }
-    if (share.parts == 1) {
+    if (MODE != BEHIND && work.parts == 1) {
       const int rr = tile * 16 + row;
       if (rr < total) {
         const float f = sum == 0.f ? 0.f : 1.f / sum;
-        TI *y = slice_of<TI>(a.o, b, hk * G + rr % G) + rr / G * a.o.st + part * NT;
+        TI *y = slice_of<TI>(a.o, b, hk * G + rr % G) + (work.t0 + rr / G) * a.o.st + part * NT;
 #pragma unroll
         for (int e = 0; e < NT; ++e) {
           if constexpr (sizeof(TI) == 4) y[e] = x[e] * f;
@@ -571,16 +524,30 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
 // groups whose sums are added in order of the groups.
 template <typename TI, int D> __global__ __launch_bounds__(256) void join_kernel(CachedArgs a) {
   constexpr int W = D / 4, NG = 256 / W;
-  __shared__ float f[256], red[8];  // (a.shares < 256)
+  __shared__ float f[256], red[8];  // (at most 256 parts)
   __shared__ f32x4 sums[NG][W];
   const int kvs = a.B * a.Hkv, s = blockIdx.x % kvs, b = s / a.Hkv, hk = s % a.Hkv;
-  const int G = a.H / a.Hkv, r = blockIdx.x / kvs, tid = threadIdx.x, wave = tid >> 6;
-  const Share share(a, r / 16, b, true);
-  if (share.parts == 1) return;  // (written by its only part)
-  const int64_t first = slot_of(a, hk, r / 16, share.first) + r % 16;
+  const int G = a.H / a.Hkv, r = blockIdx.x / kvs, tid = threadIdx.x, wave = tid >> 6;  // r: token and head
+  int64_t first, before = 0;
+  int parts, shared = 0;  // parts over the shared tokens, then the row's own
+  if constexpr (MODE == SEQUENCE) {
+    const Share share(a, r / 16, b, true);
+    if (share.parts == 1) return;  // (written by its only part)
+    first = slot_of(a, hk, r / 16, share.first) + r % 16;
+    parts = share.parts;
+  } else if constexpr (MODE == LISTED) {
+    first = slot_of(a, hk, r % G / 16, (b * a.T + r / G) * a.parts) + r % G % 16;
+    parts = a.parts;
+  } else {
+    first = slot_of(a, hk, r / 16, b * a.parts) + r % 16;
+    before = a.pre.slot(hk, b * a.T * G + r);
+    shared = a.pre.parts;
+    parts = a.parts + shared;
+  }
   float m = -INFINITY, l = 0.f;
-  if (tid < share.parts) {
-    const float2 st = reinterpret_cast<const float2 *>(a.stat)[first + 16 * tid];
+  if (tid < parts) {
+    const float2 st = tid < shared ? reinterpret_cast<const float2 *>(a.pre.stat)[before + 16 * tid]
+                                   : reinterpret_cast<const float2 *>(a.stat)[first + 16 * (tid - shared)];
     l = st.y;
     if (l != 0.f) m = st.x;  // (a part that saw a key)
   }
@@ -600,9 +567,16 @@ template <typename TI, int D> __global__ __launch_bounds__(256) void join_kernel
   const int at = tid % W, grp = tid / W;
   const f32x4 *p = reinterpret_cast<const f32x4 *>(a.part + first * D) + at;
   f32x4 x = {};
+  if constexpr (MODE == BEHIND) {
+    const f32x4 *y = reinterpret_cast<const f32x4 *>(a.pre.part + before * D) + at;
 #pragma unroll 4
-  for (int i = grp; i < share.parts; i += NG)
-    x += p[(int64_t)i * 16 * W] * f[i];  // (a NaN stays one, however small its part's weight)
+    for (int i = grp; i < parts; i += NG)
+      x += (i < shared ? y[(int64_t)i * 16 * W] : p[(int64_t)(i - shared) * 16 * W]) * f[i];
+  } else {
+#pragma unroll 4
+    for (int i = grp; i < parts; i += NG)
+      x += p[(int64_t)i * 16 * W] * f[i];  // (a NaN stays one, however small its part's weight)
+  }
   sums[grp][at] = x;
   __syncthreads();
   if (grp) return;
@@ -615,53 +589,76 @@ template <typename TI, int D> __global__ __launch_bounds__(256) void join_kernel
   else *reinterpret_cast<u32x2 *>(y) = u32x2{cvt_bf16x2(x[0], x[1]), cvt_bf16x2(x[2], x[3])};
 }
 
+enum { EXTREMA = 1, WEIGHTS = 2, JOIN = 4 };  // which passes to launch
+
 template <typename TI, int D, bool FEW, int CALIB>
-void grid_passes(const CachedArgs &a, dim3 g, hipStream_t s) {
+void grid_passes(const CachedArgs &a, dim3 g, int what, hipStream_t s) {
   const dim3 t(64 * NWAVE);
-  timed_call("kia_cache4_extrema", s, [&] {
-    hipLaunchKernelGGL((cached_kernel<TI, D, PASS_EXTREMA, CALIB, REC_LERP, FEW && CALIB != CAL_FWM>),
-                       g, t, 0, s, a);
-  });
-  timed_call("kia_cache4_attn", s, [&] {
-    if (a.recon == REC_LERP)
-      hipLaunchKernelGGL((cached_kernel<TI, D, PASS_GRID, CALIB, REC_LERP, FEW>), g, t, 0, s, a);
-    else
-      hipLaunchKernelGGL((cached_kernel<TI, D, PASS_GRID, CALIB, REC_NEAREST, FEW>), g, t, 0, s, a);
-  });
-}
-
-template <typename TI, int D, int CALIB> void grid_rows(const CachedArgs &a, dim3 g, hipStream_t s) {
-  if (a.T * (a.H / a.Hkv) <= 4) grid_passes<TI, D, true, CALIB>(a, g, s);
-  else grid_passes<TI, D, false, CALIB>(a, g, s);
-}
-
-template <typename TI, int D> void run(const CachedArgs &a, hipStream_t s) {
-  const dim3 g((unsigned)(a.shares + a.B) * a.Hkv * a.tiles);
-  if (a.recon == REC_SOFTMAX) {
-    timed_call("kia_cache4_attn", s, [&] {
-      hipLaunchKernelGGL((cached_kernel<TI, D, PASS_SOFTMAX, CAL_FWM, REC_SOFTMAX, false>), g,
-                         dim3(64 * NWAVE), 0, s, a);
+  if (what & EXTREMA)
+    timed_call("kia_cache4_extrema", s, [&] {
+      hipLaunchKernelGGL((cached_kernel<TI, D, PASS_EXTREMA, CALIB, REC_LERP, FEW && CALIB != CAL_FWM>),
+                         g, t, 0, s, a);
     });
+  if (what & WEIGHTS)
+    timed_call("kia_cache4_attn", s, [&] {
+      if (a.recon == REC_LERP)
+        hipLaunchKernelGGL((cached_kernel<TI, D, PASS_GRID, CALIB, REC_LERP, FEW>), g, t, 0, s, a);
+      else
+        hipLaunchKernelGGL((cached_kernel<TI, D, PASS_GRID, CALIB, REC_NEAREST, FEW>), g, t, 0, s, a);
+    });
+}
+
+template <typename TI, int D, int CALIB> void grid_rows(const CachedArgs &a, dim3 g, int what, hipStream_t s) {
+  if ((MODE == LISTED ? 1 : a.T) * (a.H / a.Hkv) <= 4) grid_passes<TI, D, true, CALIB>(a, g, what, s);
+  else grid_passes<TI, D, false, CALIB>(a, g, what, s);
+}
+
+template <typename TI, int D> void run(const CachedArgs &a, int what, hipStream_t s) {
+  const dim3 g((unsigned)(MODE == SEQUENCE ? a.shares + a.B : a.shares) * a.Hkv * a.tiles);
+  if (a.recon == REC_SOFTMAX) {
+    if (what & WEIGHTS)
+      timed_call("kia_cache4_attn", s, [&] {
+        hipLaunchKernelGGL((cached_kernel<TI, D, PASS_SOFTMAX, CAL_FWM, REC_SOFTMAX, false>), g,
+                           dim3(64 * NWAVE), 0, s, a);
+      });
   } else if (a.calib == CAL_MINMAX) {
-    grid_rows<TI, D, CAL_MINMAX>(a, g, s);
+    grid_rows<TI, D, CAL_MINMAX>(a, g, what, s);
   } else if (a.calib == CAL_FWM) {
-    grid_rows<TI, D, CAL_FWM>(a, g, s);
+    grid_rows<TI, D, CAL_FWM>(a, g, what, s);
   } else {
-    grid_rows<TI, D, CAL_RESOLVED>(a, g, s);
+    grid_rows<TI, D, CAL_RESOLVED>(a, g, what, s);
   }
-  if (a.shares > 1) {
+  if (what & JOIN) {
     timed_call("kia_cache4_join", s, [&] {
       hipLaunchKernelGGL((join_kernel<TI, D>), dim3((unsigned)(a.B * a.Hkv) * (a.T * (a.H / a.Hkv))), dim3(256), 0,
                          s, a);
     });
   }
 }
+template <int D> void run(const CachedArgs &a, int dtype, int what, hipStream_t s) {
+  if (dtype == KIA_F32) run<float, D>(a, what, s);
+  else run<uint16_t, D>(a, what, s);
+}
 
 }  // namespace
 
+#if KIA_MODE == 0
 template <> void launch_cached<KIA_HEAD>(const CachedArgs &a, int dtype, hipStream_t s) {
-  if (dtype == KIA_F32) run<float, KIA_HEAD>(a, s);
-  else run<uint16_t, KIA_HEAD>(a, s);
+  run<KIA_HEAD>(a, dtype, EXTREMA | WEIGHTS | (a.shares > 1 ? JOIN : 0), s);
 }
+#elif KIA_MODE == 1
+template <> void launch_listed<KIA_HEAD>(const CachedArgs &a, int dtype, hipStream_t s) {
+  run<KIA_HEAD>(a, dtype, EXTREMA | WEIGHTS | (a.parts > 1 ? JOIN : 0), s);
+}
+#else
+template <> void launch_shared<KIA_HEAD>(const CachedArgs &a, int dtype, hipStream_t s) {
+  if (a.recon != REC_SOFTMAX) {
+    launch_prefix<KIA_HEAD>(a, dtype, true, s);
+    run<KIA_HEAD>(a, dtype, EXTREMA, s);
+  }
+  launch_prefix<KIA_HEAD>(a, dtype, false, s);
+  run<KIA_HEAD>(a, dtype, WEIGHTS | JOIN, s);
+}
+#endif
 
 }  // namespace kia

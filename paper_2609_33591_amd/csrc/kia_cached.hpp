@@ -1,0 +1,167 @@
+// kia_cached.hpp -- what the kernels that attend over the 4-bit cache share: a lane's share
+// of 32 keys and values, their bf16 operands, and the interval weights of its scores.
+#pragma once
+
+#include <limits.h>
+
+#include "kia_cache.hpp"
+
+namespace kia {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// 32 keys at a time: two tiles of 16 and the next two on their way leave room for three
+// workgroups a CU in bf16 (162 registers; with 64 keys 217, two workgroups, and the
+// interval weights of 32 x 16 500 keys took 101 us against 88).
+constexpr int TILES = 2, CHUNK = 16 * TILES, NWAVE = 4;
+enum { PASS_SOFTMAX, PASS_EXTREMA, PASS_GRID };
+
+__device__ __forceinline__ f32x4 mma16(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// byte `s` of a word of codes as two bf16
+template <int S> __device__ __forceinline__ uint32_t pair(uint32_t w, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, S));
+}
+__device__ __forceinline__ uint32_t pair_at(int s, uint32_t w, float scale) {
+  return s == 0 ? pair<0>(w, scale) : s == 1 ? pair<1>(w, scale) : s == 2 ? pair<2>(w, scale)
+                                                                     : pair<3>(w, scale);
+}
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// One lane's share of a chunk: codes and scales of its keys and values.
+template <int D, bool VALUES> struct Stage4 {
+  static constexpr int N = D / 32;  // words of codes of a 16-key tile
+  uint32_t k[TILES][N], v[VALUES ? TILES : 1][N], vs[VALUES ? TILES : 1];
+  uint8_t ks[TILES];
+  int at[TILES];  // the tiles' first keys
+  int ok;         // bit t: the tile's page is one of the cache's
+  // the values of token e (of the lane's four) of tile i as zeros
+  __device__ __forceinline__ void clear(int i, int e) {
+    vs[i] &= ~(0xffu << (8 * e));
+    if constexpr (D == 128) v[i][e] = 0;
+    else if constexpr (D == 64) v[i][e / 2] &= ~(0xffffu << (16 * (e % 2)));
+    else v[i][0] &= ~(0xffu << (8 * e));
+  }
+};
+template <int N> __device__ __forceinline__ void load_words(const uint8_t *p, uint32_t (&w)[N]) {
+  if constexpr (N == 4) {
+    const u32x4 x = *reinterpret_cast<const u32x4 *>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = x[i];
+  } else if constexpr (N == 2) {
+    const u32x2 x = *reinterpret_cast<const u32x2 *>(p);
+    w[0] = x[0], w[1] = x[1];
+  } else {
+    w[0] = *reinterpret_cast<const uint32_t *>(p);
+  }
+}
+
+// Eight channels of a query as operands: channel block c of its NP pieces.
+template <typename TI, int NP, int N>
+__device__ __forceinline__ void load_query(const TI *p, bf16x8 (&q)[NP][N], int c) {
+  if constexpr (NP == 1) {
+    q[0][c] = as_op(*reinterpret_cast<const u32x4 *>(p));
+  } else {
+    float x[8];
+    load8(p, x);
+    bf16x8 y[3];
+    to_pieces<3>(x, y);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) q[i][c] = y[i];
+  }
+}
+
+// A lane's share of tile i, tokens tok .. tok + 15 of a page (codes: bytes of a block's
+// codes, block: of all of it).
+template <int D, bool VALUES>
+__device__ __forceinline__ void load_tile(const CachedArgs &a, int page, int hk, int tok, int codes, int64_t block,
+                                          int lane, int i, Stage4<D, VALUES> &x) {
+  constexpr int N = D / 32;
+  const int kb = lane >> 4, slot = lane & 15;
+  const uint8_t *kp = a.cache + cache_block<D>(page, 0, hk, a.Hkv, a.lpage);
+  load_words<N>(kp + (tok + slot) * (D / 2) + kb * (D / 8), x.k[i]);
+  x.ks[i] = kp[codes + (tok + slot) * (D / 32) + kb * (D / 4) / 32];
+  if constexpr (VALUES) {
+    const uint8_t *vp = kp + a.Hkv * block;
+    load_words<N>(vp + tok * (D / 2) + lane * (D / 8), x.v[i]);
+    x.vs[i] = *reinterpret_cast<const uint32_t *>(vp + codes + tok * (D / 32) + kb * (D / 8) +
+                                                  slot * (D / 16) / 32 * 4);
+  }
+}
+
+// Whether a lane's share has a group that holds an infinity or NaN.
+template <int D, bool VALUES> __device__ __forceinline__ bool holds_nan(const Stage4<D, VALUES> &x) {
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) {
+    bad |= x.ks[i] == 255;
+    if constexpr (VALUES) {
+      const uint32_t y = ~x.vs[i];
+      bad |= ((y - 0x01010101u) & ~y & 0x80808080u) != 0;
+    }
+  }
+  return bad;
+}
+
+// Operands of the values of 32 keys (tiles 2 u and 2 u + 1, f: their scales) in two of the
+// lane's channels.
+template <int D>
+__device__ __forceinline__ void value_ops(const Stage4<D, true> &x, const float (&f)[8], int u, int y, u32x4 &even,
+                                          u32x4 &odd) {
+  uint32_t z[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int i = 2 * u + e / 4, k = e % 4;
+    z[e] = pair_at(D == 128 ? y : D == 64 ? 2 * (k % 2) + y : k, x.v[i][D == 128 ? k : D == 64 ? k / 2 : 0], f[e]);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    even[e] = __builtin_amdgcn_perm(z[2 * e + 1], z[2 * e], 0x05040100u);
+    odd[e] = __builtin_amdgcn_perm(z[2 * e + 1], z[2 * e], 0x07060302u);
+  }
+}
+
+// The weights w of scores S on the row's grid.
+template <int CALIB, int RECON, int NE>
+__device__ __forceinline__ void grid_weights(const float (&S)[TILES][NE], float (&w)[TILES][NE],
+                                             const RowConst &rc, float Mx, float Mn, const CachedArgs &a) {
+  const float Kf = (float)a.K, edge = 2.f * Kf - 1.f, span = 1.f - rc.emh;
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < TILES; ++i)
+#pragma unroll
+    for (int e = 0; e < NE; ++e) {
+      w[i][e] = fmaf(S[i][e], rc.alpha, rc.beta);
+      any |= is_ambiguous<CALIB>(w[i][e], rc.margin2, edge);
+    }
+  if (__any(any)) {
+    // keys within rounding of a boundary: decided in 64 bits
+#pragma unroll
+    for (int i = 0; i < TILES; ++i)
+#pragma unroll
+      for (int e = 0; e < NE; ++e) {
+        const bool amb = is_ambiguous<CALIB>(w[i][e], rc.margin2, edge);
+        if (!__any(amb)) continue;
+        const float x = 0.5f * exact_v2<CALIB>(S[i][e] * a.scale, 2.f * w[i][e], Mx, Mn, a.K, a.tau);
+        w[i][e] = amb ? x : w[i][e];
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < TILES; ++i)
+#pragma unroll
+    for (int e = 0; e < NE; ++e) {
+      const KeyDec k = key_of<CALIB>(w[i][e], Kf);
+      const float up = grid_upper(k.rf, rc);
+      float x;
+      if constexpr (RECON == REC_NEAREST) x = k.up ? up : up * rc.emh;
+      else x = up * fmaf(k.t, span, rc.emh);
+      x = k.tail ? 0.f : x;
+      // an infinite or NaN score makes its row NaN
+      x = fabsf(S[i][e]) < INFINITY ? x : NAN;
+      w[i][e] = x;
+    }
+}
+
+}  // namespace kia

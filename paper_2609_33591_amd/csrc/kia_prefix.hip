@@ -1,0 +1,349 @@
+// kia_prefix.hip -- attention over the tokens that all sequences of a batch share, for one
+// head dimension (KIA_HEAD): the part of each row's sums that kia_cached.hip's passes over
+// what lies behind them complete.
+//
+// The rows (sequence, token, head of the group) of a key head meet the same keys, so they
+// are one product: 16 rows a tile as in kia_cached.hip, with its operands and orders, and RT
+// tiles a wave, which takes the codes of 32 keys apart once for all of them. That work, some
+// 100 vector operations, and a tile's weights, about as many, bound the kernel before
+// the matrix unit does; the keys come out of the L2 after the first tile. Key heads go round
+// the workgroups, so that an XCD's share of them are few and fit.
+#include "kia_cached.hpp"
+#include "kia_host.hpp"
+
+namespace kia {
+namespace {
+
+// The last key of the shared tokens that a row at `pos` sees.
+__device__ __forceinline__ int last_of(const CachedArgs &a, int pos) { return min(pos, a.shared - 1); }
+
+template <typename TI, int D, int PASS, int CALIB, int RECON, int RT>
+__global__ __launch_bounds__(64 * NWAVE, 2) void prefix_kernel(CachedArgs a) {
+  constexpr int NP = Pieces<TI>::N, N = D / 32, NT = D / 16;
+  constexpr bool VALUES = PASS != PASS_EXTREMA;
+  __shared__ float red[RT][NWAVE][16][2];
+  __shared__ __attribute__((aligned(16))) float rows[VALUES ? NWAVE * 16 * (D + 4) : 4];
+  const int tid = threadIdx.x, lane = tid & 63, kb = lane >> 4, slot = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hk = blockIdx.x % a.Hkv, groups = (a.pre.tiles + RT - 1) / RT;
+  const int tile0 = (int)(blockIdx.x / a.Hkv) % groups * RT, part = blockIdx.x / a.Hkv / groups;
+  const int G = a.H / a.Hkv, per = a.T * G;  // rows of a sequence
+  const int64_t total = (int64_t)a.B * per;
+
+  // this lane's row of each tile, and the last key that it sees (below 0: none)
+  int last[RT], lo = INT_MAX, hi = -1;
+  bf16x8 q[RT][NP][N];
+#pragma unroll
+  for (int x = 0; x < RT; ++x) {
+    const int64_t row = min((int64_t)(tile0 + x) * 16 + slot, total - 1);
+    const int b = (int)(row / per), r = (int)(row % per), t = r / G;
+    const int n = (int)min((int64_t)max(a.lengths[b], 0), (int64_t)a.width << a.lpage);
+    last[x] = last_of(a, n - a.T + t);
+    lo = min(lo, last[x]), hi = max(hi, last[x]);
+    const TI *p = slice_of<TI>(a.q, b, hk * G + r % G) + t * a.q.st + kb * (D / 4);
+#pragma unroll
+    for (int c = 0; c < N; ++c) load_query<TI>(p + 8 * c, q[x], c);
+  }
+#pragma unroll
+  for (int i = 1; i < 16; i *= 2) {
+    lo = min(lo, __shfl_xor(lo, i));
+    hi = max(hi, __shfl_xor(hi, i));
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo), hi = __builtin_amdgcn_readfirstlane(hi);
+  const int chunks = a.shared / CHUNK, seen = hi < 0 ? 0 : hi / CHUNK + 1;
+  const int c0 = (int)((int64_t)chunks * part / a.pre.parts);
+  const int c1 = min(seen, (int)((int64_t)chunks * (part + 1) / a.pre.parts));
+
+  const int codes = D / 2 << a.lpage;
+  const int64_t block = (int64_t)codes + (D / 32 << a.lpage);
+  auto load = [&](int c, Stage4<D, VALUES> &x) {
+    x.ok = 0;
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+      const int key = c * CHUNK + 16 * i;
+      const int page = __builtin_amdgcn_readfirstlane(a.table[key >> a.lpage]);
+      const bool ok = page >= 0 && page < a.pages;
+      x.at[i] = key;
+      x.ok |= ok << i;
+      load_tile<D, VALUES>(a, ok ? page : 0, hk, key & ((1 << a.lpage) - 1), codes, block, lane, i, x);
+    }
+  };
+
+  RowConst rc[RT] = {};
+  float Mx[RT], Mn[RT];
+  if constexpr (PASS == PASS_GRID) {
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+      const int64_t row = min((int64_t)(tile0 + x) * 16 + slot, total - 1);
+      const int b = (int)(row / per), r = (int)(row % per);
+      Mx[x] = -INFINITY, Mn[x] = INFINITY;
+      auto among = [&](const float *ext, int64_t first, int parts) {
+        const float2 *e = reinterpret_cast<const float2 *>(ext) + first;
+        for (int i = kb; i < parts; i += 4) {
+          const float2 y = e[16 * i];
+          Mx[x] = fmaxf(Mx[x], y.x);
+          Mn[x] = fminf(Mn[x], y.y);
+        }
+      };
+      among(a.pre.ext, a.pre.slot(hk, row), a.pre.parts);
+      among(a.ext, (((int64_t)hk * a.tiles + r / 16) * a.shares + (int64_t)b * a.parts) * 16 + r % 16, a.parts);
+      Mx[x] = fmaxf(Mx[x], __shfl_xor(Mx[x], 16));
+      Mx[x] = fmaxf(Mx[x], __shfl_xor(Mx[x], 32));
+      Mn[x] = fminf(Mn[x], __shfl_xor(Mn[x], 16));
+      Mn[x] = fminf(Mn[x], __shfl_xor(Mn[x], 32));
+      Mx[x] *= a.scale, Mn[x] *= a.scale;
+      rc[x] = row_const(Mx[x], Mn[x], a.K, CALIB, a.tau, a.scale);
+    }
+  }
+  const float c2 = a.scale * 1.44269504f;
+
+  f32x4 o[RT][VALUES ? NT : 1] = {};
+  float m[RT], l[RT], low[RT];
+#pragma unroll
+  for (int x = 0; x < RT; ++x) m[x] = -INFINITY, l[x] = 0.f, low[x] = INFINITY;
+  Stage4<D, VALUES> cur, nxt;
+  int c = c0 + wave;
+  if (c < c1) load(c, cur);
+  for (; c < c1; c += NWAVE) {
+    if (c + NWAVE < c1) load(c + NWAVE, nxt);
+    const int j = cur.at[0];
+    const bool all = j + CHUNK - 1 <= lo && cur.ok == (1 << TILES) - 1;
+    auto sees = [&](int x, int i, int e) { return j + 16 * i + 4 * kb + e <= last[x] && (cur.ok >> i & 1); };
+    const bool bad = __any(holds_nan<D, VALUES>(cur));
+    // scores of all tiles from the keys' operands
+    float S[RT][TILES][4];
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+      const float f = scale_of(cur.ks[i]);
+      u32x4 w[N];
+#pragma unroll
+      for (int y = 0; y < N; ++y)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[y][e] = pair_at(e, cur.k[i][y], f);
+      uint64_t nan = 0;
+      if (__builtin_expect(bad, 0)) {
+        nan = __ballot(cur.ks[i] == 255);
+        nan |= nan >> 32;
+        nan |= nan >> 16;
+      }
+#pragma unroll
+      for (int x = 0; x < RT; ++x) {
+        f32x4 acc = {};
+#pragma unroll
+        for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+          for (int y = 0; y < N; ++y) acc = mma16(as_op(w[y]), q[x][p][y], acc);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          S[x][i][e] = nan >> (4 * kb + e) & 1 ? NAN : acc[e];
+          if (!all) S[x][i][e] = sees(x, i, e) ? S[x][i][e] : -INFINITY;
+        }
+      }
+    }
+    if constexpr (PASS == PASS_EXTREMA) {
+#pragma unroll
+      for (int x = 0; x < RT; ++x)
+#pragma unroll
+        for (int i = 0; i < TILES; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            m[x] = fmaxf(m[x], S[x][i][e]);
+            if constexpr (CALIB != CAL_FWM) low[x] = all || sees(x, i, e) ? fminf(low[x], S[x][i][e]) : low[x];
+          }
+    } else {
+      // weights, as operands of the product with the values
+      bf16x8 p[RT][NP];
+#pragma unroll
+      for (int x = 0; x < RT; ++x) {
+        float w[TILES][4];
+        if constexpr (PASS == PASS_SOFTMAX) {
+          float top = S[x][0][0];
+#pragma unroll
+          for (int i = 0; i < TILES; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = fmaxf(top, S[x][i][e]);
+          top = fmaxf(top, __shfl_xor(top, 16));
+          top = fmaxf(top, __shfl_xor(top, 32));
+          // (moved, and the sums scaled, only when passed by 2^8)
+          const bool up = (top - m[x]) * c2 > 8.f;
+          if (__any(up)) {
+            const float f = up ? __builtin_amdgcn_exp2f((m[x] - top) * c2) : 1.f;
+            m[x] = up ? top : m[x];
+            l[x] *= f;
+#pragma unroll
+            for (int y = 0; y < NT; ++y) o[x][y] *= f;
+          }
+          const float mm = m[x] == -INFINITY ? 0.f : m[x];
+#pragma unroll
+          for (int i = 0; i < TILES; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[i][e] = __builtin_amdgcn_exp2f((S[x][i][e] - mm) * c2);
+        } else {
+          grid_weights<CALIB, RECON, 4>(S[x], w, rc[x], Mx[x], Mn[x], a);
+          if (!all) {
+#pragma unroll
+            for (int i = 0; i < TILES; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) w[i][e] = sees(x, i, e) ? w[i][e] : 0.f;
+          }
+        }
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
+          l[x] += (w[i][0] + w[i][1]) + (w[i][2] + w[i][3]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[4 * i + e] = w[i][e];
+        }
+        to_pieces<NP>(y, p[x]);
+      }
+      if (!all) {
+        // values of tokens that no row sees (on no page, behind the last row) as zeros
+#pragma unroll
+        for (int i = 0; i < TILES; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (j + 16 * i + 4 * kb + e > hi || !(cur.ok >> i & 1)) cur.clear(i, e);
+      }
+      if (__builtin_expect(bad, 0)) {
+        // groups of NaN: their values as zeros here, and NaN for the rows that see them
+        bf16x8 is;
+#pragma unroll
+        for (int i = 0; i < TILES; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const bool nan = (cur.vs[i] >> (8 * e) & 255) == 255;
+            if (nan) cur.clear(i, e);
+            is[4 * i + e] = (__bf16)(nan ? 1.f : 0.f);
+          }
+#pragma unroll
+        for (int x = 0; x < RT; ++x) {
+          bf16x8 one;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) one[e] = (__bf16)(sees(x, e / 4, e % 4) ? 1.f : 0.f);
+          f32x4 k = {};
+          k = mma16(is, one, k);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int y = 0; y < NT; ++y) o[x][y][e] = k[e] > 0.f ? NAN : o[x][y][e];
+        }
+      }
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = scale_of(cur.vs[e / 4] >> (8 * (e % 4)) & 255);
+#pragma unroll
+      for (int y = 0; y < NT / 2; ++y) {
+        u32x4 even, odd;
+        value_ops<D>(cur, f, 0, y, even, odd);
+#pragma unroll
+        for (int x = 0; x < RT; ++x)
+#pragma unroll
+          for (int i = NP - 1; i >= 0; --i) {
+            o[x][2 * y] = mma16(as_op(even), p[x][i], o[x][2 * y]);
+            o[x][2 * y + 1] = mma16(as_op(odd), p[x][i], o[x][2 * y + 1]);
+          }
+      }
+    }
+    cur = nxt;
+  }
+
+  // the waves' parts, joined in their order
+#pragma unroll
+  for (int x = 0; x < RT; ++x) {
+    if constexpr (PASS == PASS_EXTREMA) {
+      m[x] = fmaxf(m[x], __shfl_xor(m[x], 16)), m[x] = fmaxf(m[x], __shfl_xor(m[x], 32));
+      low[x] = fminf(low[x], __shfl_xor(low[x], 16)), low[x] = fminf(low[x], __shfl_xor(low[x], 32));
+      if (kb == 0) red[x][wave][slot][0] = m[x], red[x][wave][slot][1] = low[x];
+    } else {
+      l[x] += __shfl_xor(l[x], 16);
+      l[x] += __shfl_xor(l[x], 32);
+      if (kb == 0) red[x][wave][slot][0] = m[x], red[x][wave][slot][1] = l[x];
+    }
+  }
+  if constexpr (PASS == PASS_EXTREMA) {
+    __syncthreads();
+    if (tid < RT * 16) {
+      const int x = tid / 16;
+      const int64_t row = (int64_t)(tile0 + x) * 16 + slot;
+      if (row < total) {
+        float mx = red[x][0][slot][0], mn = red[x][0][slot][1];
+#pragma unroll
+        for (int i = 1; i < NWAVE; ++i) {
+          mx = fmaxf(mx, red[x][i][slot][0]);
+          mn = fminf(mn, red[x][i][slot][1]);
+        }
+        float *e = a.pre.ext + (a.pre.slot(hk, row) + 16 * (int64_t)part) * 2;
+        e[0] = mx, e[1] = mn;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+      // channel (4 kb + e) NT + y of row `slot`
+      float *mine = rows + (wave * 16 + slot) * (D + 4);
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int y = 0; y < NT; ++y) mine[(4 * kb + e) * NT + y] = o[x][y][e];
+      __syncthreads();
+      const int row16 = tid / 16, at = tid % 16;
+      const int64_t row = (int64_t)(tile0 + x) * 16 + row16;
+      float top = 0.f, sum = 0.f, z[NT] = {};
+      if constexpr (PASS == PASS_SOFTMAX) {
+        top = red[x][0][row16][0];
+#pragma unroll
+        for (int i = 1; i < NWAVE; ++i) top = fmaxf(top, red[x][i][row16][0]);
+        if (top == -INFINITY) top = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < NWAVE; ++i) {
+        const float f = PASS == PASS_SOFTMAX ? __builtin_amdgcn_exp2f((red[x][i][row16][0] - top) * c2) : 1.f;
+        sum = fmaf(red[x][i][row16][1], f, sum);
+#pragma unroll
+        for (int e = 0; e < NT; ++e) z[e] = fmaf(rows[(i * 16 + row16) * (D + 4) + at * NT + e], f, z[e]);
+      }
+      if (row < total) {
+        const int64_t out = a.pre.slot(hk, row) + 16 * (int64_t)part;
+        float *y = a.pre.part + out * D + at * NT;
+#pragma unroll
+        for (int e = 0; e < NT; ++e) y[e] = z[e];
+        if (at == 0) a.pre.stat[out * 2] = top, a.pre.stat[out * 2 + 1] = sum;
+      }
+    }
+  }
+}
+
+template <typename TI, int D, int CALIB, int RT> void grid_launch(const CachedArgs &a, dim3 g, bool extrema, hipStream_t s) {
+  const dim3 t(64 * NWAVE);
+  if (extrema) hipLaunchKernelGGL((prefix_kernel<TI, D, PASS_EXTREMA, CALIB, REC_LERP, RT>), g, t, 0, s, a);
+  else if (a.recon == REC_LERP) hipLaunchKernelGGL((prefix_kernel<TI, D, PASS_GRID, CALIB, REC_LERP, RT>), g, t, 0, s, a);
+  else hipLaunchKernelGGL((prefix_kernel<TI, D, PASS_GRID, CALIB, REC_NEAREST, RT>), g, t, 0, s, a);
+}
+
+template <typename TI, int D, int RT> void launch_rows(const CachedArgs &a, bool extrema, hipStream_t s) {
+  const dim3 g((unsigned)a.Hkv * ((a.pre.tiles + RT - 1) / RT) * a.pre.parts);
+  timed_call(extrema ? "kia_cache4_extrema" : "kia_cache4_attn", s, [&] {
+    if (a.recon == REC_SOFTMAX)
+      hipLaunchKernelGGL((prefix_kernel<TI, D, PASS_SOFTMAX, CAL_FWM, REC_SOFTMAX, RT>), g, dim3(64 * NWAVE), 0, s, a);
+    else if (a.calib == CAL_MINMAX) grid_launch<TI, D, CAL_MINMAX, RT>(a, g, extrema, s);
+    else if (a.calib == CAL_FWM) grid_launch<TI, D, CAL_FWM, RT>(a, g, extrema, s);
+    else grid_launch<TI, D, CAL_RESOLVED, RT>(a, g, extrema, s);
+  });
+}
+
+}  // namespace
+
+template <> void launch_prefix<KIA_HEAD>(const CachedArgs &a, int dtype, bool extrema, hipStream_t s) {
+  constexpr int D = KIA_HEAD;
+  if (prefix_tiles(a.pre.tiles, D, dtype) == 1) {
+    if (dtype == KIA_F32) launch_rows<float, D, 1>(a, extrema, s);
+    else launch_rows<uint16_t, D, 1>(a, extrema, s);
+  } else {
+    // (fp32 heads of 128: two tiles do not fit the registers)
+    if (dtype == KIA_F32) launch_rows<float, D, D == 128 ? 1 : 2>(a, extrema, s);
+    else launch_rows<uint16_t, D, 2>(a, extrema, s);
+  }
+}
+
+}  // namespace kia

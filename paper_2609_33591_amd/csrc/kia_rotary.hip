@@ -42,14 +42,7 @@ __global__ __launch_bounds__(ROT_NT) void rotary_kernel(RotArgs a) {
     float s = 0.f, c = 0.f;
     if (t < a.T) {
       const int p = a.pos ? a.pos[(int64_t)b * a.pos_sb + t] : a.first + t;
-      // quarter turns: q whole ones and a rest of at most a half
-      const double x = (double)p * a.freq[e % n] * 0.63661977236758134308;
-      const double q = rint(x);
-      sincospif(0.5f * (float)(x - q), &s, &c);
-      // (a large q is a multiple of 4 plus these bits whatever its size)
-      const int k = (int)(q - 4.0 * floor(q * 0.25));
-      if (k & 1) { const float y = s; s = c; c = -y; }
-      if (k & 2) { s = -s; c = -c; }
+      turn_of(p, a.freq[e % n], s, c);
     }
     turn[e] = make_float2(c * a.factor, a.back ? -(s * a.factor) : s * a.factor);
   }
