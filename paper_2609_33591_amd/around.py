@@ -227,7 +227,10 @@ def _fast():
     _host.bind(torch, _kia._check, {
         n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in (
             "kia_rotary", "kia_window_fwd", "kia_window_ws_bytes", "kia_window_bwd",
-            "kia_cache4_write", "kia_cache4_read", "kia_cache4_ws_bytes", "kia_cache4_attn")})
+            "kia_cache4_write", "kia_cache4_read", "kia_cache4_ws_bytes", "kia_cache4_attn",
+            "kia_cache4_append", "kia_cache4_select_ws_bytes", "kia_cache4_select",
+            "kia_cache4_pages_ws_bytes", "kia_cache4_attn_pages", "kia_cache4_shared_ws_bytes",
+            "kia_cache4_attn_shared")})
     return _host
 
 
@@ -789,6 +792,10 @@ def cache4_append(q, k, v, cache, table, starts, plan, counts=None, bounds=None)
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
         raise KiaError("appending to a 4-bit cache is forward only: call it under torch.no_grad")
     _eager(q, k, v)
+    made = _fast().cache4_append(q, k, v, cache.data, cache.page, cache.d, table, starts, counts, plan.freq,
+                                 plan.factor, LAYOUT.get(plan.layout, -1), bounds)
+    if made is not None:
+        return made
     like, H = _Like("k", k), _heads(k, q)
     q, vq = like.take("q", q, H)
     k, vk = like.take("k", k)
@@ -860,6 +867,9 @@ def cache4_select(q, cache, bounds, table, lengths, count, first=1, last=1):
     head's queries. For cache4_attention(..., pages=)."""
     import torch
     _eager(q)
+    made = _fast().cache4_select(q, cache.data, cache.page, cache.d, table, lengths, bounds, count, first, last)
+    if made is not None:
+        return made
     like, need = _select_checked(q, cache, table, count, first, last)
     q, vq = like.take("q", q)
     B, H, T, d = like.shape
@@ -930,6 +940,9 @@ def _served(q, cache, table, lengths, op, window, sinks, pages, shared):
         raise KiaError("pages and shared tokens are not taken together")
     if window != 0 or sinks != 0:
         raise KiaError("a window is not taken with pages or shared tokens")
+    made = _fast().cache4_served(q, cache.data, cache.page, cache.d, table, lengths, pages, shared, *op[:4])
+    if made is not None:
+        return made
     if pages is not None:
         name, (like, args, need) = "kia_cache4_attn_pages", _pages_checked(q, cache, table, lengths, pages)
     else:

@@ -56,18 +56,13 @@ __device__ __forceinline__ void turn64(double x, double &s, double &c) {
   if (k & 2) s = -s, c = -c;
 }
 
-// Codes and scale byte of eight channels y of a token from 64 bits (the group's other
-// channels are the next lanes').
-__device__ __forceinline__ void quantise64(const double (&y)[8], uint32_t &w, uint32_t &s) {
-  double top = 0;
-  bool bad = false;
+// The code and scale byte of a channel y from 64 bits: the other 31 of its group are the next
+// lanes' of 32.
+__device__ __forceinline__ void quantise64(double y, uint32_t &w, uint32_t &s) {
+  double top = fabs(y);
+  bool bad = !(top < INFINITY);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    bad |= !(fabs(y[e]) < INFINITY);
-    top = fmax(top, fabs(y[e]));
-  }
-#pragma unroll
-  for (int i = 1; i < 4; i *= 2) {
+  for (int i = 1; i < 32; i *= 2) {
     top = fmax(top, __shfl_xor(top, i));
     bad |= (bool)__shfl_xor((int)bad, i);
   }
@@ -75,22 +70,15 @@ __device__ __forceinline__ void quantise64(const double (&y)[8], uint32_t &w, ui
   const uint64_t bits = (uint64_t)__double_as_longlong(top);
   int e = (int)(bits >> 52) - 1023 - ((bits & 0xfffffffffffffull) <= 0x8000000000000ull ? 2 : 1);
   e = min(max(e, -126), 125);
-  const double f = __longlong_as_double((long long)(1023 - e) << 52);
-  w = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const double a = fabs(y[i]) * f;
-    const uint32_t level = (a > 0.25) + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) +
-                           (a >= 3.5) + (a > 5.0);
-    w |= (level | (signbit(y[i]) ? 8u : 0u)) << (4 * i);
-  }
-  w = bad ? 0u : w;
+  const double a = fabs(y) * __longlong_as_double((long long)(1023 - e) << 52);
+  w = (a > 0.25) + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5) + (a > 5.0);
+  w = bad ? 0u : w | (signbit(y) ? 8u : 0u);
   s = bad ? 255u : (uint32_t)(e + 127);
 }
 
 // The eight channels of a token that a thread has, and their partners in the rotation.
-template <int MODE> struct Chunk {
-  float x[8], y[8];  // y: the partners
+struct Chunk {
+  float x[8], y[8];
 };
 
 // Channel c = 8 oct + e of a rotated part of 2 n: its pair, its partner's channel, and
@@ -112,95 +100,152 @@ template <int MODE> struct Pair {
   }
 };
 
+// Eight channels as they are loaded.
+template <typename TI> struct Raw;
+template <> struct Raw<uint16_t> {
+  u32x4 w = {};
+  __device__ __forceinline__ void load(const uint16_t *p) { w = *reinterpret_cast<const u32x4 *>(p); }
+  __device__ __forceinline__ void values(float (&x)[8]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+  }
+  // the lane's at `from`
+  __device__ __forceinline__ Raw of(int from) const {
+    Raw r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r.w[e] = (uint32_t)__shfl((int)w[e], from);
+    return r;
+  }
+};
+template <> struct Raw<float> {
+  f32x4 w[2] = {};
+  __device__ __forceinline__ void load(const float *p) { w[0] = load4(p), w[1] = load4(p + 4); }
+  __device__ __forceinline__ void values(float (&x)[8]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = w[e / 4][e % 4];
+  }
+  __device__ __forceinline__ Raw of(int from) const {
+    Raw r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r.w[e / 4][e % 4] = __shfl(w[e / 4][e % 4], from);
+    return r;
+  }
+};
+
+// The partners' values: neighbours are the thread's own, a chunk of eight another lane's of
+// the token, all else (row: the token, or nullptr) is read again.
 template <typename TI, int MODE>
-__device__ __forceinline__ void load_pairs(const TI *row, int oct, int n, Chunk<MODE> &k) {
-  load8(row + 8 * oct, k.x);
+__device__ __forceinline__ void pairs_of(const Raw<TI> &own, const TI *row, int oct, int n, Chunk &k) {
+  own.values(k.x);
   if constexpr (MODE == NEIGHBOURS) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) k.y[e] = k.x[e ^ 1];
   } else if constexpr (MODE == HALF8) {
     const Pair<MODE> p(8 * oct, n);
-    load8(row + (p.turns ? p.partner : 8 * oct), k.y);
+    own.of((threadIdx.x & 63) + (p.turns ? (p.partner - 8 * oct) / 8 : 0)).values(k.y);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const Pair<MODE> p(8 * oct + e, n);
-      k.y[e] = load1(row + (p.turns ? p.partner : 8 * oct + e));
+      k.y[e] = p.turns && row ? load1(row + p.partner) : 0.f;
     }
   }
 }
 
-// The rotated chunk; tol: what its values may be off by, at most.
-template <int MODE, bool TOL>
-__device__ __forceinline__ void turned(const Chunk<MODE> &k, const float2 *turn, int oct, int n,
-                                       float factor, float (&z)[8], float (&tol)[8]) {
+// Where a token's table holds a pair's cosine and sine: those of a chunk in pairs of pairs,
+// the chunks' first ones side by side, so that neighbouring lanes read neighbouring 16 bytes
+// (in order, they met in a quarter of the banks: 67 us for the prompts below).
+template <int MODE> struct Table {
+  static constexpr int OF = MODE == HALF8 ? 8 : 4;  // pairs of a chunk
+  int chunks;
+  __host__ __device__ __forceinline__ explicit Table(int n) : chunks((n + OF - 1) / OF) {}
+  __host__ __device__ __forceinline__ int size() const { return chunks * OF; }
+  __device__ __forceinline__ int at(int pair) const { return pair % OF / 2 * 2 * chunks + pair / OF * 2 + pair % 2; }
+};
+
+// The rotated chunk, and the largest magnitude of its pairs: |x| + |y|.
+template <int MODE>
+__device__ __forceinline__ float turned(const Chunk &k, const float2 *turn, int oct, int n, float (&z)[8]) {
+  const Pair<MODE> chunk(8 * oct, n);
+  const Table<MODE> table(n);
+  const float2 *at = turn + 2 * (MODE == HALF8 ? chunk.pair / 8 : oct);
+  float size = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const Pair<MODE> p(8 * oct + e, n);
-    const float2 w = p.turns ? turn[p.pair] : make_float2(1.f, 0.f);
-    const float r = p.first ? fmaf(k.x[e], w.x, -(k.y[e] * w.y)) : fmaf(k.x[e], w.x, k.y[e] * w.y);
+    Pair<MODE> p = MODE == HALF8 ? chunk : Pair<MODE>(8 * oct + e, n);
+    if (MODE == NEIGHBOURS) p.first = e % 2 == 0;
+    const int j = MODE == HALF8 ? e : e / 2;  // of the chunk's pairs
+    const float2 w = !p.turns ? make_float2(1.f, 0.f)
+                     : MODE == HALF ? turn[table.at(p.pair)] : at[j / 2 * 2 * table.chunks + j % 2];
+    const float r = fmaf(k.x[e], w.x, p.first ? -(k.y[e] * w.y) : k.y[e] * w.y);
     z[e] = p.turns ? r : k.x[e];
-    if constexpr (TOL) tol[e] = p.turns ? (fabsf(k.x[e]) + fabsf(k.y[e])) * factor : 0.f;
+    size = fmaxf(size, p.turns ? fabsf(k.x[e]) + fabsf(k.y[e]) : 0.f);
   }
+  return size;
+}
+
+// Codes of eight values over 2^e (the conversion divides by a scale by itself).
+__device__ __forceinline__ uint32_t codes_over(const float (&x)[8], float scale) {
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
 }
 
 // Codes and scale of a rotated key's chunk from 32 bits; whether the exact rotation's
 // could be others.
 template <int MODE>
-__device__ __forceinline__ bool quantise_turned(const Chunk<MODE> &k, const float2 *turn, int oct, int n,
-                                                float factor, uint32_t &w, uint32_t &s) {
-  float z[8], tol[8], hi = 0.f, lo = 0.f;
-  turned<MODE, true>(k, turn, oct, n, fabsf(factor) * 0x1p-20f, z, tol);
+__device__ __forceinline__ bool quantise_turned(const Chunk &k, const float2 *turn, int oct, int n, float factor,
+                                                uint32_t &w, uint32_t &s) {
+  float z[8];
+  // what a turned channel may be off by
+  const float off = turned<MODE>(k, turn, oct, n, z) * fabsf(factor) * 0x1.4p-21f;
+  uint32_t top = 0;  // (as bits: NaN above infinity above every finite value)
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    // (NaN: as large as it gets)
-    const float up = fabsf(z[e]) + tol[e];
-    hi = up > hi || up != up ? up : hi;
-    lo = fmaxf(lo, fabsf(z[e]) - tol[e]);
-  }
-  uint32_t h = __float_as_uint(hi) & 0x7fffffffu;
-#pragma unroll
-  for (int i = 1; i < 4; i *= 2) {
-    h = max(h, (uint32_t)__shfl_xor((int)h, i));
-    lo = fmaxf(lo, __shfl_xor(lo, i));
-  }
-  const int e = scale_exp(h);
-  const float f = __uint_as_float((uint32_t)(127 - e) << 23);
+  for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(z[e]) & 0x7fffffffu);
+  const float far = __uint_as_float(quad_max(__float_as_uint(off)));
+  const float t = __uint_as_float(quad_max(top));
+  const int e = scale_exp(__float_as_uint(t + far));
+  s = (uint32_t)(e + 127);
   float up[8], down[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    up[i] = (z[i] + tol[i]) * f;
-    down[i] = (z[i] - tol[i]) * f;
+    const float o = MODE == HALF8 || Pair<MODE>(8 * oct + i, n).turns ? off : 0.f;
+    up[i] = z[i] + o;
+    down[i] = z[i] - o;
   }
-  w = codes_of(up);
-  s = (uint32_t)(e + 127);
-  return h >= 0x7f800000u || e != scale_exp(__float_as_uint(lo)) || w != codes_of(down);
+  const float scale = __uint_as_float(s << 23);
+  w = codes_over(up, scale);
+  // (far NaN, or top: not below infinity)
+  return !(t + far < INFINITY) || e != scale_exp(__float_as_uint(fmaxf(t - far, 0.f))) || w != codes_over(down, scale);
 }
-// The exact rotation's.
-template <int MODE>
-__device__ __forceinline__ void quantise_turned64(const Chunk<MODE> &k, double pos, int oct, int n,
-                                                  const AppendArgs &a, uint32_t &w, uint32_t &s) {
-  double y[8] = {};
-  const double factor = (double)a.factor;
-  // (channel by channel: rare, and unrolled it would take twice the kernel's registers)
-#pragma unroll 1
-  for (int i = 0; i < 8; ++i) {
-    float x = k.x[0], o = k.y[0];
+// The exact rotation's, of the row's channel c; the codes of eight channels in the first of
+// their lanes.
+template <typename TI, int MODE>
+__device__ __forceinline__ void quantise_turned64(const TI *row, double pos, int c, int n, const AppendArgs &a,
+                                                  uint32_t &w, uint32_t &s) {
+  const Pair<MODE> p(c, n);
+  const double x = (double)load1(row + c), o = (double)load1(row + (p.turns ? p.partner : c));
+  double sn, cs;
+  turn64(pos * a.freq[p.turns ? p.pair : 0], sn, cs);
+  const double b = o * (sn * (double)a.factor), r = fma(x, cs * (double)a.factor, p.first ? -b : b);
+  quantise64(p.turns ? r : x, w, s);
 #pragma unroll
-    for (int j = 1; j < 8; ++j) x = i == j ? k.x[j] : x, o = i == j ? k.y[j] : o;
-    const Pair<MODE> p(8 * oct + i, n);
-    double sn, cs;
-    turn64(pos * a.freq[p.turns ? p.pair : 0], sn, cs);
-    const double b = (double)o * (sn * factor);
-    const double r = fma((double)x, cs * factor, p.first ? -b : b);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = i == j ? (p.turns ? r : (double)x) : y[j];
-  }
-  quantise64(y, w, s);
+  for (int i = 1; i < 8; i *= 2) w |= (uint32_t)__shfl_down((int)w, i) << (4 * i);
 }
 
-__device__ __forceinline__ float least(float a, float b) { return b < a || b != b ? b : a; }
-__device__ __forceinline__ float most(float a, float b) { return b > a || b != b ? b : a; }
+// Two bf16 as integers of their order, and back; NaN is the largest.
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t ordered(uint32_t x) { return x ^ ((x >> 15 & 0x00010001u) * 0x7fffu); }
+__device__ __forceinline__ i16x2 pack2(uint32_t x) { return __builtin_bit_cast(i16x2, x); }
+struct Ends {
+  i16x2 lo = {0x7fff, 0x7fff}, hi = {-0x8000, -0x8000};
+  __device__ __forceinline__ void take(uint32_t l, uint32_t h) {
+    lo = __builtin_elementwise_min(lo, pack2(l));
+    hi = __builtin_elementwise_max(hi, pack2(h));
+  }
+};
 
 // The bounds of the pages of 64 positions from their tokens' values in LDS, of tokens
 // from .. to - 1; page_at(t): where those of token t's page go, or nullptr. `go_on`: the
@@ -208,7 +253,14 @@ __device__ __forceinline__ float most(float a, float b) { return b > a || b != b
 // next write to l.val needs none, the next call does.
 template <int D> struct BoundsLds {
   uint32_t val[SUB][D / 2];
-  float4 part[Threads<D>::N];
+  uint2 part[Threads<D>::N];
+};
+// Of a key stream: the groups of four lanes (token and group of a span) to take in 64 bits, as
+// a list and how many. Stream i of a workgroup counts in i % 3, so that a barrier a stream
+// is enough: the next but one's is cleared behind it.
+template <int D> struct Again {
+  uint16_t list[SUB * D / 32];
+  int count[3];
 };
 template <int D, class F>
 __device__ __forceinline__ void bounds_of(BoundsLds<D> &l, int lpage, int from, int to, bool go_on, F page_at) {
@@ -218,35 +270,34 @@ __device__ __forceinline__ void bounds_of(BoundsLds<D> &l, int lpage, int from, 
   // thread: two channels of a page, and a part of its tokens
   const int p = g % pages, part = g / pages, size = (1 << ltok) / parts;
   const int t0 = max(from, (p << ltok) + part * size), t1 = min(to, (p << ltok) + (part + 1) * size);
-  float4 r = make_float4(INFINITY, INFINITY, -INFINITY, -INFINITY);
-  for (int t = t0; t < t1; ++t) {
-    const uint32_t v = l.val[t][c];
-    const float x = __uint_as_float(v << 16), y = __uint_as_float(v & 0xffff0000u);
-    r = make_float4(least(r.x, x), least(r.y, y), most(r.z, x), most(r.w, y));
-  }
-  l.part[tid] = r;
+  Ends r;
+  for (int t = t0; t < t1; ++t) r.take(l.val[t][c], l.val[t][c]);
+  l.part[tid] = make_uint2(__builtin_bit_cast(uint32_t, r.lo), __builtin_bit_cast(uint32_t, r.hi));
   __syncthreads();
   if (part) return;
   for (int i = 1; i < parts; ++i) {
-    const float4 o = l.part[tid + i * pages * C];
-    r = make_float4(least(r.x, o.x), least(r.y, o.y), most(r.z, o.z), most(r.w, o.w));
+    const uint2 o = l.part[tid + i * pages * C];
+    r.take(o.x, o.y);
   }
   uint32_t *b = max(from, p << ltok) < min(to, (p + 1) << ltok) ? page_at(p << ltok) : nullptr;
   if (!b) return;
   if (go_on) {
-    const uint32_t x = b[c], y = b[C + c];
-    r = make_float4(least(r.x, __uint_as_float(x << 16)), least(r.y, __uint_as_float(x & 0xffff0000u)),
-                    most(r.z, __uint_as_float(y << 16)), most(r.w, __uint_as_float(y & 0xffff0000u)));
+    const uint32_t x = ordered(b[c]), y = ordered(b[C + c]);
+    r.take(x, y);
   }
-  b[c] = cvt_bf16x2(r.x, r.y);
-  b[C + c] = cvt_bf16x2(r.z, r.w);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) r.lo[i] = r.hi[i] > 0x7f80 ? r.hi[i] : r.lo[i];  // (NaN)
+  b[c] = ordered(__builtin_bit_cast(uint32_t, r.lo));
+  b[C + c] = ordered(__builtin_bit_cast(uint32_t, r.hi));
 }
 
+// Eight channels of token t for its page's bounds.
 template <int D> __device__ __forceinline__ void keep(BoundsLds<D> &l, int t, int oct, uint32_t w, uint32_t s) {
-  float x[8];
-  values_of(w, s == 255 ? NAN : __uint_as_float(s << 23), x);
+  const float f = __uint_as_float(s << 23);
+  u32x4 x = {pair<0>(w, f), pair<1>(w, f), pair<2>(w, f), pair<3>(w, f)};
 #pragma unroll
-  for (int e = 0; e < 4; ++e) l.val[t][4 * oct + e] = cvt_bf16x2(x[2 * e], x[2 * e + 1]);
+  for (int e = 0; e < 4; ++e) x[e] = s == 255 ? 0x7fc07fc0u : ordered(x[e]);
+  *reinterpret_cast<u32x4 *>(&l.val[t][4 * oct]) = x;
 }
 
 // The page of position `pos` of sequence b, or -1.
@@ -256,84 +307,194 @@ __device__ __forceinline__ int page_of(const CacheArgs &c, int b, int64_t pos) {
   return page < 0 || page >= c.pages ? -1 : page;
 }
 
+// A workgroup's 64 positions, in the 64-bit and the thread's own terms: `base` the first one;
+// tokens lo .. hi - 1 of them are new, those before `to` held, those from `old` on for the
+// bounds of pages that get tokens. Thread: token t0 + r TOKENS, channels 8 oct on.
+struct Span {
+  int64_t base, first;  // first: of token 0 of the 64, in the call's tokens
+  int lo, hi, to, old;
+};
+
+// One head after the other of a workgroup's share, from h on in steps; each thread's rows of
+// the next head are on their way while one is worked on.
+template <typename TI, int REP> struct Rows {
+  const TI *p[REP];
+  Raw<TI> next[REP];
+  bool in[REP];
+  int64_t step;
+  __device__ __forceinline__ Rows(const View &v, int b, int h, int by, const Span &s, int t0, int tokens, int oct) {
+    step = by * v.sh;
+#pragma unroll
+    for (int r = 0; r < REP; ++r) {
+      const int t = t0 + r * tokens;
+      in[r] = t >= s.lo && t < s.hi;
+      p[r] = slice_of<TI>(v, b, h) + (s.first + (in[r] ? t : s.lo)) * v.st + 8 * oct;
+      if (in[r]) next[r].load(p[r]);
+    }
+  }
+  // row r of this head; with `more` the next head's is asked for
+  __device__ __forceinline__ Raw<TI> take(int r, bool more) {
+    const Raw<TI> x = next[r];
+    p[r] += step;
+    if (in[r] && more) next[r].load(p[r]);
+    return x;
+  }
+};
+
 template <typename TI, int D, int MODE>
-__global__ __launch_bounds__(Threads<D>::N) void append_kernel(AppendArgs a) {
-  constexpr int NT = Threads<D>::N, OCTS = D / 8, TOKENS = NT / OCTS;
+__global__ __launch_bounds__(Threads<D>::N, 4) void append_kernel(AppendArgs a) {
+  constexpr int NT = Threads<D>::N, OCTS = D / 8, TOKENS = NT / OCTS, REP = SUB / TOKENS;
   __shared__ __attribute__((aligned(16))) BoundsLds<D> lds;
-  extern __shared__ float2 turn[];  // [64][n]
+  __shared__ Again<D> again;
+  __shared__ int held_on[4];  // pages of the 64 positions (or -1)
+  extern __shared__ __attribute__((aligned(16))) float2 turn[];  // [64][table.size()]
   const CacheArgs &c = a.c;
-  const int tid = threadIdx.x, oct = tid % OCTS, n = a.rot / 2;
-  const int b = blockIdx.x / a.spans, lspan = max(c.lpage, 6);
+  const int tid = threadIdx.x, oct = tid % OCTS, t0 = tid / OCTS, n = a.rot / 2;
+  const Table<MODE> table(n);
+  const int b = blockIdx.x / a.spans, lspan = max(c.lpage, 6), ltok = min(c.lpage, 6);
   const int64_t start = c.starts[b], end = start + c.T;
   const int64_t p0 = ((start >> lspan) + (int)(blockIdx.x % a.spans)) << lspan;
   if (p0 >= end) return;
   const int64_t held = start + (c.counts ? min(max(c.counts[b], 0), c.T) : c.T);  // end of what is held
-  const int heads = c.Hkv, streams = 2 * c.Hkv + a.H;
+  // the share's kind (keys, values, queries), first head, heads and step
+  const int share = blockIdx.y, kind = share < a.kshares ? 0 : share < a.kshares + a.vshares ? 1 : 2;
+  const int h0 = share - (kind == 0 ? 0 : kind == 1 ? a.kshares : a.kshares + a.vshares);
+  const int by = kind == 0 ? a.kshares : kind == 1 ? a.vshares : (int)gridDim.y - a.kshares - a.vshares;
+  const int heads = kind == 2 ? a.H : c.Hkv;
+  const bool bounds = kind == 0 && a.bounds && held > start;
+  if (tid < 3) again.count[tid] = 0;
+  int turns = 0;  // heads of keys so far
   for (int sub = 0; sub < 1 << (lspan - 6); ++sub) {
-    const int64_t base = p0 + sub * SUB;
-    if (base >= end) break;
-    const int lo = (int)max((int64_t)0, start - base), hi = (int)min((int64_t)SUB, end - base);  // (lo > hi: none)
-    if (lo >= hi && !a.bounds) continue;
-    // angles of the new tokens
+    Span s;
+    s.base = p0 + sub * SUB;
+    if (s.base >= end) break;
+    s.first = s.base - start;
+    s.lo = (int)min((int64_t)SUB, max((int64_t)0, -s.first)), s.hi = (int)min((int64_t)SUB, end - s.base);
+    if (s.lo >= s.hi && !bounds) continue;
+    const int64_t page0 = max(start >> c.lpage << c.lpage, (int64_t)0);
+    s.old = (int)min((int64_t)SUB, max((int64_t)0, page0 - s.base));
+    s.to = (int)max((int64_t)0, min((int64_t)SUB, held - s.base));
+    Rows<TI, REP> rows(kind == 0 ? c.k : kind == 1 ? c.v : a.q, b, h0, by, s, t0, TOKENS, oct);
     __syncthreads();
-    for (int e = tid; e < (hi - lo) * n; e += NT) {
-      float s, w;
-      turn_of((double)(base + lo + e / n), a.freq[e % n], s, w);
-      turn[lo * n + e] = make_float2(w * a.factor, s * a.factor);
+    if (tid < 4) held_on[tid] = tid < SUB >> ltok ? page_of(c, b, s.base + (tid << ltok)) : -1;
+    if (kind != 1) {
+      // angles of the new tokens
+      for (int e = tid; e < (s.hi - s.lo) * n; e += NT) {
+        const int t = s.lo + e / n, m = e % n;
+        float sn, cs;
+        turn_of((double)(s.base + t), a.freq[m], sn, cs);
+        turn[t * table.size() + table.at(m)] = make_float2(cs * a.factor, sn * a.factor);
+      }
     }
     __syncthreads();
-    // tokens whose keys are on a page that gets tokens: in bounds from `old` on
-    const int64_t page0 = max(start >> c.lpage << c.lpage, (int64_t)0);
-    const int old = (int)min((int64_t)SUB, max((int64_t)0, page0 - base));
-    const int to = (int)max((int64_t)0, min((int64_t)SUB, held - base));
-    for (int st = blockIdx.y; st < streams; st += gridDim.y) {
-      const int kind = st < heads ? 0 : st < 2 * heads ? 1 : 2;  // keys, values, queries
-      const int h = kind == 0 ? st : kind == 1 ? st - heads : st - 2 * heads;
-      const View &v = kind == 0 ? c.k : kind == 1 ? c.v : a.q;
-      const TI *src = slice_of<TI>(v, b, h);
-      const bool bounds = kind == 0 && a.bounds && held > start;
+    if (kind == 2) {
+      TI *out[REP];
+#pragma unroll
+      for (int r = 0; r < REP; ++r)
+        out[r] = slice_of<TI>(a.qo, b, h0) + (s.first + t0 + r * TOKENS) * a.qo.st + 8 * oct;
 #pragma unroll 1
-      for (int t = tid / OCTS; t < SUB; t += TOKENS) {
-        const bool in = t >= lo && t < hi;
-        const TI *row = src + (base + t - start) * v.st;
-        Chunk<MODE> x = {};
-        if (in) {
-          if (kind == 1) load8(row + 8 * oct, x.x);
-          else load_pairs<TI, MODE>(row, oct, n, x);
+      for (int h = h0; h < heads; h += by) {
+#pragma unroll
+        for (int r = 0; r < REP; ++r) {
+          const TI *row = rows.p[r] - 8 * oct;
+          const Raw<TI> raw = rows.take(r, h + by < heads);
+          Chunk x;
+          pairs_of<TI, MODE>(raw, rows.in[r] ? row : nullptr, oct, n, x);
+          float z[8];
+          turned<MODE>(x, turn + (t0 + r * TOKENS) * table.size(), oct, n, z);
+          if (rows.in[r]) store8(out[r], z);
+          out[r] += by * a.qo.sh;
         }
-        if (kind == 2) {
-          if (!in) continue;
-          float z[8], tol[8];
-          turned<MODE, false>(x, turn + t * n, oct, n, 0.f, z, tol);
-          store8(slice_of<TI>(a.qo, b, h) + (base + t - start) * a.qo.st + 8 * oct, z);
-          continue;
-        }
-        const bool live = in && base + t < held, before = bounds && t >= old && base + t < start;
-        const int page = live || before ? page_of(c, b, base + t) : -1;
-        uint32_t w, s;
-        if (kind == 0) {
-          const bool open = quantise_turned<MODE>(x, turn + (live ? t : 0) * n, oct, n, a.factor, w, s);
-          // a group goes again if one of its four lanes asks for it
-          const uint64_t again = __ballot(open && live && page >= 0) >> (tid & 60) & 15;
-          if (__builtin_expect(__any(again != 0), 0)) {
-            if (again) quantise_turned64<MODE>(x, (double)(base + t), oct, n, a, w, s);
-          }
-        } else {
-          quantise(x.x, w, s);
-        }
-        if (page < 0) continue;
-        const int tok = (int)((base + t) & ((1 << c.lpage) - 1));
-        uint8_t *at = c.cache + cache_block<D>(page, kind, h, c.Hkv, c.lpage);
-        if (live) put<D>(w, s, at, tok, kind, oct, c.lpage);
-        else held_of<D>(at, tok, kind, oct, c.lpage, w, s);
-        if (bounds) keep<D>(lds, t, oct, w, s);
       }
-      if (!bounds) continue;
+      continue;
+    }
+    // where the thread's tokens are held: the codes of its channels, and their group's scale
+    // byte behind them; steps of a head
+    const int codes = D / 2 << c.lpage;
+    const int64_t block = codes + (D / 32 << c.lpage);
+    uint8_t *at[REP];
+#pragma unroll
+    for (int r = 0; r < REP; ++r) {
+      const int t = t0 + r * TOKENS, page = t < s.to ? held_on[t >> ltok] : -1;
+      at[r] = page < 0 ? nullptr : c.cache + (((int64_t)page * 2 + kind) * c.Hkv + h0) * block;
+    }
+    auto token_of = [&](int t) { return (int)((s.base + t) & ((1 << c.lpage) - 1)); };
+    if (kind == 1) {
+#pragma unroll 1
+      for (int h = h0; h < heads; h += by) {
+#pragma unroll
+        for (int r = 0; r < REP; ++r) {
+          const Raw<TI> raw = rows.take(r, h + by < heads);
+          float x[8];
+          raw.values(x);
+          uint32_t w, sc;
+          quantise(x, w, sc);
+          if (at[r]) {
+            if (rows.in[r]) put<D>(w, sc, at[r], token_of(t0 + r * TOKENS), 1, oct, c.lpage);
+            at[r] += by * block;
+          }
+        }
+      }
+      continue;
+    }
+#pragma unroll 1
+    for (int h = h0; h < heads; h += by, ++turns) {
+      if (bounds && s.old < s.lo) {
+        // the page's earlier tokens
+        uint32_t w[REP], sc[REP];
+#pragma unroll
+        for (int r = 0; r < REP; ++r) {
+          const int t = t0 + r * TOKENS;
+          sc[r] = 256;
+          if (at[r] && t >= s.old && t < s.lo) held_of<D>(at[r], token_of(t), 0, oct, c.lpage, w[r], sc[r]);
+        }
+#pragma unroll
+        for (int r = 0; r < REP; ++r)
+          if (sc[r] < 256) keep<D>(lds, t0 + r * TOKENS, oct, w[r], sc[r]);
+      }
+#pragma unroll
+      for (int r = 0; r < REP; ++r) {
+        const int t = t0 + r * TOKENS;
+        const TI *row = rows.p[r] - 8 * oct;
+        const Raw<TI> raw = rows.take(r, h + by < heads);
+        if (!__any(rows.in[r])) continue;
+        Chunk x;
+        pairs_of<TI, MODE>(raw, rows.in[r] ? row : nullptr, oct, n, x);
+        uint32_t w, sc;
+        const bool open = quantise_turned<MODE>(x, turn + (rows.in[r] ? t : s.lo) * table.size(), oct, n, a.factor, w, sc);
+        const bool live = rows.in[r] && at[r];
+        // a group goes again if one of its four lanes asks for it
+        if (__ballot(open && live) >> (tid & 60) & 15) {
+          if (tid % 4 == 0) again.list[atomicAdd(&again.count[turns % 3], 1)] = (uint16_t)(t * (D / 32) + oct / 4);
+        } else if (live) {
+          put<D>(w, sc, at[r], token_of(t), 0, oct, c.lpage);
+          if (bounds) keep<D>(lds, t, oct, w, sc);
+        }
+      }
       __syncthreads();
-      bounds_of<D>(lds, c.lpage, old, to, sub > 0, [&](int t) -> uint32_t * {
-        const int page = page_of(c, b, base + t);
-        return page < 0 ? nullptr : a.bounds + ((int64_t)page * c.Hkv + h) * D;
-      });
+      const int count = again.count[turns % 3];
+      if (tid == 0) again.count[(turns + 2) % 3] = 0;
+      if (count) {
+        // (a lane a channel)
+        const TI *src = slice_of<TI>(c.k, b, h) + s.first * c.k.st;
+        for (int e = tid / 32; e < count; e += NT / 32) {
+          const int t = again.list[e] / (D / 32), ch = again.list[e] % (D / 32) * 32 + tid % 32;
+          uint32_t w, sc;
+          quantise_turned64<TI, MODE>(src + t * c.k.st, (double)(s.base + t), ch, n, a, w, sc);
+          if (ch % 8) continue;
+          put<D>(w, sc, c.cache + cache_block<D>(held_on[t >> ltok], 0, h, c.Hkv, c.lpage), token_of(t), 0, ch / 8, c.lpage);
+          if (bounds) keep<D>(lds, t, ch / 8, w, sc);
+        }
+        __syncthreads();
+      }
+      if (bounds)
+        bounds_of<D>(lds, c.lpage, s.old, s.to, sub > 0, [&](int t) -> uint32_t * {
+          const int page = held_on[t >> ltok];
+          return page < 0 ? nullptr : a.bounds + ((int64_t)page * c.Hkv + h) * D;
+        });
+#pragma unroll
+      for (int r = 0; r < REP; ++r)
+        if (at[r]) at[r] += by * block;
     }
   }
 }
@@ -371,14 +532,14 @@ template <int D> __global__ __launch_bounds__(Threads<D>::N) void bounds_kernel(
   }
 }
 
+template <typename TI, int D, int MODE> void append_mode(const AppendArgs &a, dim3 grid, hipStream_t s) {
+  const size_t lds = (size_t)SUB * Table<MODE>(a.rot / 2).size() * sizeof(float2);
+  hipLaunchKernelGGL((append_kernel<TI, D, MODE>), grid, dim3(Threads<D>::N), lds, s, a);
+}
 template <typename TI, int D> void append_as(const AppendArgs &a, dim3 grid, hipStream_t s) {
-  const size_t lds = (size_t)SUB * (a.rot / 2) * sizeof(float2);
-  if (a.layout == KIA_ROTARY_NEIGHBOURS)
-    hipLaunchKernelGGL((append_kernel<TI, D, NEIGHBOURS>), grid, dim3(Threads<D>::N), lds, s, a);
-  else if (a.rot / 2 % 8 == 0)
-    hipLaunchKernelGGL((append_kernel<TI, D, HALF8>), grid, dim3(Threads<D>::N), lds, s, a);
-  else
-    hipLaunchKernelGGL((append_kernel<TI, D, HALF>), grid, dim3(Threads<D>::N), lds, s, a);
+  if (a.layout == KIA_ROTARY_NEIGHBOURS) append_mode<TI, D, NEIGHBOURS>(a, grid, s);
+  else if (a.rot / 2 % 8 == 0) append_mode<TI, D, HALF8>(a, grid, s);
+  else append_mode<TI, D, HALF>(a, grid, s);
 }
 template <int D> void append_d(const AppendArgs &a, dim3 grid, int dtype, hipStream_t s) {
   if (dtype == KIA_F32) append_as<float, D>(a, grid, s);
@@ -387,10 +548,14 @@ template <int D> void append_d(const AppendArgs &a, dim3 grid, int dtype, hipStr
 
 }  // namespace
 
-void launch_append(const AppendArgs &a, int d, int dtype, int cus, hipStream_t s) {
-  const unsigned spans = (unsigned)a.c.B * a.spans, streams = 2u * a.c.Hkv + a.H;
-  const unsigned shares = std::min(streams, std::max(1u, (4u * cus + spans - 1) / spans));
-  const dim3 grid(spans, shares);
+// Workgroups: the spans of 64 positions (or a page), and of each span's heads as many shares
+// as it takes to reach `per CU` of them; keys, values and queries have shares of their own.
+void launch_append(AppendArgs a, int d, int dtype, int cus, hipStream_t s) {
+  const unsigned spans = (unsigned)a.c.B * a.spans;
+  const int want = (int)std::max(1u, (4u * cus + spans - 1) / spans), all = 2 * a.c.Hkv + a.H;
+  auto part = [&](int heads) { return std::min(heads, std::max(1, (heads * want + all - 1) / all)); };
+  a.kshares = a.vshares = part(a.c.Hkv);
+  const dim3 grid(spans, 2 * a.kshares + part(a.H));
   if (d == 32) append_d<32>(a, grid, dtype, s);
   else if (d == 64) append_d<64>(a, grid, dtype, s);
   else append_d<128>(a, grid, dtype, s);

@@ -103,12 +103,13 @@ struct AppendArgs {
   float factor;
   int layout, rot, H;
   int spans;  // of a sequence's new tokens: 64 positions or a page, whichever is more
+  int kshares, vshares;  // shares of the key heads' keys and values (the launcher's)
 };
 inline int append_spans(int T, int lpage) {
   const int l = lpage > 6 ? lpage : 6;
   return ((T - 1 + (1 << l) - 1) >> l) + 1;
 }
-void launch_append(const AppendArgs &a, int d, int dtype, int cus, hipStream_t s);
+void launch_append(AppendArgs a, int d, int dtype, int cus, hipStream_t s);
 void launch_bounds(const AppendArgs &a, int d, hipStream_t s);
 
 // ---- selected pages (kia_select.hip) ------------------------------------------------

@@ -55,6 +55,15 @@ __device__ __forceinline__ void values_of(uint32_t w, float f, float (&x)[8]) {
   pair_of<3>(w, f, x);
 }
 
+// byte `s` of a word of codes as two bf16
+template <int S> __device__ __forceinline__ uint32_t pair(uint32_t w, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, S));
+}
+__device__ __forceinline__ uint32_t pair_at(int s, uint32_t w, float scale) {
+  return s == 0 ? pair<0>(w, scale) : s == 1 ? pair<1>(w, scale) : s == 2 ? pair<2>(w, scale)
+                                                                     : pair<3>(w, scale);
+}
+
 // The exponent of a group's scale from its largest magnitude (as bits: NaN above infinity
 // above every finite value): top = 1.m 2^k is at most 6 2^(k - 2) if 1.m <= 1.5, and
 // 6 2^(k - 1) otherwise.
@@ -63,14 +72,19 @@ __device__ __forceinline__ int scale_exp(uint32_t top) {
   return min(max(e, -126), 125);
 }
 
+// The largest of a group's four lanes.
+__device__ __forceinline__ uint32_t quad_max(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xb1, 0xf, 0xf, true));    // quad_perm 1 0 3 2
+  return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4e, 0xf, 0xf, true));  // quad_perm 2 3 0 1
+}
+
 // The codes w and the scale byte s of eight channels of a token: the other 24 of the group
 // are the next lanes' of four.
 __device__ __forceinline__ void quantise(const float (&x)[8], uint32_t &w, uint32_t &s) {
   uint32_t top = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
-  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+  top = quad_max(top);
   const int e = scale_exp(top);
   const bool bad = top >= 0x7f800000u;
   const float f = __uint_as_float((uint32_t)(127 - e) << 23);

@@ -8,8 +8,6 @@
 
 namespace kia {
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
 // 32 keys at a time: two tiles of 16 and the next two on their way leave room for three
 // workgroups a CU in bf16 (162 registers; with 64 keys 217, two workgroups, and the
 // interval weights of 32 x 16 500 keys took 101 us against 88).
@@ -20,14 +18,6 @@ __device__ __forceinline__ f32x4 mma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// byte `s` of a word of codes as two bf16
-template <int S> __device__ __forceinline__ uint32_t pair(uint32_t w, float scale) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, S));
-}
-__device__ __forceinline__ uint32_t pair_at(int s, uint32_t w, float scale) {
-  return s == 0 ? pair<0>(w, scale) : s == 1 ? pair<1>(w, scale) : s == 2 ? pair<2>(w, scale)
-                                                                     : pair<3>(w, scale);
-}
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 // One lane's share of a chunk: codes and scales of its keys and values.

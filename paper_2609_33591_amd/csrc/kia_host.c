@@ -37,6 +37,19 @@ static int (*p_attn_ws)(int, int, int, int, int, int, int, int, int, size_t *);
 static int (*p_attn)(const kia_view *, const kia_view *, const void *, int, int, const int32_t *, int,
                      const int32_t *, void *, int, int, int, int, int, int, int, float, int, int, int,
                      int, void *);
+static int (*p_append)(const kia_view *, const kia_view *, const kia_view *, const kia_view *, void *, void *,
+                       int, int, const int32_t *, int, const int32_t *, const int32_t *, const double *, float,
+                       int, int, int, int, int, int, int, int, void *);
+static int (*p_select_ws)(int, int, int, int, int, int, int, size_t *);
+static int (*p_select)(const kia_view *, const void *, int, int, const int32_t *, int, const int32_t *, void *,
+                       int32_t *, int, int, int, int, int, int, int, int, int, void *);
+static int (*p_pages_ws)(int, int, int, int, int, int, int, int, size_t *);
+static int (*p_attn_pages)(const kia_view *, const kia_view *, const void *, int, int, const int32_t *, int,
+                           const int32_t *, const int32_t *, int, void *, int, int, int, int, int, int, int, float,
+                           int, int, void *);
+static int (*p_shared_ws)(int, int, int, int, int, int, int, int, size_t *);
+static int (*p_attn_shared)(const kia_view *, const kia_view *, const void *, int, int, const int32_t *, int,
+                            const int32_t *, int, void *, int, int, int, int, int, int, int, float, int, int, void *);
 
 /* ---- reading a tensor: 1 as wanted, 0 not (no exception is left) ---------------- */
 typedef struct {
@@ -417,6 +430,137 @@ static PyObject *cache4_attention(PyObject *self, PyObject *const *a, Py_ssize_t
   return done(rc, o);
 }
 
+/* a cache's bounds [pages, heads, 2, d] in bf16, contiguous, on the cache's device */
+static int bounds_of(PyObject *o, const tensor *c, long d, uintptr_t *out) {
+  tensor t;
+  if (!read_tensor(o, &t) || t.dims != 4 || t.dtype != KIA_BF16 || t.device != c->device || !t.ptr || t.ptr % 16)
+    return 0;
+  if (t.n[0] != c->n[0] || t.n[1] != c->n[2] || t.n[2] != 2 || t.n[3] != d) return 0;
+  if (t.s[3] != 1 || t.s[2] != d || (t.n[1] > 1 && t.s[1] != 2 * d) || (t.n[0] > 1 && t.s[0] != 2 * d * t.n[1]))
+    return 0;
+  *out = t.ptr;
+  return 1;
+}
+
+/* cache4_append(q, k, v, data, page, d, table, starts, counts, freq, factor, layout, bounds) -> q turned */
+static PyObject *cache4_append(PyObject *self, PyObject *const *a, Py_ssize_t na) {
+  tensor q, k, c, f;
+  kia_view vq, vo, vk, vv;
+  int page, d, layout, rc = 0;
+  long width;
+  const int32_t *table, *starts, *counts;
+  uintptr_t bounds = 0;
+  void *stream;
+  if (na != 13 || !view_of(a[1], &k, &vk) || !view_of(a[0], &q, &vq) || !view_like(a[0], &k, q.n[1], &vq) ||
+      !view_like(a[2], &k, k.n[1], &vv) || !an_int(a[4], 1, &page) || !an_int(a[5], 1, &d) ||
+      !cache_args(a[3], a[6], &k, &c, &width, &table) || d != k.n[3] || c.n[2] != k.n[1] ||
+      !ints_of(a[7], &k, 1, &k.n[0], 0, &starts) || !ints_of(a[8], &k, 1, &k.n[0], 1, &counts) ||
+      !an_int(a[11], 0, &layout) || (a[12] != Py_None && !bounds_of(a[12], &c, d, &bounds)))
+    NONE;
+  if (!read_tensor(a[9], &f) || f.dims != 1 || f.device != k.device || f.ptr % 8 || f.n[0] < 1 ||
+      (f.n[0] > 1 && f.s[0] != 1) || 2 * f.n[0] > d)
+    NONE;
+  PyObject *dtype = PyObject_GetAttr(a[9], s_dtype);
+  Py_XDECREF(dtype);
+  const double factor = PyFloat_AsDouble(a[10]);
+  if (PyErr_Occurred()) {
+    PyErr_Clear();
+    NONE;
+  }
+  if (dtype != f64 || !stream_of(&k, &stream)) NONE;
+  PyObject *o = new_like(a[0], &q, &vo);
+  if (!o) return NULL;
+  CALL(p_append(&vq, &vo, &vk, &vv, (void *)c.ptr, (void *)bounds, (int)c.n[0], page, table, (int)width, starts,
+                counts, (const double *)f.ptr, (float)factor, layout, (int)k.n[0], (int)q.n[1], (int)k.n[1],
+                (int)k.n[2], d, (int)(2 * f.n[0]), k.dtype, stream));
+  return done(rc, o);
+}
+
+/* what the calls of queries on a cache share: q, data, page, d, table, lengths */
+static int served_args(PyObject *const *a, tensor *q, tensor *c, kia_view *vq, int *page, int *d, long *width,
+                       const int32_t **table, const int32_t **lengths) {
+  return view_of(a[0], q, vq) && an_int(a[2], 1, page) && an_int(a[3], 1, d) &&
+         cache_args(a[1], a[4], q, c, width, table) && *d == q->n[3] &&
+         ints_of(a[5], q, 1, &q->n[0], 0, lengths);
+}
+
+/* cache4_select(q, data, page, d, table, lengths, bounds, count, first, last) -> pages */
+static PyObject *cache4_select(PyObject *self, PyObject *const *a, Py_ssize_t na) {
+  tensor q, c;
+  kia_view vq;
+  int page, d, count, first, last, rc = 0;
+  long width;
+  const int32_t *table, *lengths;
+  uintptr_t bounds, ws, list;
+  void *stream;
+  size_t need;
+  if (na != 10 || !served_args(a, &q, &c, &vq, &page, &d, &width, &table, &lengths) ||
+      !bounds_of(a[6], &c, d, &bounds) || !an_int(a[7], 1, &count) || !an_int(a[8], 0, &first) ||
+      !an_int(a[9], 1, &last) || (long)first + last > count || !stream_of(&q, &stream) ||
+      p_select_ws(page, (int)width, (int)q.n[0], (int)q.n[1], (int)c.n[2], (int)q.n[2], d, &need))
+    NONE;
+  const long n[4] = {q.n[0], c.n[2], q.n[2], count}, bytes = (long)need;
+  PyObject *o = new_of(a[0], n, 4, i32, &list);
+  PyObject *w = o ? new_of(a[0], &bytes, 1, u8, &ws) : NULL;
+  if (!w) {
+    Py_XDECREF(o);
+    return NULL;
+  }
+  CALL(p_select(&vq, (const void *)bounds, (int)c.n[0], page, table, (int)width, lengths, (void *)ws, (int32_t *)list,
+                count, first, last, (int)q.n[0], (int)q.n[1], (int)c.n[2], (int)q.n[2], d, q.dtype, stream));
+  Py_DECREF(w);
+  return done(rc, o);
+}
+
+/* cache4_served(q, data, page, d, table, lengths, pages or None, shared, K, calib, tau, recon) -> o */
+static PyObject *cache4_served(PyObject *self, PyObject *const *a, Py_ssize_t na) {
+  tensor q, c, t;
+  kia_view vq, vo;
+  int page, d, shared, K, calib, recon, rc = 0;
+  long width;
+  const int32_t *table, *lengths, *list = NULL;
+  void *stream;
+  if (na != 12 || !served_args(a, &q, &c, &vq, &page, &d, &width, &table, &lengths) ||
+      !an_int(a[7], 0, &shared) || !an_int(a[8], INT32_MIN, &K) || !an_int(a[9], INT32_MIN, &calib) ||
+      !an_int(a[11], INT32_MIN, &recon))
+    NONE;
+  const double tau = PyFloat_AsDouble(a[10]);
+  if (PyErr_Occurred()) {
+    PyErr_Clear();
+    NONE;
+  }
+  const int listed = a[6] != Py_None;
+  if (listed == (shared != 0)) NONE; /* (one of the two) */
+  if (listed) {
+    if (!read_tensor(a[6], &t) || t.dims != 4) NONE;
+    const long n[4] = {q.n[0], c.n[2], q.n[2], t.n[3]};
+    if (!ints_of(a[6], &q, 4, n, 0, &list) || t.n[3] < 1 || t.n[3] > INT32_MAX) NONE;
+  }
+  size_t need;
+  if (!stream_of(&q, &stream) ||
+      (listed ? p_pages_ws(page, (int)width, (int)t.n[3], (int)q.n[0], (int)q.n[1], (int)c.n[2], (int)q.n[2], d, &need)
+              : p_shared_ws(page, (int)width, shared, (int)q.n[0], (int)q.n[1], (int)c.n[2], (int)q.n[2], d, &need)))
+    NONE;
+  uintptr_t ws;
+  const long bytes = (long)need;
+  PyObject *o = new_like(a[0], &q, &vo);
+  PyObject *w = o ? new_of(a[0], &bytes, 1, u8, &ws) : NULL;
+  if (!w) {
+    Py_XDECREF(o);
+    return NULL;
+  }
+  if (listed)
+    CALL(p_attn_pages(&vq, &vo, (const void *)c.ptr, (int)c.n[0], page, table, (int)width, lengths, list, (int)t.n[3],
+                      (void *)ws, (int)q.n[0], (int)q.n[1], (int)c.n[2], (int)q.n[2], d, K, calib, (float)tau, recon,
+                      q.dtype, stream));
+  else
+    CALL(p_attn_shared(&vq, &vo, (const void *)c.ptr, (int)c.n[0], page, table, (int)width, lengths, shared,
+                       (void *)ws, (int)q.n[0], (int)q.n[1], (int)c.n[2], (int)q.n[2], d, K, calib, (float)tau, recon,
+                       q.dtype, stream));
+  Py_DECREF(w);
+  return done(rc, o);
+}
+
 /* bind(torch, check, addresses of the entry points by name): before any other call */
 static PyObject *bind(PyObject *self, PyObject *args) {
   PyObject *torch, *fns;
@@ -438,7 +582,11 @@ static PyObject *bind(PyObject *self, PyObject *args) {
       {&p_rotary, "kia_rotary"}, {&p_window_fwd, "kia_window_fwd"},
       {&p_window_ws, "kia_window_ws_bytes"}, {&p_window_bwd, "kia_window_bwd"},
       {&p_write, "kia_cache4_write"}, {&p_read, "kia_cache4_read"},
-      {&p_attn_ws, "kia_cache4_ws_bytes"}, {&p_attn, "kia_cache4_attn"}};
+      {&p_attn_ws, "kia_cache4_ws_bytes"}, {&p_attn, "kia_cache4_attn"},
+      {&p_append, "kia_cache4_append"}, {&p_select_ws, "kia_cache4_select_ws_bytes"},
+      {&p_select, "kia_cache4_select"}, {&p_pages_ws, "kia_cache4_pages_ws_bytes"},
+      {&p_attn_pages, "kia_cache4_attn_pages"}, {&p_shared_ws, "kia_cache4_shared_ws_bytes"},
+      {&p_attn_shared, "kia_cache4_attn_shared"}};
   for (size_t i = 0; i < sizeof entry / sizeof *entry; ++i) {
     PyObject *x = PyDict_GetItemString(fns, entry[i].name);
     void *p = x ? PyLong_AsVoidPtr(x) : NULL;
@@ -455,7 +603,8 @@ static PyMethodDef methods[] = {
     {"bind", bind, METH_VARARGS, NULL},
 #define FAST(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
     FAST(rotary), FAST(window_forward), FAST(window_backward), FAST(cache4_write), FAST(cache4_read),
-    FAST(cache4_attention), {NULL, NULL, 0, NULL}};
+    FAST(cache4_attention), FAST(cache4_append), FAST(cache4_select), FAST(cache4_served),
+    {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", NULL, -1, methods};
 
 PyMODINIT_FUNC PyInit__host(void) {

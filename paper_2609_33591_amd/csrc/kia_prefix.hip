@@ -120,12 +120,6 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void prefix_kernel(CachedArgs a) {
       for (int y = 0; y < N; ++y)
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[y][e] = pair_at(e, cur.k[i][y], f);
-      uint64_t nan = 0;
-      if (__builtin_expect(bad, 0)) {
-        nan = __ballot(cur.ks[i] == 255);
-        nan |= nan >> 32;
-        nan |= nan >> 16;
-      }
 #pragma unroll
       for (int x = 0; x < RT; ++x) {
         f32x4 acc = {};
@@ -134,11 +128,28 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void prefix_kernel(CachedArgs a) {
 #pragma unroll
           for (int y = 0; y < N; ++y) acc = mma16(as_op(w[y]), q[x][p][y], acc);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          S[x][i][e] = nan >> (4 * kb + e) & 1 ? NAN : acc[e];
-          if (!all) S[x][i][e] = sees(x, i, e) ? S[x][i][e] : -INFINITY;
-        }
+        for (int e = 0; e < 4; ++e) S[x][i][e] = acc[e];
       }
+    }
+    if (__builtin_expect(bad, 0)) {
+#pragma unroll
+      for (int i = 0; i < TILES; ++i) {
+        uint64_t nan = __ballot(cur.ks[i] == 255);
+        nan |= nan >> 32;
+        nan |= nan >> 16;
+#pragma unroll
+        for (int x = 0; x < RT; ++x)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) S[x][i][e] = nan >> (4 * kb + e) & 1 ? NAN : S[x][i][e];
+      }
+    }
+    if (!all) {
+#pragma unroll
+      for (int x = 0; x < RT; ++x)
+#pragma unroll
+        for (int i = 0; i < TILES; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) S[x][i][e] = sees(x, i, e) ? S[x][i][e] : -INFINITY;
     }
     if constexpr (PASS == PASS_EXTREMA) {
 #pragma unroll
@@ -162,22 +173,23 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void prefix_kernel(CachedArgs a) {
           for (int i = 0; i < TILES; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) top = fmaxf(top, S[x][i][e]);
-          top = fmaxf(top, __shfl_xor(top, 16));
-          top = fmaxf(top, __shfl_xor(top, 32));
-          // (moved, and the sums scaled, only when passed by 2^8)
-          const bool up = (top - m[x]) * c2 > 8.f;
-          if (__any(up)) {
+          // (moved, and the sums scaled, only when passed by 2^8: where no lane sees that, no row
+          // does)
+          if (__any((top - m[x]) * c2 > 8.f)) {
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const bool up = (top - m[x]) * c2 > 8.f;
             const float f = up ? __builtin_amdgcn_exp2f((m[x] - top) * c2) : 1.f;
             m[x] = up ? top : m[x];
             l[x] *= f;
 #pragma unroll
             for (int y = 0; y < NT; ++y) o[x][y] *= f;
           }
-          const float mm = m[x] == -INFINITY ? 0.f : m[x];
+          const float mm = m[x] == -INFINITY ? 0.f : m[x] * c2;
 #pragma unroll
           for (int i = 0; i < TILES; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[i][e] = __builtin_amdgcn_exp2f((S[x][i][e] - mm) * c2);
+            for (int e = 0; e < 4; ++e) w[i][e] = __builtin_amdgcn_exp2f(fmaf(S[x][i][e], c2, -mm));
         } else {
           grid_weights<CALIB, RECON, 4>(S[x], w, rc[x], Mx[x], Mn[x], a);
           if (!all) {
