@@ -188,9 +188,9 @@ static PyObject *new_like(PyObject *ref, const tensor *t, kia_view *v) {
   v->st = t->n[3], v->sh = t->n[2] * t->n[3], v->sb = t->n[1] * v->sh;
   return o;
 }
-/* torch.empty(*n, dtype=, device=ref.device) */
+/* torch.empty(*n, dtype=, device=ref.device), of up to four dimensions */
 static PyObject *new_of(PyObject *ref, const long *n, int dims, PyObject *dtype, uintptr_t *ptr) {
-  PyObject *args[5] = {NULL}, *o = NULL;
+  PyObject *args[6] = {NULL}, *o = NULL;
   long long v;
   int i, ok = 1;
   for (i = 0; i < dims; ++i) ok = (args[i] = PyLong_FromLong(n[i])) != NULL && ok;
