@@ -33,8 +33,7 @@ OBJECTS = {
     "kia_serve.o": [("kia_serve_abi.hip", []), ("kia_append.hip", []), ("kia_select.hip", [])],
     "kia_window.o": [("kia_window.hip", [f"-DKIA_HEAD={d}"]) for d in HEADS],
     "kia_cached.o": [("kia_cached.hip", [f"-DKIA_HEAD={d}"]) for d in HEADS[1:]],
-    "kia_served.o": [("kia_cached.hip", [f"-DKIA_HEAD={d}", f"-DKIA_MODE={m}"]) for d in HEADS[1:] for m in (1, 2)]
-                    + [("kia_prefix.hip", [f"-DKIA_HEAD={d}"]) for d in HEADS[1:]],
+    "kia_served.o": [("kia_cached.hip", [f"-DKIA_HEAD={d}", f"-DKIA_MODE={m}"]) for d in HEADS[1:] for m in (1, 2)],
 }
 # (source, flags, object file) of every compilation
 UNITS = [(src, flags, obj if len(parts) == 1 else f"{obj[:-2]}_{i}.o")

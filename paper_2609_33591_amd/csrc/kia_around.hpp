@@ -131,6 +131,7 @@ void launch_select(const SelectArgs &a, int d, int dtype, hipStream_t s);
 struct Prefix {
   float *ext, *stat, *part;  // as CachedArgs'
   int tiles, parts;
+  unsigned blocks;  // workgroups
   __host__ __device__ int64_t slot(int hk, int64_t row) const {
     return (((int64_t)hk * tiles + row / 16) * parts) * 16 + row % 16;
   }
@@ -175,6 +176,5 @@ inline CachedLayout cached_layout(const CachedArgs &a, int d) {
 template <int D> void launch_cached(const CachedArgs &a, int dtype, hipStream_t s);
 template <int D> void launch_listed(const CachedArgs &a, int dtype, hipStream_t s);
 template <int D> void launch_shared(const CachedArgs &a, int dtype, hipStream_t s);
-template <int D> void launch_prefix(const CachedArgs &a, int dtype, bool extrema, hipStream_t s);
 
 }  // namespace kia

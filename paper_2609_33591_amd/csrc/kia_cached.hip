@@ -28,8 +28,8 @@
 // queries and weights go as three bf16 pieces (exact for 2^-100 to 2^126; smaller ones lose
 // less than 2^-133), which the idle matrix unit takes for free. Sums, extrema and
 // statistics are fp32.
-#include "kia_cached.hpp"
 #include "kia_host.hpp"
+#include "kia_prefix.hpp"
 
 #ifndef KIA_MODE
 #define KIA_MODE 0
@@ -40,7 +40,8 @@ namespace {
 
 // Which keys a row sees: all of its sequence's up to its own (within a window, and the
 // first ones); those of the pages that a list names for its token and key head; or those
-// behind the tokens that the batch shares (kia_prefix.hip takes these).
+// behind the tokens that the batch shares (kia_prefix.hpp takes these, in the launch's first
+// workgroups).
 enum { SEQUENCE, LISTED, BEHIND };
 constexpr int MODE = KIA_MODE;
 
@@ -183,11 +184,13 @@ struct Work {
 // Nearest with MinMax 124 -> 107 and its extrema 73 -> 65. The softmax, whose maximum then
 // crosses more lanes, is not (118 and 119 us there), nor are extrema without the minimum
 // (16 of those sequences in fp32: 40 -> 45 us).
-template <typename TI, int D, int PASS, int CALIB, int RECON, bool FEW>
+// RT: row tiles of a wave over shared tokens (0: there are none).
+template <typename TI, int D, int PASS, int CALIB, int RECON, bool FEW, int RT>
 __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
   constexpr int NP = Pieces<TI>::N, N = D / 32, NT = D / 16, NE = FEW ? 1 : 4;
   constexpr bool VALUES = PASS != PASS_EXTREMA;
-  __shared__ float red[NWAVE][16][2];
+  __shared__ WaveStats stats[RT ? RT : 1];
+  WaveStats &red = stats[0];
   __shared__ int2 listed[MODE == LISTED ? LISTED_MOST : 1];
   __shared__ __attribute__((aligned(16))) float rows[VALUES ? NWAVE * 16 * (D + 4) : 4];
   const int tid = threadIdx.x, lane = tid & 63, kb = lane >> 4;
@@ -195,8 +198,16 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
   const int col = FEW ? slot & 3 : slot;    // its row
   const int own = FEW ? slot >> 2 : 0;      // of its four scores a tile, the one it weighs
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int hk = blockIdx.x % a.Hkv, tile = (int)(blockIdx.x / a.Hkv) % a.tiles;
-  const int w = blockIdx.x / (a.Hkv * a.tiles);
+  unsigned block_id = blockIdx.x;
+  if constexpr (RT > 0) {
+    if (block_id < a.pre.blocks) {
+      prefix_part<TI, D, PASS, CALIB, RECON, RT>(a, stats, rows);
+      return;
+    }
+    block_id -= a.pre.blocks;
+  }
+  const int hk = block_id % a.Hkv, tile = (int)(block_id / a.Hkv) % a.tiles;
+  const int w = block_id / (a.Hkv * a.tiles);
   const Work work(a, tile, w);
   if (work.b < 0) return;
   const int b = work.b, G = a.H / a.Hkv, total = work.rows, lo = work.lo, hi = work.hi;
@@ -589,75 +600,69 @@ template <typename TI, int D> __global__ __launch_bounds__(256) void join_kernel
   else *reinterpret_cast<u32x2 *>(y) = u32x2{cvt_bf16x2(x[0], x[1]), cvt_bf16x2(x[2], x[3])};
 }
 
-enum { EXTREMA = 1, WEIGHTS = 2, JOIN = 4 };  // which passes to launch
-
-template <typename TI, int D, bool FEW, int CALIB>
-void grid_passes(const CachedArgs &a, dim3 g, int what, hipStream_t s) {
+// The passes' launches (g: workgroups, join: whether a row has several parts).
+template <typename TI, int D, bool FEW, int CALIB, int RT>
+void grid_passes(const CachedArgs &a, dim3 g, hipStream_t s) {
   const dim3 t(64 * NWAVE);
-  if (what & EXTREMA)
-    timed_call("kia_cache4_extrema", s, [&] {
-      hipLaunchKernelGGL((cached_kernel<TI, D, PASS_EXTREMA, CALIB, REC_LERP, FEW && CALIB != CAL_FWM>),
-                         g, t, 0, s, a);
-    });
-  if (what & WEIGHTS)
-    timed_call("kia_cache4_attn", s, [&] {
-      if (a.recon == REC_LERP)
-        hipLaunchKernelGGL((cached_kernel<TI, D, PASS_GRID, CALIB, REC_LERP, FEW>), g, t, 0, s, a);
-      else
-        hipLaunchKernelGGL((cached_kernel<TI, D, PASS_GRID, CALIB, REC_NEAREST, FEW>), g, t, 0, s, a);
-    });
+  timed_call("kia_cache4_extrema", s, [&] {
+    hipLaunchKernelGGL((cached_kernel<TI, D, PASS_EXTREMA, CALIB, REC_LERP, FEW && CALIB != CAL_FWM, RT>),
+                       g, t, 0, s, a);
+  });
+  timed_call("kia_cache4_attn", s, [&] {
+    if (a.recon == REC_LERP)
+      hipLaunchKernelGGL((cached_kernel<TI, D, PASS_GRID, CALIB, REC_LERP, FEW, RT>), g, t, 0, s, a);
+    else
+      hipLaunchKernelGGL((cached_kernel<TI, D, PASS_GRID, CALIB, REC_NEAREST, FEW, RT>), g, t, 0, s, a);
+  });
 }
 
-template <typename TI, int D, int CALIB> void grid_rows(const CachedArgs &a, dim3 g, int what, hipStream_t s) {
-  if ((MODE == LISTED ? 1 : a.T) * (a.H / a.Hkv) <= 4) grid_passes<TI, D, true, CALIB>(a, g, what, s);
-  else grid_passes<TI, D, false, CALIB>(a, g, what, s);
+template <typename TI, int D, int CALIB, int RT> void grid_rows(const CachedArgs &a, dim3 g, hipStream_t s) {
+  if ((MODE == LISTED ? 1 : a.T) * (a.H / a.Hkv) <= 4) grid_passes<TI, D, true, CALIB, RT>(a, g, s);
+  else grid_passes<TI, D, false, CALIB, RT>(a, g, s);
 }
 
-template <typename TI, int D> void run(const CachedArgs &a, int what, hipStream_t s) {
-  const dim3 g((unsigned)(MODE == SEQUENCE ? a.shares + a.B : a.shares) * a.Hkv * a.tiles);
+template <typename TI, int D, int RT> void run(const CachedArgs &a, bool join, hipStream_t s) {
+  const int parts = MODE == SEQUENCE ? a.shares + a.B : a.shares;
+  const dim3 g((RT ? a.pre.blocks : 0) + (unsigned)parts * a.Hkv * a.tiles);
   if (a.recon == REC_SOFTMAX) {
-    if (what & WEIGHTS)
-      timed_call("kia_cache4_attn", s, [&] {
-        hipLaunchKernelGGL((cached_kernel<TI, D, PASS_SOFTMAX, CAL_FWM, REC_SOFTMAX, false>), g,
-                           dim3(64 * NWAVE), 0, s, a);
-      });
+    timed_call("kia_cache4_attn", s, [&] {
+      hipLaunchKernelGGL((cached_kernel<TI, D, PASS_SOFTMAX, CAL_FWM, REC_SOFTMAX, false, RT>), g,
+                         dim3(64 * NWAVE), 0, s, a);
+    });
   } else if (a.calib == CAL_MINMAX) {
-    grid_rows<TI, D, CAL_MINMAX>(a, g, what, s);
+    grid_rows<TI, D, CAL_MINMAX, RT>(a, g, s);
   } else if (a.calib == CAL_FWM) {
-    grid_rows<TI, D, CAL_FWM>(a, g, what, s);
+    grid_rows<TI, D, CAL_FWM, RT>(a, g, s);
   } else {
-    grid_rows<TI, D, CAL_RESOLVED>(a, g, what, s);
+    grid_rows<TI, D, CAL_RESOLVED, RT>(a, g, s);
   }
-  if (what & JOIN) {
+  if (join) {
     timed_call("kia_cache4_join", s, [&] {
       hipLaunchKernelGGL((join_kernel<TI, D>), dim3((unsigned)(a.B * a.Hkv) * (a.T * (a.H / a.Hkv))), dim3(256), 0,
                          s, a);
     });
   }
 }
-template <int D> void run(const CachedArgs &a, int dtype, int what, hipStream_t s) {
-  if (dtype == KIA_F32) run<float, D>(a, what, s);
-  else run<uint16_t, D>(a, what, s);
+template <int D, int RT> void run_as(const CachedArgs &a, int dtype, bool join, hipStream_t s) {
+  // (fp32 heads of 128: two tiles do not fit the registers)
+  if (dtype == KIA_F32) run<float, D, RT == 2 && D == 128 ? 1 : RT>(a, join, s);
+  else run<uint16_t, D, RT>(a, join, s);
 }
 
 }  // namespace
 
 #if KIA_MODE == 0
 template <> void launch_cached<KIA_HEAD>(const CachedArgs &a, int dtype, hipStream_t s) {
-  run<KIA_HEAD>(a, dtype, EXTREMA | WEIGHTS | (a.shares > 1 ? JOIN : 0), s);
+  run_as<KIA_HEAD, 0>(a, dtype, a.shares > 1, s);
 }
 #elif KIA_MODE == 1
 template <> void launch_listed<KIA_HEAD>(const CachedArgs &a, int dtype, hipStream_t s) {
-  run<KIA_HEAD>(a, dtype, EXTREMA | WEIGHTS | (a.parts > 1 ? JOIN : 0), s);
+  run_as<KIA_HEAD, 0>(a, dtype, a.parts > 1, s);
 }
 #else
 template <> void launch_shared<KIA_HEAD>(const CachedArgs &a, int dtype, hipStream_t s) {
-  if (a.recon != REC_SOFTMAX) {
-    launch_prefix<KIA_HEAD>(a, dtype, true, s);
-    run<KIA_HEAD>(a, dtype, EXTREMA, s);
-  }
-  launch_prefix<KIA_HEAD>(a, dtype, false, s);
-  run<KIA_HEAD>(a, dtype, WEIGHTS | JOIN, s);
+  if (prefix_tiles(a.pre.tiles, KIA_HEAD, dtype) == 1) run_as<KIA_HEAD, 1>(a, dtype, true, s);
+  else run_as<KIA_HEAD, 2>(a, dtype, true, s);
 }
 #endif
 

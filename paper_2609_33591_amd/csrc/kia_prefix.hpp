@@ -1,6 +1,6 @@
-// kia_prefix.hip -- attention over the tokens that all sequences of a batch share, for one
-// head dimension (KIA_HEAD): the part of each row's sums that kia_cached.hip's passes over
-// what lies behind them complete.
+// kia_prefix.hpp -- attention over the tokens that all sequences of a batch share: the part
+// of each row's sums that those over what lies behind them (kia_cached.hip) complete, in
+// workgroups of the same launch.
 //
 // The rows (sequence, token, head of the group) of a key head meet the same keys, so they
 // are one product: 16 rows a tile as in kia_cached.hip, with its operands and orders, and RT
@@ -8,21 +8,22 @@
 // 100 vector operations, and a tile's weights, about as many, bound the kernel before
 // the matrix unit does; the keys come out of the L2 after the first tile. Key heads go round
 // the workgroups, so that an XCD's share of them are few and fit.
+#pragma once
+
 #include "kia_cached.hpp"
-#include "kia_host.hpp"
 
 namespace kia {
-namespace {
 
 // The last key of the shared tokens that a row at `pos` sees.
 __device__ __forceinline__ int last_of(const CachedArgs &a, int pos) { return min(pos, a.shared - 1); }
 
+// LDS of a workgroup: its waves' statistics and, tile by tile, their rows.
+typedef float WaveStats[NWAVE][16][2];
+
 template <typename TI, int D, int PASS, int CALIB, int RECON, int RT>
-__global__ __launch_bounds__(64 * NWAVE, 2) void prefix_kernel(CachedArgs a) {
+__device__ __forceinline__ void prefix_part(const CachedArgs &a, WaveStats *red, float *rows) {
   constexpr int NP = Pieces<TI>::N, N = D / 32, NT = D / 16;
   constexpr bool VALUES = PASS != PASS_EXTREMA;
-  __shared__ float red[RT][NWAVE][16][2];
-  __shared__ __attribute__((aligned(16))) float rows[VALUES ? NWAVE * 16 * (D + 4) : 4];
   const int tid = threadIdx.x, lane = tid & 63, kb = lane >> 4, slot = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hk = blockIdx.x % a.Hkv, groups = (a.pre.tiles + RT - 1) / RT;
@@ -323,38 +324,6 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void prefix_kernel(CachedArgs a) {
         if (at == 0) a.pre.stat[out * 2] = top, a.pre.stat[out * 2 + 1] = sum;
       }
     }
-  }
-}
-
-template <typename TI, int D, int CALIB, int RT> void grid_launch(const CachedArgs &a, dim3 g, bool extrema, hipStream_t s) {
-  const dim3 t(64 * NWAVE);
-  if (extrema) hipLaunchKernelGGL((prefix_kernel<TI, D, PASS_EXTREMA, CALIB, REC_LERP, RT>), g, t, 0, s, a);
-  else if (a.recon == REC_LERP) hipLaunchKernelGGL((prefix_kernel<TI, D, PASS_GRID, CALIB, REC_LERP, RT>), g, t, 0, s, a);
-  else hipLaunchKernelGGL((prefix_kernel<TI, D, PASS_GRID, CALIB, REC_NEAREST, RT>), g, t, 0, s, a);
-}
-
-template <typename TI, int D, int RT> void launch_rows(const CachedArgs &a, bool extrema, hipStream_t s) {
-  const dim3 g((unsigned)a.Hkv * ((a.pre.tiles + RT - 1) / RT) * a.pre.parts);
-  timed_call(extrema ? "kia_cache4_extrema" : "kia_cache4_attn", s, [&] {
-    if (a.recon == REC_SOFTMAX)
-      hipLaunchKernelGGL((prefix_kernel<TI, D, PASS_SOFTMAX, CAL_FWM, REC_SOFTMAX, RT>), g, dim3(64 * NWAVE), 0, s, a);
-    else if (a.calib == CAL_MINMAX) grid_launch<TI, D, CAL_MINMAX, RT>(a, g, extrema, s);
-    else if (a.calib == CAL_FWM) grid_launch<TI, D, CAL_FWM, RT>(a, g, extrema, s);
-    else grid_launch<TI, D, CAL_RESOLVED, RT>(a, g, extrema, s);
-  });
-}
-
-}  // namespace
-
-template <> void launch_prefix<KIA_HEAD>(const CachedArgs &a, int dtype, bool extrema, hipStream_t s) {
-  constexpr int D = KIA_HEAD;
-  if (prefix_tiles(a.pre.tiles, D, dtype) == 1) {
-    if (dtype == KIA_F32) launch_rows<float, D, 1>(a, extrema, s);
-    else launch_rows<uint16_t, D, 1>(a, extrema, s);
-  } else {
-    // (fp32 heads of 128: two tiles do not fit the registers)
-    if (dtype == KIA_F32) launch_rows<float, D, D == 128 ? 1 : 2>(a, extrema, s);
-    else launch_rows<uint16_t, D, 2>(a, extrema, s);
   }
 }
 

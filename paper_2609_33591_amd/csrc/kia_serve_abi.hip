@@ -209,7 +209,8 @@ int shared_shape(CachedArgs &a, int page, int width, int B, int H, int Hkv, int 
   const int64_t blocks = (int64_t)Hkv * ((a.pre.tiles + rt - 1) / rt);
   a.pre.parts = (int)std::max<int64_t>(
       1, std::min<int64_t>({2 * (int64_t)host_cus() / blocks, ((int64_t)shared + 127) / 128, 128}));
-  if (too_many((double)groups * a.parts) || too_many((double)blocks * a.pre.parts)) return KIA_ERR_SHAPE;
+  if (too_many((double)groups * a.parts + (double)blocks * a.pre.parts)) return KIA_ERR_SHAPE;
+  a.pre.blocks = (unsigned)(blocks * a.pre.parts);
   a.shares = B * a.parts;
   return KIA_OK;
 }
