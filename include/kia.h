@@ -708,8 +708,8 @@ int kia_cache4_bounds(const void *cache, void *bounds, int pages, int page,
  *   sum_c max(q_c lo_c, q_c hi_c),
  * which no score q.k of the page passes; the lower number first between equals.
  * The sums are fp64; one that is NaN counts as infinite. Table entries that
- * name no page are not taken. For few tokens, and at most 64 KB of a key head's
- * queries of a token in fp32 (else KIA_ERR_SHAPE).
+ * name no page are not taken. For few tokens, and (H / Hkv) * d up to 8192 (else
+ * KIA_ERR_SHAPE).
  * `ws`: kia_cache4_select_ws_bytes bytes, 256-byte aligned, uninitialized.
  */
 int kia_cache4_select_ws_bytes(int page, int width, int B, int H, int Hkv,

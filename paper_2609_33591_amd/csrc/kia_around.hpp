@@ -117,12 +117,17 @@ struct SelectArgs {
   const uint32_t *bounds;
   const int *table, *lengths;
   View q;
-  uint64_t *score;  // workspace [B][Hkv][T][width]
-  int *list;        // [B][Hkv][T][count]
+  void *ws;   // select_space(width) bytes for each of [B][Hkv][T]
+  int *list;  // [B][Hkv][T][count]
   int pages, lpage, width, B, H, Hkv, T;
   int count, first, last;
-  int tokens;  // of a workgroup that scores: their rows of a key head are in its LDS
+  bool own;   // a workgroup ranks the pages that it selects from
+  int batch;  // else: pages that one ranks, 64 at least
 };
+constexpr int SELECT_OWN = 1024;  // pages that it can
+__host__ __device__ inline size_t select_space(int width) {
+  return ((size_t)width * 12 + ((size_t)width + 63) / 64 * 16 + 7) / 8 * 8;
+}
 void launch_select(const SelectArgs &a, int d, int dtype, hipStream_t s);
 
 // ---- attention over the cache (kia_cached.hip) ----------------------------------------

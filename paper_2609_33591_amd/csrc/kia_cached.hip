@@ -162,7 +162,8 @@ struct Work {
     if constexpr (MODE == LISTED) {
       t0 = w / parts % a.T, rows = G;
       lo = hi = n - a.T + t0;
-      chunks.count = lo < 0 ? 0 : (int)((((int64_t)a.count << a.lpage) + CHUNK - 1) / CHUNK);
+      // (before the text too, so that the list need not wait for the length)
+      chunks.count = (int)((((int64_t)a.count << a.lpage) + CHUNK - 1) / CHUNK);
     } else {
       t0 = 0, rows = a.T * G;
       lo = rows16.lo, hi = rows16.hi;
@@ -302,6 +303,10 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
   if (c < c1) load(c, cur);
   for (; c < c1; c += NWAVE) {
     if (c + NWAVE < c1) load(c + NWAVE, nxt);
+    if (MODE == LISTED && !cur.ok) {
+      cur = nxt;
+      continue;
+    }
     // every row of the tile sees every key of the chunk
     const int j = cur.at[0], end = (MODE == LISTED ? max(cur.at[0], cur.at[1]) + 16 : j + CHUNK) - 1;
     const bool all = end <= lo && cur.ok == (1 << TILES) - 1 &&

@@ -66,22 +66,15 @@ extern "C" int kia_cache4_bounds(const void *cache, void *bounds, int pages, int
 // ---- selected pages --------------------------------------------------------------------
 namespace {
 
-// Tokens of a workgroup that scores: up to 32 KB of query rows in fp32 (0: not even one).
-int select_tokens(int G, int T, int d) {
-  const int64_t row = (int64_t)G * d * 4;
-  return row > 65536 ? 0 : (int)std::min<int64_t>(T, std::max<int64_t>(1, 32768 / row));
-}
-
 int check_select(int page, int width, int B, int H, int Hkv, int T, int d, int count) {
   const int rc = check_common(B, H, Hkv, T, d, KIA_BF16, false);
   if (rc) return rc;
   if (H % Hkv) return KIA_ERR_HEADS;
   if (page_log(page) < 0) return KIA_ERR_CACHE;
   if (width < 1 || (int64_t)width * page > INT_MAX || count < 1) return KIA_ERR_SHAPE;
-  const int tokens = select_tokens(H / Hkv, T, d), batch = 8 * 256 / d;
-  if (!tokens || (T + tokens - 1) / tokens > 65535) return KIA_ERR_SHAPE;
-  if (too_many((double)B * Hkv * ((width + batch - 1) / batch)) || too_many((double)B * Hkv * T))
-    return KIA_ERR_SHAPE;
+  if ((int64_t)(H / Hkv) * d * 4 > 32768) return KIA_ERR_SHAPE;  // (a token's rows in LDS)
+  // (batches of 64 pages; selections of up to 1024 threads)
+  if (too_many((double)B * Hkv * T * std::max(4, (width + 63) / 64))) return KIA_ERR_SHAPE;
   return KIA_OK;
 }
 
@@ -93,7 +86,7 @@ extern "C" int kia_cache4_select_ws_bytes(int page, int width, int B, int H, int
   *bytes = 0;
   const int rc = check_select(page, width, B, H, Hkv, T, d, 1);
   if (rc) return rc;
-  *bytes = (size_t)B * Hkv * T * width * 8;
+  *bytes = (size_t)B * Hkv * T * select_space(width);
   return KIA_OK;
 }
 
@@ -112,12 +105,17 @@ extern "C" int kia_cache4_select(const kia_view *q, const void *bounds, int page
   a.bounds = static_cast<const uint32_t *>(bounds);
   a.table = table, a.lengths = lengths;
   a.q = view_of(q, B, H, T);
-  a.score = static_cast<uint64_t *>(ws);
+  a.ws = ws;
   a.list = list;
   a.pages = pages, a.lpage = page_log(page), a.width = width;
   a.B = B, a.H = H, a.Hkv = Hkv, a.T = T;
   a.count = count, a.first = first, a.last = last;
-  a.tokens = select_tokens(H / Hkv, T, d);
+  // A workgroup pulls some 30 GB/s of bounds: it ranks up to 100 KB of them itself, or where
+  // there is one for every CU. Else workgroups of a launch of their own, two for a CU, do.
+  const int64_t tokens = (int64_t)B * Hkv * T;
+  a.own = width <= SELECT_OWN && ((int64_t)width * d <= 25600 || tokens >= host_cus());
+  a.batch = 64;
+  while (a.batch < 1024 && tokens * ((width + a.batch - 1) / a.batch) > 2 * host_cus()) a.batch *= 2;
   launch_select(a, d, dtype, static_cast<hipStream_t>(stream));
   return launched();
 }

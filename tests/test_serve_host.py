@@ -88,7 +88,7 @@ def test_own_arguments(lib):
     assert call(lib, "bounds", counts=P, bounds=None) == NULL and call(lib, "bounds", counts=P, bounds=P + 4) == ALIGN
     assert call(lib, "bounds", counts=P, B=1 << 23) == SHAPE
     for kw in (dict(first=-1), dict(last=0), dict(count=2, first=2, last=1), dict(first=2147483647, last=2147483647),
-               dict(H=1024, Hkv=1), dict(B=1 << 22, Hkv=4, H=4)):
+               dict(H=1024, Hkv=1, d=64), dict(B=1 << 22, Hkv=4, H=4)):
         assert call(lib, "select", **kw) == SHAPE, kw
     for kw in (dict(count=200001), dict(count=1 << 28, page=256), dict(count=-5)):
         assert call(lib, "pages", **kw) == SHAPE, kw
