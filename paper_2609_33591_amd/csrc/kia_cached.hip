@@ -240,6 +240,18 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
 
   const int codes = D / 2 << a.lpage;
   const int64_t block = (int64_t)codes + (D / 32 << a.lpage);  // bytes of a head's block
+  // (the table's entries of a chunk are asked for a turn before its keys)
+  int entry[TILES];
+  auto ask = [&](int c) {
+    if constexpr (MODE != LISTED) {
+#pragma unroll
+      for (int i = 0; i < TILES; ++i) {
+        const int at = (work.chunks.at(min(c, c1 - 1)) + 16 * i) >> a.lpage;
+        entry[i] = entry_of(a.table, (int64_t)b * a.width + min(at, a.width - 1));
+        if (at >= a.width) entry[i] = -1;
+      }
+    }
+  };
   auto load = [&](int c, Stage4<D, VALUES> &x) {
     x.ok = 0;
 #pragma unroll
@@ -255,14 +267,13 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
         if (key > pos) page = -1;
       } else {
         key = work.chunks.at(c) + 16 * i;
-        const int at = key >> a.lpage;
-        page = at < a.width ? a.table[(int64_t)b * a.width + at] : -1;
-        page = __builtin_amdgcn_readfirstlane(page);
+        page = entry[i];
       }
       const bool ok = page >= 0 && page < a.pages;
       x.at[i] = key;
       x.ok |= ok << i;
-      load_tile<D, VALUES>(a, ok ? page : 0, hk, key & ((1 << a.lpage) - 1), codes, block, lane, i, x);
+      load_tile<D, VALUES>(a.cache + cache_block<D>(ok ? page : 0, 0, hk, a.Hkv, a.lpage), a.Hkv * block,
+                           key & ((1 << a.lpage) - 1), codes, lane, i, x);
     }
   };
 
@@ -300,9 +311,16 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
   float m = -INFINITY, l = 0.f, low = INFINITY;  // (extrema: m and low)
   Stage4<D, VALUES> cur, nxt;
   int c = c0 + wave;
-  if (c < c1) load(c, cur);
+  if (c < c1) {
+    ask(c);
+    load(c, cur);
+    ask(c + NWAVE);
+  }
   for (; c < c1; c += NWAVE) {
-    if (c + NWAVE < c1) load(c + NWAVE, nxt);
+    // (the last chunk again at the end: behind a branch, the wait for this chunk would be one for
+    // what the branch may have asked for too)
+    load(min(c + NWAVE, c1 - 1), nxt);
+    ask(c + 2 * NWAVE);
     if (MODE == LISTED && !cur.ok) {
       cur = nxt;
       continue;
@@ -648,26 +666,28 @@ template <typename TI, int D, int RT> void run(const CachedArgs &a, bool join, h
     });
   }
 }
-template <int D, int RT> void run_as(const CachedArgs &a, int dtype, bool join, hipStream_t s) {
-  // (fp32 heads of 128: two tiles do not fit the registers)
-  if (dtype == KIA_F32) run<float, D, RT == 2 && D == 128 ? 1 : RT>(a, join, s);
-  else run<uint16_t, D, RT>(a, join, s);
-}
-
 }  // namespace
+
+template <int RT> static void run_typed(const CachedArgs &a, int dtype, bool join, hipStream_t s) {
+  if (dtype == KIA_F32) run<float, KIA_HEAD, RT>(a, join, s);
+  else run<uint16_t, KIA_HEAD, RT>(a, join, s);
+}
 
 #if KIA_MODE == 0
 template <> void launch_cached<KIA_HEAD>(const CachedArgs &a, int dtype, hipStream_t s) {
-  run_as<KIA_HEAD, 0>(a, dtype, a.shares > 1, s);
+  run_typed<0>(a, dtype, a.shares > 1, s);
 }
 #elif KIA_MODE == 1
 template <> void launch_listed<KIA_HEAD>(const CachedArgs &a, int dtype, hipStream_t s) {
-  run_as<KIA_HEAD, 0>(a, dtype, a.parts > 1, s);
+  run_typed<0>(a, dtype, a.parts > 1, s);
 }
 #else
 template <> void launch_shared<KIA_HEAD>(const CachedArgs &a, int dtype, hipStream_t s) {
-  if (prefix_tiles(a.pre.tiles, KIA_HEAD, dtype) == 1) run_as<KIA_HEAD, 1>(a, dtype, true, s);
-  else run_as<KIA_HEAD, 2>(a, dtype, true, s);
+  const int rt = prefix_tiles(a.pre.tiles, KIA_HEAD, dtype);
+  if (rt == 1) run_typed<1>(a, dtype, true, s);
+  else if (dtype == KIA_BF16) run<uint16_t, KIA_HEAD, 2>(a, true, s);
+  // (fp32 heads of 128: two tiles do not fit the registers)
+  else run<float, KIA_HEAD, KIA_HEAD == 128 ? 1 : 2>(a, true, s);
 }
 #endif
 

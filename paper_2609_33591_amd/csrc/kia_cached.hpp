@@ -63,18 +63,23 @@ __device__ __forceinline__ void load_query(const TI *p, bf16x8 (&q)[NP][N], int 
   }
 }
 
-// A lane's share of tile i, tokens tok .. tok + 15 of a page (codes: bytes of a block's
-// codes, block: of all of it).
+// An entry of a table at an index that all lanes have, by a scalar load: a vector load would have
+// the loop wait for what it asked for before, the next keys among it.
+__device__ __forceinline__ int entry_of(const int *table, int64_t i) {
+  return ((const __attribute__((address_space(4))) int *)table)[i];
+}
+
+// A lane's share of tile i, tokens tok .. tok + 15 of a page, of which kp is a head's block of
+// keys and `values` bytes on that of its values (codes: bytes of a block's codes).
 template <int D, bool VALUES>
-__device__ __forceinline__ void load_tile(const CachedArgs &a, int page, int hk, int tok, int codes, int64_t block,
-                                          int lane, int i, Stage4<D, VALUES> &x) {
+__device__ __forceinline__ void load_tile(const uint8_t *kp, int64_t values, int tok, int codes, int lane, int i,
+                                          Stage4<D, VALUES> &x) {
   constexpr int N = D / 32;
   const int kb = lane >> 4, slot = lane & 15;
-  const uint8_t *kp = a.cache + cache_block<D>(page, 0, hk, a.Hkv, a.lpage);
   load_words<N>(kp + (tok + slot) * (D / 2) + kb * (D / 8), x.k[i]);
   x.ks[i] = kp[codes + (tok + slot) * (D / 32) + kb * (D / 4) / 32];
   if constexpr (VALUES) {
-    const uint8_t *vp = kp + a.Hkv * block;
+    const uint8_t *vp = kp + values;
     load_words<N>(vp + tok * (D / 2) + lane * (D / 8), x.v[i]);
     x.vs[i] = *reinterpret_cast<const uint32_t *>(vp + codes + tok * (D / 32) + kb * (D / 8) +
                                                   slot * (D / 16) / 32 * 4);

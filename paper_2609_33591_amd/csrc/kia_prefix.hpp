@@ -20,6 +20,52 @@ __device__ __forceinline__ int last_of(const CachedArgs &a, int pos) { return mi
 // LDS of a workgroup: its waves' statistics and, tile by tile, their rows.
 typedef float WaveStats[NWAVE][16][2];
 
+// A row's extrema (scaled) over the shared tokens and what lies behind them, from the first pass.
+__device__ __forceinline__ void row_extrema(const CachedArgs &a, int hk, int64_t row, int kb, float &Mx, float &Mn) {
+  const int per = a.T * (a.H / a.Hkv), b = (int)(row / per), r = (int)(row % per);
+  Mx = -INFINITY, Mn = INFINITY;
+  auto among = [&](const float *ext, int64_t first, int parts) {
+    const float2 *e = reinterpret_cast<const float2 *>(ext) + first;
+    for (int i = kb; i < parts; i += 4) {
+      const float2 y = e[16 * i];
+      Mx = fmaxf(Mx, y.x);
+      Mn = fminf(Mn, y.y);
+    }
+  };
+  among(a.pre.ext, a.pre.slot(hk, row), a.pre.parts);
+  among(a.ext, (((int64_t)hk * a.tiles + r / 16) * a.shares + (int64_t)b * a.parts) * 16 + r % 16, a.parts);
+  Mx = fmaxf(Mx, __shfl_xor(Mx, 16)), Mx = fmaxf(Mx, __shfl_xor(Mx, 32));
+  Mn = fminf(Mn, __shfl_xor(Mn, 16)), Mn = fminf(Mn, __shfl_xor(Mn, 32));
+  Mx *= a.scale, Mn *= a.scale;
+}
+
+// Weights of a row's scores of 32 keys against its running maximum m. That is moved, and the
+// sums scaled, only when passed by 2^8: where no lane sees that, no row does.
+template <int NT>
+__device__ __forceinline__ void softmax_weights(const float (&S)[TILES][4], float (&w)[TILES][4], float &m, float &sum,
+                                                f32x4 (&o)[NT], float c2) {
+  float top = S[0][0];
+#pragma unroll
+  for (int i = 0; i < TILES; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = fmaxf(top, S[i][e]);
+  if (__any((top - m) * c2 > 8.f)) {
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const bool up = (top - m) * c2 > 8.f;
+    const float f = up ? __builtin_amdgcn_exp2f((m - top) * c2) : 1.f;
+    m = up ? top : m;
+    sum *= f;
+#pragma unroll
+    for (int y = 0; y < NT; ++y) o[y] *= f;
+  }
+  const float mm = m == -INFINITY ? 0.f : m * c2;
+#pragma unroll
+  for (int i = 0; i < TILES; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[i][e] = __builtin_amdgcn_exp2f(fmaf(S[i][e], c2, -mm));
+}
+
 template <typename TI, int D, int PASS, int CALIB, int RECON, int RT>
 __device__ __forceinline__ void prefix_part(const CachedArgs &a, WaveStats *red, float *rows) {
   constexpr int NP = Pieces<TI>::N, N = D / 32, NT = D / 16;
@@ -56,17 +102,24 @@ __device__ __forceinline__ void prefix_part(const CachedArgs &a, WaveStats *red,
   const int c1 = min(seen, (int)((int64_t)chunks * (part + 1) / a.pre.parts));
 
   const int codes = D / 2 << a.lpage;
-  const int64_t block = (int64_t)codes + (D / 32 << a.lpage);
+  const int64_t block = (int64_t)codes + (D / 32 << a.lpage), stride = 2 * a.Hkv * block;
+  const uint8_t *head = a.cache + hk * block;
+  // (the table's entries of a chunk are asked for a turn before its keys)
+  int entry[TILES];
+  auto ask = [&](int c) {
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) entry[i] = entry_of(a.table, (min(c, c1 - 1) * CHUNK + 16 * i) >> a.lpage);
+  };
   auto load = [&](int c, Stage4<D, VALUES> &x) {
     x.ok = 0;
 #pragma unroll
     for (int i = 0; i < TILES; ++i) {
       const int key = c * CHUNK + 16 * i;
-      const int page = __builtin_amdgcn_readfirstlane(a.table[key >> a.lpage]);
+      const int page = entry[i];
       const bool ok = page >= 0 && page < a.pages;
       x.at[i] = key;
       x.ok |= ok << i;
-      load_tile<D, VALUES>(a, ok ? page : 0, hk, key & ((1 << a.lpage) - 1), codes, block, lane, i, x);
+      load_tile<D, VALUES>(head + (ok ? page : 0) * stride, a.Hkv * block, key & ((1 << a.lpage) - 1), codes, lane, i, x);
     }
   };
 
@@ -75,24 +128,7 @@ __device__ __forceinline__ void prefix_part(const CachedArgs &a, WaveStats *red,
   if constexpr (PASS == PASS_GRID) {
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
-      const int64_t row = min((int64_t)(tile0 + x) * 16 + slot, total - 1);
-      const int b = (int)(row / per), r = (int)(row % per);
-      Mx[x] = -INFINITY, Mn[x] = INFINITY;
-      auto among = [&](const float *ext, int64_t first, int parts) {
-        const float2 *e = reinterpret_cast<const float2 *>(ext) + first;
-        for (int i = kb; i < parts; i += 4) {
-          const float2 y = e[16 * i];
-          Mx[x] = fmaxf(Mx[x], y.x);
-          Mn[x] = fminf(Mn[x], y.y);
-        }
-      };
-      among(a.pre.ext, a.pre.slot(hk, row), a.pre.parts);
-      among(a.ext, (((int64_t)hk * a.tiles + r / 16) * a.shares + (int64_t)b * a.parts) * 16 + r % 16, a.parts);
-      Mx[x] = fmaxf(Mx[x], __shfl_xor(Mx[x], 16));
-      Mx[x] = fmaxf(Mx[x], __shfl_xor(Mx[x], 32));
-      Mn[x] = fminf(Mn[x], __shfl_xor(Mn[x], 16));
-      Mn[x] = fminf(Mn[x], __shfl_xor(Mn[x], 32));
-      Mx[x] *= a.scale, Mn[x] *= a.scale;
+      row_extrema(a, hk, min((int64_t)(tile0 + x) * 16 + slot, total - 1), kb, Mx[x], Mn[x]);
       rc[x] = row_const(Mx[x], Mn[x], a.K, CALIB, a.tau, a.scale);
     }
   }
@@ -104,9 +140,16 @@ __device__ __forceinline__ void prefix_part(const CachedArgs &a, WaveStats *red,
   for (int x = 0; x < RT; ++x) m[x] = -INFINITY, l[x] = 0.f, low[x] = INFINITY;
   Stage4<D, VALUES> cur, nxt;
   int c = c0 + wave;
-  if (c < c1) load(c, cur);
+  if (c < c1) {
+    ask(c);
+    load(c, cur);
+    ask(c + NWAVE);
+  }
   for (; c < c1; c += NWAVE) {
-    if (c + NWAVE < c1) load(c + NWAVE, nxt);
+    // (the last chunk again at the end: behind a branch, the wait for this chunk would be one for
+    // what the branch may have asked for too)
+    load(min(c + NWAVE, c1 - 1), nxt);
+    ask(c + 2 * NWAVE);
     const int j = cur.at[0];
     const bool all = j + CHUNK - 1 <= lo && cur.ok == (1 << TILES) - 1;
     auto sees = [&](int x, int i, int e) { return j + 16 * i + 4 * kb + e <= last[x] && (cur.ok >> i & 1); };
@@ -169,28 +212,7 @@ __device__ __forceinline__ void prefix_part(const CachedArgs &a, WaveStats *red,
       for (int x = 0; x < RT; ++x) {
         float w[TILES][4];
         if constexpr (PASS == PASS_SOFTMAX) {
-          float top = S[x][0][0];
-#pragma unroll
-          for (int i = 0; i < TILES; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) top = fmaxf(top, S[x][i][e]);
-          // (moved, and the sums scaled, only when passed by 2^8: where no lane sees that, no row
-          // does)
-          if (__any((top - m[x]) * c2 > 8.f)) {
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const bool up = (top - m[x]) * c2 > 8.f;
-            const float f = up ? __builtin_amdgcn_exp2f((m[x] - top) * c2) : 1.f;
-            m[x] = up ? top : m[x];
-            l[x] *= f;
-#pragma unroll
-            for (int y = 0; y < NT; ++y) o[x][y] *= f;
-          }
-          const float mm = m[x] == -INFINITY ? 0.f : m[x] * c2;
-#pragma unroll
-          for (int i = 0; i < TILES; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[i][e] = __builtin_amdgcn_exp2f(fmaf(S[x][i][e], c2, -mm));
+          softmax_weights<NT>(S[x], w, m[x], l[x], o[x], c2);
         } else {
           grid_weights<CALIB, RECON, 4>(S[x], w, rc[x], Mx[x], Mn[x], a);
           if (!all) {

@@ -200,13 +200,18 @@ int shared_shape(CachedArgs &a, int page, int width, int B, int H, int Hkv, int 
   a.shared = shared;
   const int G = H / Hkv;
   a.tiles = (T * G + 15) / 16;
-  const int64_t groups = (int64_t)B * Hkv * a.tiles, own = keys - shared;
-  a.parts = (int)std::max<int64_t>(1, std::min<int64_t>({resident(dtype) / groups, (own + 255) / 256, 64}));
+  // Two workgroups a CU run at once: those over the shared tokens get their part of the work's
+  // worth of that (a chunk of two row tiles costs 1.6 times one of one), half of it at least
+  // (64 sequences behind 8192 tokens, 1000 of their own at most: with all of it 29.5 us, so 25).
+  const int64_t groups = (int64_t)B * Hkv * a.tiles, own = keys - shared, cus = host_cus();
+  a.parts = (int)std::max<int64_t>(1, std::min<int64_t>({2 * cus / groups, (own + 255) / 256, 64}));
   a.pre.tiles = (int)(((int64_t)B * T * G + 15) / 16);
   const int rt = prefix_tiles(a.pre.tiles, d, dtype);
   const int64_t blocks = (int64_t)Hkv * ((a.pre.tiles + rt - 1) / rt);
+  const double work = 0.8 * Hkv * a.pre.tiles * shared, rest = (double)groups * own;
+  const int64_t slots = (int64_t)(2.0 * cus * std::max(0.5, work / (work + rest)));
   a.pre.parts = (int)std::max<int64_t>(
-      1, std::min<int64_t>({2 * (int64_t)host_cus() / blocks, ((int64_t)shared + 127) / 128, 128}));
+      1, std::min<int64_t>({(slots + blocks / 2) / blocks, ((int64_t)shared + 127) / 128, 128}));
   if (too_many((double)groups * a.parts + (double)blocks * a.pre.parts)) return KIA_ERR_SHAPE;
   a.pre.blocks = (unsigned)(blocks * a.pre.parts);
   a.shares = B * a.parts;

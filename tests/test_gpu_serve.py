@@ -201,6 +201,43 @@ def test_shared_many_rows(op, dtype):
     check_shared(draw((B, 3, 3, 128), dtype, 104), cache, table, k, v, lengths, shared, **op)
 
 
+@pytest.mark.parametrize("op", OPS, ids=name)
+@pytest.mark.parametrize("d,page,shared", ((128, 64, 512), (64, 16, 288), (32, 256, 256)))
+def test_shared_rows_of_many_tiles(op, d, page, shared):
+    """Tiles of rows that no sequence fills, texts that end within the shared tokens, keys and
+    values of NaN and entries of no page among them."""
+    B = 60
+    lengths = tuple((shared + (7 * b) % 90, 5 * b, shared, 0)[0 if b % 4 else b // 4 % 4] for b in range(B))
+    cache, table, _, k, v = filled((shared + 90,) * B, 1, d, page, torch.bfloat16, 150, 0.7, shared)
+    q = draw((B, 3, 3, d), torch.bfloat16, 154)
+    o = check_shared(q, cache, table, k, v, lengths, shared, **op)
+    # a NaN key and a NaN value of the shared tokens reach the rows that see them, a NaN value
+    # its own channels
+    clean = cache.data.clone()
+    pos = torch.tensor(lengths, device="cuda")[:, None] - 3 + torch.arange(3, device="cuda")
+    for at in (9, shared - 20):
+        hit = (pos >= at)[:, None].expand(B, 3, 3)
+        for which in (0, 1):
+            x = [y.clone() for y in kia.cache4_read(cache, table[:1], ints(at), 1, torch.bfloat16)]
+            x[which][0, 0, 0, d - 3] = math.nan
+            kia.cache4_write(*x, cache, table[:1], ints(at))
+            y = kia.cache4_attention(q, cache, table, ints(*lengths), shared=shared, **op)
+            assert torch.equal(y[~hit], o[~hit])
+            some = slice(0, d) if which == 0 else slice(d - 32, d)
+            assert bool(torch.isnan(y[hit][:, some]).all())
+            assert which == 0 or torch.equal(y[hit][:, :d - 32], o[hit][:, :d - 32])
+            cache.data.copy_(clean)
+    # entries of no page are not seen
+    if d == 64:
+        bad = table.clone()
+        bad[0, 3] = cache.pages
+        y = kia.cache4_attention(q, cache, bad, ints(*lengths), shared=shared, **op)
+        keep = torch.arange(shared + 90, device="cuda") // page != 3
+        for b in (1, 2, 17):
+            at = keep[:lengths[b]].nonzero()[:, 0]
+            ref.within(y[b], *ref.cached(q[b], k[b][:, at], v[b][:, at], len(at), **{**FULL, **op}), "no page")
+
+
 def test_shared_is_the_first_rows():
     """Only the first sequence's entries are looked at for the shared tokens, and all of a
     table may be shared."""
