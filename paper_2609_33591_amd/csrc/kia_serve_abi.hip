@@ -161,9 +161,9 @@ int check_sizes(CachedArgs &a, int page, int width, int B, int H, int Hkv, int T
   return KIA_OK;
 }
 
-// Extrema, maxima and sums, and rows of `n` parts' rows, from `at` on.
+// Extrema, maxima and sums, and rows of `n` parts' rows, from `at` on (ws nullptr: their size).
 size_t lay(size_t at, size_t n, int d, float *ws, float *&ext, float *&stat, float *&part) {
-  ext = ws + at, stat = ext + 2 * n, part = stat + 2 * n;
+  if (ws) ext = ws + at, stat = ext + 2 * n, part = stat + 2 * n;
   return at + (4 + (size_t)d) * n;
 }
 

@@ -66,6 +66,37 @@ def test_append(dtype, d, rot, layout, page):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d,page", ((32, 16), (64, 256), (128, 128), (128, 32)))
+def test_prompts_over_pages(dtype, d, page):
+    """Prompts over several pages, whole and begun, of one head and of many; a NaN in a key makes
+    its group's bounds NaN, in that page alone."""
+    B, H, Hkv, T = 2, 9, 5, 600
+    starts = [page + 3, 0]
+    table, pages = table_of([s + T for s in starts], page, 17)
+    cache, plan = kia.new_cache4(pages, Hkv, page, d), kia.rotary_plan(d)
+    old = draw((B, Hkv, max(starts), d), dtype, 31)
+    kia.cache4_write(old, old, cache, table, ints(0, 0), ints(*starts))
+    q, k, v = (draw((B, h, T, d), dtype, 32 + i) for i, h in enumerate((H, Hkv, Hkv)))
+    k[1, 2, 333, 7] = math.nan
+    bounds = kia.new_bounds4(cache)
+    out = kia.cache4_append(q, k, v, cache, table, ints(*starts), plan, bounds=bounds)
+    ref.within(out, *turned(q, plan, starts), "q")
+    held = ref.held(turned(k, plan, starts)[0])
+    got = kia.cache4_read(cache, table, ints(*starts), T, torch.float32)
+    assert torch.equal(got[0].double().nan_to_num(9e99), held.nan_to_num(9e99))
+    assert torch.equal(got[1].double(), ref.held(v))
+    for b, s in enumerate(starts):
+        every = torch.cat((ref.held(old)[b, :, :s], held[b]), 1)
+        for w in range(s // page, (s + T - 1) // page + 1):
+            want = bounds_of(every, s + T, page, w)
+            assert torch.equal(bounds[table[b, w]].double().nan_to_num(9e99), want.nan_to_num(9e99))
+    # the same from what the cache holds
+    again = kia.new_bounds4(cache)
+    kia.cache4_bounds(cache, again, table, ints(*starts), ints(*(s + T for s in starts)))
+    assert torch.equal(again.float().nan_to_num(9e9), bounds.float().nan_to_num(9e9))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("layout", ("half", "interleaved"))
 def test_keys_at_borders(dtype, layout):
     """A key at position 0 is held as it is: every midpoint and level on either side, least

@@ -260,6 +260,49 @@ def test_shared_is_the_first_rows():
 
 
 # ---- both ------------------------------------------------------------------------------
+@pytest.mark.parametrize("op", (OPS[0], OPS[2]), ids=name)
+def test_many_rows_of_few_parts(op):
+    """Rows whose parts are joined many to a workgroup."""
+    page, d, n = 16, 32, 1000
+    cache, table, bounds, k, v = filled((n,) * 16, 1, d, page, torch.bfloat16, 160, 0.7)
+    q = draw((16, 128, 1, d), torch.bfloat16, 164)
+    pages = kia.cache4_select(q, cache, bounds, table, ints(*[n] * 16), 60)
+    o = kia.cache4_attention(q, cache, table, ints(*[n] * 16), pages=pages, **op)
+    for b in range(16):
+        want = over_pages(q[b], k[b], v[b], n, page, pages[b].tolist(), **{**FULL, **op})
+        ref.within(o[b], *want, f"sequence {b}")
+    B, shared = 128, 512
+    lengths = tuple(shared + b % 50 for b in range(B))
+    cache, table, _, k, v = filled(lengths, 2, d, page, torch.bfloat16, 170, 0.7, shared)
+    check_shared(draw((B, 32, 1, d), torch.bfloat16, 174), cache, table, k, v, lengths, shared, **op)
+
+
+def test_past_four_gigabytes():
+    """Pages, bounds and lists at the end of a cache of 4.4 GB."""
+    page, d, Hkv, pages = 256, 128, 8, 15_800
+    data = torch.empty(pages, 2, Hkv, page * (d // 2 + d // 32), dtype=torch.uint8, device="cuda")
+    cache = kia.Cache4(data, d)
+    bounds = torch.empty(pages, Hkv, 2, d, dtype=torch.bfloat16, device="cuda")
+    table = torch.arange(pages - 1, pages - 9, -1, dtype=torch.int32, device="cuda").view(2, 4)
+    table[1, 0] = table[0, 0]  # a shared first page
+    n, T = 4 * page - 5, 4 * page - 5
+    k, v = draw((2, Hkv, T, d), torch.bfloat16, 1, 0.7), draw((2, Hkv, T, d), torch.bfloat16, 2)
+    k[1, :, :page], v[1, :, :page] = k[0, :, :page], v[0, :, :page]
+    plan = kia.RotaryPlan(torch.zeros(d // 2, dtype=torch.float64, device="cuda"))  # turns nothing
+    x = kia.cache4_append(k[1:], k[1:], v[1:], cache, table[1:].contiguous(), ints(0), plan, bounds=bounds)
+    x = kia.cache4_append(k[:1], k[:1], v[:1], cache, table[:1].contiguous(), ints(0), plan, bounds=bounds)
+    assert torch.equal(x, k[:1])
+    q, lens, hk, hv = draw((2, 16, 1, d), torch.bfloat16, 3), ints(n, n), ref.held(k), ref.held(v)
+    got = kia.cache4_select(q, cache, bounds, table, lens, 3)
+    o = kia.cache4_attention(q, cache, table, lens, pages=got, recon="softmax")
+    y = kia.cache4_attention(q, cache, table, lens, shared=page, recon="softmax")
+    for b in range(2):
+        want = select(q[b], by_table(bounds, table[b]), table[b].tolist(), n, page, pages, 3, 1, 1)
+        assert got[b].tolist() == want
+        ref.within(o[b], *over_pages(q[b], hk[b], hv[b], n, page, want, recon="softmax"), "pages")
+        ref.within(y[b], *ref.cached(q[b], hk[b], hv[b], n, recon="softmax"), "shared")
+
+
 def calls(cache, table, bounds, n, T, H, d, dtype, seed, op, shared):
     q = draw((table.shape[0], H, T, d), dtype, seed)
     pages = torch.arange(table.shape[1], dtype=torch.int32, device="cuda").expand(
