@@ -347,7 +347,7 @@ __global__ __launch_bounds__(Threads<D>::N, 4) void append_kernel(AppendArgs a) 
   __shared__ __attribute__((aligned(16))) BoundsLds<D> lds;
   __shared__ Again<D> again;
   __shared__ int held_on[4];  // pages of the 64 positions (or -1)
-  extern __shared__ __attribute__((aligned(16))) float2 turn[];  // [64][table.size()]
+  extern __shared__ __attribute__((aligned(16))) float2 turns_of[];  // [min(T, 64)][table.size()]
   const CacheArgs &c = a.c;
   const int tid = threadIdx.x, oct = tid % OCTS, t0 = tid / OCTS, n = a.rot / 2;
   const Table<MODE> table(n);
@@ -383,10 +383,11 @@ __global__ __launch_bounds__(Threads<D>::N, 4) void append_kernel(AppendArgs a) 
         const int t = s.lo + e / n, m = e % n;
         float sn, cs;
         turn_of((double)(s.base + t), a.freq[m], sn, cs);
-        turn[t * table.size() + table.at(m)] = make_float2(cs * a.factor, sn * a.factor);
+        turns_of[(t - s.lo) * table.size() + table.at(m)] = make_float2(cs * a.factor, sn * a.factor);
       }
     }
     __syncthreads();
+    auto turn_at = [&](int t, bool in) { return turns_of + (in ? t - s.lo : 0) * table.size(); };
     if (kind == 2) {
       TI *out[REP];
 #pragma unroll
@@ -401,7 +402,7 @@ __global__ __launch_bounds__(Threads<D>::N, 4) void append_kernel(AppendArgs a) 
           Chunk x;
           pairs_of<TI, MODE>(raw, rows.in[r] ? row : nullptr, oct, n, x);
           float z[8];
-          turned<MODE>(x, turn + (t0 + r * TOKENS) * table.size(), oct, n, z);
+          turned<MODE>(x, turn_at(t0 + r * TOKENS, rows.in[r]), oct, n, z);
           if (rows.in[r]) store8(out[r], z);
           out[r] += by * a.qo.sh;
         }
@@ -461,7 +462,7 @@ __global__ __launch_bounds__(Threads<D>::N, 4) void append_kernel(AppendArgs a) 
         Chunk x;
         pairs_of<TI, MODE>(raw, rows.in[r] ? row : nullptr, oct, n, x);
         uint32_t w, sc;
-        const bool open = quantise_turned<MODE>(x, turn + (rows.in[r] ? t : s.lo) * table.size(), oct, n, a.factor, w, sc);
+        const bool open = quantise_turned<MODE>(x, turn_at(t, rows.in[r]), oct, n, a.factor, w, sc);
         const bool live = rows.in[r] && at[r];
         // a group goes again if one of its four lanes asks for it
         if (__ballot(open && live) >> (tid & 60) & 15) {
@@ -533,7 +534,7 @@ template <int D> __global__ __launch_bounds__(Threads<D>::N) void bounds_kernel(
 }
 
 template <typename TI, int D, int MODE> void append_mode(const AppendArgs &a, dim3 grid, hipStream_t s) {
-  const size_t lds = (size_t)SUB * Table<MODE>(a.rot / 2).size() * sizeof(float2);
+  const size_t lds = (size_t)std::min(a.c.T, SUB) * Table<MODE>(a.rot / 2).size() * sizeof(float2);
   hipLaunchKernelGGL((append_kernel<TI, D, MODE>), grid, dim3(Threads<D>::N), lds, s, a);
 }
 template <typename TI, int D> void append_as(const AppendArgs &a, dim3 grid, hipStream_t s) {
