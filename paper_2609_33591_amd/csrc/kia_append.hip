@@ -7,7 +7,11 @@
 // its heads; sine and cosine of its tokens go to LDS once for all of them. Spans start at
 // multiples of their size, so that the tokens of a page are one workgroup's, and the bounds
 // need no atomics and no second pass: the held values of the page's tokens go to LDS, the
-// earlier ones read back from the page.
+// earlier ones read back from the page. 4 prompts of 2048 tokens, 16
+// heads of 128 for queries and keys, bf16, with bounds: 47 us for 152 MB, 3.3 TB/s of the 5.1
+// that a copy reaches; rotating, finding codes and bounds takes 19 million wave instructions, two
+// thirds of what the vector units can issue in that time. A token each of 32 sequences, 16 heads
+// of 128 over 4: 10 us, loads of the length, page, keys and earlier tokens one after another.
 //
 // A rotated key is rounded once, to its 4 bits. The rotation in 32 bits is off by up to
 // 2^-21 of the pair's magnitudes, which decides another code for about one value in 10^7: where
@@ -154,7 +158,7 @@ __device__ __forceinline__ void pairs_of(const Raw<TI> &own, const TI *row, int 
 
 // Where a token's table holds a pair's cosine and sine: those of a chunk in pairs of pairs,
 // the chunks' first ones side by side, so that neighbouring lanes read neighbouring 16 bytes
-// (in order, they met in a quarter of the banks: 67 us for the prompts below).
+// (in order, they met in a quarter of the banks: 67 us for the prompts above).
 template <int MODE> struct Table {
   static constexpr int OF = MODE == HALF8 ? 8 : 4;  // pairs of a chunk
   int chunks;
@@ -550,7 +554,9 @@ template <int D> void append_d(const AppendArgs &a, dim3 grid, int dtype, hipStr
 }  // namespace
 
 // Workgroups: the spans of 64 positions (or a page), and of each span's heads as many shares
-// as it takes to reach `per CU` of them; keys, values and queries have shares of their own.
+// as make four workgroups a CU (the prompts above with three / four / six / eight / twelve: 49 /
+// 47 / 51 / 58 / 66 us, as more of them compute the same angles); keys, values and queries have
+// shares of their own.
 void launch_append(AppendArgs a, int d, int dtype, int cus, hipStream_t s) {
   const unsigned spans = (unsigned)a.c.B * a.spans;
   const int want = (int)std::max(1u, (4u * cus + spans - 1) / spans), all = 2 * a.c.Hkv + a.H;

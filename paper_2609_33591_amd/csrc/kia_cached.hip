@@ -18,13 +18,15 @@
 // Softmax runs in one pass with a running maximum. The interval weights' grid
 // depends on the row's extrema, so a first pass over the keys alone (a third of the
 // bytes) finds them; the weights are absolute then and the parts' sums just add.
-// 32 sequences of up to 32 000 keys, 16 heads of 128 over 4, LERP: extrema 35 us (144 MB,
-// 4.2 TB/s), weights 74 us (289 MB, 3.9 TB/s), join 6; Nearest takes as long.
+// 32 sequences of up to 32 000 keys, 16 heads of 128 over 4, LERP: extrema 32 us (144 MB,
+// 4.5 TB/s), weights 63 us (289 MB, 4.6 TB/s), join 6; Nearest takes as long, softmax 60 and 6.
+// (While a tile's loads stood behind branches and the page's number came by vector loads, each
+// wait was for all of them: 35 and 74 us.)
 //
 // bf16 queries: scores are sums of exact products, weights are rounded to bf16 (2^-8
 // of each) for the product with V: an output's error is up to 1.4 times that of its own
-// rounding (2-norm; with weights in two pieces 1.0 times, and their pass takes 6 to 8%
-// longer: 76 -> 81 us above, the softmax of kia_around_abi.hip's figures 59 -> 63). fp32
+// rounding (2-norm; with weights in two pieces 1.0 times, and their pass took 6 to 8%
+// longer). fp32
 // queries and weights go as three bf16 pieces (exact for 2^-100 to 2^126; smaller ones lose
 // less than 2^-133), which the idle matrix unit takes for free. Sums, extrema and
 // statistics are fp32.
@@ -97,7 +99,7 @@ struct Rows16 {
 // The parts that the sequences' keys are cut into for one key head's row tile: about
 // a.shares in all, of one size for every sequence, so that a batch of unequal lengths
 // keeps all workgroups busy for the same time (32 000 keys to 1 000, 32 sequences:
-// 158 us with eight parts for each, 134 us so). Every sequence has one at least. Part w of
+// 18% longer with eight parts for each). Every sequence has one at least. Part w of
 // all of them is part w - first of sequence b. (64 sequences at a time; at most
 // a.shares + B parts in all.)
 struct Share {
@@ -181,10 +183,10 @@ struct Work {
 // FEW: a key head has at most four rows. The 16 columns then hold them four times over, and
 // of the four keys that a lane has scores of it takes one's weight, the (l / 4)-th: a
 // quarter of the work on weights. The interval weights are bound by that work: LERP over
-// the 32 sequences above 86 -> 76 us; 32 sequences of 16 000 keys, 32 heads of 128 over 8,
-// Nearest with MinMax 124 -> 107 and its extrema 73 -> 65. The softmax, whose maximum then
-// crosses more lanes, is not (118 and 119 us there), nor are extrema without the minimum
-// (16 of those sequences in fp32: 40 -> 45 us).
+// the 32 sequences above 76 -> 63 us; 32 sequences of 16 000 keys, 32 heads of 128 over 8,
+// Nearest 117 -> 101. The softmax, whose maximum then crosses more lanes, gains nothing to
+// speak of (103 and 101 us there), and extrema without the minimum lose by it (16 of those
+// sequences in fp32: 40 -> 45 us).
 // RT: row tiles of a wave over shared tokens (0: there are none).
 template <typename TI, int D, int PASS, int CALIB, int RECON, bool FEW, int RT>
 __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
@@ -397,11 +399,11 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
         for (int i = 0; i < TILES; ++i)
 #pragma unroll
           for (int e = 0; e < NE; ++e) top = fmaxf(top, S[i][e]);
-        top = across<FEW>(top, [](float x, float y) { return fmaxf(x, y); });
         // (moved, and the sums scaled, only when passed by 2^8, row by row: no row's bits
-        // depend on another's)
-        const bool up = (top - m) * c2 > 8.f;
-        if (__any(up)) {
+        // depend on another's. Where no lane sees that, no row does)
+        if (__any((top - m) * c2 > 8.f)) {
+          top = across<FEW>(top, [](float x, float y) { return fmaxf(x, y); });
+          const bool up = (top - m) * c2 > 8.f;
           const float f = up ? __builtin_amdgcn_exp2f((m - top) * c2) : 1.f;
           m = up ? top : m;
           l *= f;

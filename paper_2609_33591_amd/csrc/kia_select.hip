@@ -7,16 +7,18 @@
 // pages are ranked in 64 bits: of bf16 queries the terms and nearly every sum are exact there,
 // so that the order depends on no order of summation.
 //
-// Sums in 64 bits for all pages would take three times as long as reading the bounds. The
-// matrix unit finds them within an error E first (16 pages by 16 heads, bf16 operands,
-// fp32 queries as three pieces), and the count-th largest, c, digit by digit of its bits.
-// An approximate rank above c + 2 E is one of the count largest for certain, one
-// below c - 2 E is none; only what lies between is summed in 64 bits and chosen from. E is
-// 2^-13 of the largest page's sum of magnitudes, eight times what 256 roundings to 24 bits can
-// add up to; magnitudes below 2^-96 count as that, for what the matrix unit may flush.
-// 500 pages of 32 sequences, four heads of 128 a key head (33 MB of bounds): @@ us; 64-bit sums for all
-// took 22.
-//
+// Sums in 64 bits for all pages would take longer than reading the bounds. The matrix unit
+// finds them within an error E first (16 pages by 16 heads, bf16 operands, fp32 queries as
+// three pieces), and the count-th largest, c, digit by digit of its bits. An approximate rank
+// above c + 2 E is one of the count largest for certain, one below c - 2 E is none; only what
+// lies between is summed in 64 bits and chosen from. E is 2^-13 of the largest page's sum of
+// magnitudes: 2 D <= 256 products of bf16 queries, each rounded to 24 bits in the sum, add up
+// to an eighth of that (three pieces: 768, to three eighths); magnitudes below 2^-96 count as
+// that, for what the matrix unit may flush.
+// 500 pages of 32 sequences, 16 heads of 128 over 4 (33 MB of bounds), bf16: ranks 9.9 us
+// (3.3 TB/s), the cut and the list 8.3; with 64-bit sums for all 12.3 and 6.2. One token of 12
+// heads of 64 over 63 pages, one launch: 8.3; in two of 64-bit sums 9.
+
 // A workgroup selects for a token and key head. Where it can rank all of its pages soon
 // enough, it does that itself; else a launch before ranks them in batches.
 #include "kia_around.hpp"
