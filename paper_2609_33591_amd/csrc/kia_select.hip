@@ -15,10 +15,10 @@
 // magnitudes: 2 D <= 256 products of bf16 queries, each rounded to 24 bits in the sum, add up
 // to an eighth of that (three pieces: 768, to three eighths); magnitudes below 2^-96 count as
 // that, for what the matrix unit may flush.
-// 500 pages of 32 sequences, 16 heads of 128 over 4 (33 MB of bounds), bf16: ranks 9.9 us
-// (3.3 TB/s), the cut and the list 8.3; with 64-bit sums for all 12.3 and 6.2. One token of 12
-// heads of 64 over 63 pages, one launch: 8.3; in two of 64-bit sums 9.
-
+// Up to 500 pages of 32 sequences, 16 heads of 128 over 4 (17 MB of bounds), bf16: ranks 9.1 us,
+// the cut and the list 7.8, both mostly loads that wait for each other; with 64-bit sums for all
+// 12.3 and 6.2. One token of 12 heads of 64 over 63 pages, one launch: 8.4.
+//
 // A workgroup selects for a token and key head. Where it can rank all of its pages soon
 // enough, it does that itself; else a launch before ranks them in batches.
 #include "kia_around.hpp"
