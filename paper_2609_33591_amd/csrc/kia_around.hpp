@@ -137,7 +137,7 @@ struct Prefix {
   float *ext, *stat, *part;  // as CachedArgs'
   int tiles, parts;
   unsigned blocks;  // workgroups
-  __host__ __device__ int64_t slot(int hk, int64_t row) const {
+  __host__ __device__ int64_t slot(int hk, unsigned row) const {
     return (((int64_t)hk * tiles + row / 16) * parts) * 16 + row % 16;
   }
 };

@@ -86,10 +86,10 @@ struct Chunks {
 struct Rows16 {
   int n, lo, hi;  // n: the sequence's keys
   __device__ __forceinline__ Rows16(const CachedArgs &a, int b, int tile) {
-    const int G = a.H / a.Hkv, total = a.T * G;
+    const unsigned G = (unsigned)a.H / (unsigned)a.Hkv, total = a.T * G;
     n = (int)min((int64_t)max(a.lengths[b], 0), (int64_t)a.width << a.lpage);
-    lo = n - a.T + tile * 16 / G;
-    hi = n - a.T + min(tile * 16 + 15, total - 1) / G;
+    lo = n - a.T + (int)(tile * 16u / G);
+    hi = n - a.T + (int)(min(tile * 16u + 15, total - 1) / G);
   }
   __device__ __forceinline__ Chunks chunks(const CachedArgs &a) const {
     return Chunks(a, max(lo, 0), hi);
@@ -149,20 +149,21 @@ struct Work {
   int b, t0, rows, n, lo, hi, first, parts, c0, c1;
   Chunks chunks;
   __device__ __forceinline__ Work(const CachedArgs &a, int tile, int w) {
-    const int G = a.H / a.Hkv;
+    const int G = (unsigned)a.H / (unsigned)a.Hkv;
     if constexpr (MODE == SEQUENCE) {
       const Share share(a, tile, w, false);
       b = share.b, first = share.first, parts = share.parts;
       if (b < 0) return;
     } else {
       // (as many parts for every sequence, or for every token of one)
-      parts = a.parts, first = w / parts * parts;
-      b = MODE == LISTED ? w / parts / a.T : w / parts;
+      const unsigned id = (unsigned)w / (unsigned)a.parts;
+      parts = a.parts, first = id * parts;
+      b = MODE == LISTED ? id / (unsigned)a.T : id;
     }
     const Rows16 rows16(a, b, tile);
     n = rows16.n;
     if constexpr (MODE == LISTED) {
-      t0 = w / parts % a.T, rows = G;
+      t0 = first / parts - b * a.T, rows = G;
       lo = hi = n - a.T + t0;
       // (before the text too, so that the list need not wait for the length)
       chunks.count = (int)((((int64_t)a.count << a.lpage) + CHUNK - 1) / CHUNK);
@@ -175,8 +176,8 @@ struct Work {
         chunks.count = max(0, chunks.count - chunks.low);
       }
     }
-    c0 = (int)((int64_t)chunks.count * (w - first) / parts);
-    c1 = (int)((int64_t)chunks.count * (w - first + 1) / parts);
+    c0 = share_of(chunks.count, w - first, parts);
+    c1 = share_of(chunks.count, w - first + 1, parts);
   }
 };
 
@@ -209,13 +210,14 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
     }
     block_id -= a.pre.blocks;
   }
-  const int hk = block_id % a.Hkv, tile = (int)(block_id / a.Hkv) % a.tiles;
-  const int w = block_id / (a.Hkv * a.tiles);
+  const unsigned pair = block_id / (unsigned)a.Hkv;
+  const int hk = block_id % (unsigned)a.Hkv, tile = pair % (unsigned)a.tiles, w = pair / (unsigned)a.tiles;
   const Work work(a, tile, w);
   if (work.b < 0) return;
-  const int b = work.b, G = a.H / a.Hkv, total = work.rows, lo = work.lo, hi = work.hi;
+  const int b = work.b, G = (unsigned)a.H / (unsigned)a.Hkv, total = work.rows, lo = work.lo, hi = work.hi;
   // this lane's row, and its position (-1 or less: before the text, sees nothing)
-  const int r = min(tile * 16 + col, total - 1), t = work.t0 + r / G, h = hk * G + r % G;
+  const unsigned r = min(tile * 16 + col, total - 1);
+  const int t = work.t0 + r / (unsigned)G, h = hk * G + r % (unsigned)G;
   const int pos = work.n - a.T + t;
   const int c0 = work.c0, c1 = work.c1;
 
@@ -254,7 +256,9 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
       }
     }
   };
+  Offsets<D> where(lane);
   auto load = [&](int c, Stage4<D, VALUES> &x) {
+    where.hold();
     x.ok = 0;
 #pragma unroll
     for (int i = 0; i < TILES; ++i) {
@@ -275,7 +279,7 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
       x.at[i] = key;
       x.ok |= ok << i;
       load_tile<D, VALUES>(a.cache + cache_block<D>(ok ? page : 0, 0, hk, a.Hkv, a.lpage), a.Hkv * block,
-                           key & ((1 << a.lpage) - 1), codes, lane, i, x);
+                           key & ((1 << a.lpage) - 1), codes, where, i, x);
     }
   };
 
@@ -562,8 +566,9 @@ template <typename TI, int D> __global__ __launch_bounds__(256) void join_kernel
   constexpr int W = D / 4, NG = 256 / W;
   __shared__ float f[256], red[8];  // (at most 256 parts)
   __shared__ f32x4 sums[NG][W];
-  const int kvs = a.B * a.Hkv, s = blockIdx.x % kvs, b = s / a.Hkv, hk = s % a.Hkv;
-  const int G = a.H / a.Hkv, r = blockIdx.x / kvs, tid = threadIdx.x, wave = tid >> 6;  // r: token and head
+  const unsigned kvs = a.B * a.Hkv, s = blockIdx.x % kvs, b = s / (unsigned)a.Hkv, hk = s % (unsigned)a.Hkv;
+  const unsigned G = (unsigned)a.H / (unsigned)a.Hkv, r = blockIdx.x / kvs;  // r: token and head
+  const int tid = threadIdx.x, wave = tid >> 6;
   int64_t first, before = 0;
   int parts, shared = 0;  // parts over the shared tokens, then the row's own
   if constexpr (MODE == SEQUENCE) {
@@ -631,18 +636,18 @@ template <typename TI, int D> __global__ __launch_bounds__(256) void join_kernel
 constexpr int FEW_PARTS = 8, MANY_ROWS = 2048;
 template <typename TI, int D> __global__ __launch_bounds__(256) void join_few_kernel(CachedArgs a) {
   constexpr int W = D / 4, ROWS = 256 / W;
-  const int G = a.H / a.Hkv, per = a.T * G, at = threadIdx.x % W;
-  const int64_t id = (int64_t)blockIdx.x * ROWS + threadIdx.x / W;
-  if (id >= (int64_t)a.B * a.H * a.T) return;
+  const unsigned G = (unsigned)a.H / (unsigned)a.Hkv, per = a.T * G, id = blockIdx.x * ROWS + threadIdx.x / W;
+  const int at = threadIdx.x % W;
+  if (id >= (unsigned)a.B * a.H * a.T) return;
   // rows of a key head and sequence side by side
-  const int r = (int)(id % per), hk = (int)(id / per % a.Hkv), b = (int)(id / per / a.Hkv);
+  const unsigned r = id % per, hk = id / per % (unsigned)a.Hkv, b = id / per / (unsigned)a.Hkv;
   int64_t first, before = 0;
   int shared = 0;
   if constexpr (MODE == LISTED) {
     first = slot_of(a, hk, r % G / 16, (b * a.T + r / G) * a.parts) + r % G % 16;
   } else {
     first = slot_of(a, hk, r / 16, b * a.parts) + r % 16;
-    before = a.pre.slot(hk, (int64_t)b * per + r);
+    before = a.pre.slot(hk, b * per + r);
     shared = a.pre.parts;
   }
   const int parts = a.parts + shared;

@@ -20,6 +20,13 @@ __device__ __forceinline__ f32x4 mma16(bf16x8 a, bf16x8 b, f32x4 c) {
 
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
+// Where part p of `parts` begins: count * p / parts, without a product of more than 32 bits
+// (p <= parts < 2^15).
+__device__ __forceinline__ int share_of(int count, unsigned p, unsigned parts) {
+  const unsigned q = (unsigned)count / parts, rest = (unsigned)count % parts;
+  return (int)(q * p + rest * p / parts);
+}
+
 // One lane's share of a chunk: codes and scales of its keys and values.
 template <int D, bool VALUES> struct Stage4 {
   static constexpr int N = D / 32;  // words of codes of a 16-key tile
@@ -69,20 +76,31 @@ __device__ __forceinline__ int entry_of(const int *table, int64_t i) {
   return ((const __attribute__((address_space(4))) int *)table)[i];
 }
 
+// Where a lane's share of a tile stands behind what all lanes have of its address.
+template <int D> struct Offsets {
+  uint32_t k, ks, v, vs;  // bytes
+  __device__ __forceinline__ explicit Offsets(uint32_t lane) {
+    const uint32_t kb = lane >> 4, slot = lane & 15;
+    k = slot * (D / 2) + kb * (D / 8), ks = slot * (D / 32) + kb * (D / 4) / 32;
+    v = lane * (D / 8), vs = kb * (D / 8) + slot * (D / 16) / 32 * 4;
+  }
+  // (once a turn of a loop: known to stay the same they would be kept in 64 bits and added to
+  // the address, where a load takes 32 bits beside a scalar one)
+  __device__ __forceinline__ void hold() { asm volatile("" : "+v"(k), "+v"(ks), "+v"(v), "+v"(vs)); }
+};
+
 // A lane's share of tile i, tokens tok .. tok + 15 of a page, of which kp is a head's block of
 // keys and `values` bytes on that of its values (codes: bytes of a block's codes).
 template <int D, bool VALUES>
-__device__ __forceinline__ void load_tile(const uint8_t *kp, int64_t values, int tok, int codes, int lane, int i,
-                                          Stage4<D, VALUES> &x) {
+__device__ __forceinline__ void load_tile(const uint8_t *kp, int64_t values, int tok, int codes, const Offsets<D> &at,
+                                          int i, Stage4<D, VALUES> &x) {
   constexpr int N = D / 32;
-  const int kb = lane >> 4, slot = lane & 15;
-  load_words<N>(kp + (tok + slot) * (D / 2) + kb * (D / 8), x.k[i]);
-  x.ks[i] = kp[codes + (tok + slot) * (D / 32) + kb * (D / 4) / 32];
+  const uint8_t *k = kp + tok * (D / 2), *s = kp + codes + tok * (D / 32);
+  load_words<N>(k + at.k, x.k[i]);
+  x.ks[i] = s[at.ks];
   if constexpr (VALUES) {
-    const uint8_t *vp = kp + values;
-    load_words<N>(vp + tok * (D / 2) + lane * (D / 8), x.v[i]);
-    x.vs[i] = *reinterpret_cast<const uint32_t *>(vp + codes + tok * (D / 32) + kb * (D / 8) +
-                                                  slot * (D / 16) / 32 * 4);
+    load_words<N>(k + values + at.v, x.v[i]);
+    x.vs[i] = *reinterpret_cast<const uint32_t *>(s + values + at.vs);
   }
 }
 

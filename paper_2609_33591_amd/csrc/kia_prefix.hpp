@@ -21,8 +21,8 @@ __device__ __forceinline__ int last_of(const CachedArgs &a, int pos) { return mi
 typedef float WaveStats[NWAVE][16][2];
 
 // A row's extrema (scaled) over the shared tokens and what lies behind them, from the first pass.
-__device__ __forceinline__ void row_extrema(const CachedArgs &a, int hk, int64_t row, int kb, float &Mx, float &Mn) {
-  const int per = a.T * (a.H / a.Hkv), b = (int)(row / per), r = (int)(row % per);
+__device__ __forceinline__ void row_extrema(const CachedArgs &a, int hk, unsigned row, int kb, float &Mx, float &Mn) {
+  const unsigned per = a.T * ((unsigned)a.H / (unsigned)a.Hkv), b = row / per, r = row % per;
   Mx = -INFINITY, Mn = INFINITY;
   auto among = [&](const float *ext, int64_t first, int parts) {
     const float2 *e = reinterpret_cast<const float2 *>(ext) + first;
@@ -72,18 +72,17 @@ __device__ __forceinline__ void prefix_part(const CachedArgs &a, WaveStats *red,
   constexpr bool VALUES = PASS != PASS_EXTREMA;
   const int tid = threadIdx.x, lane = tid & 63, kb = lane >> 4, slot = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int hk = blockIdx.x % a.Hkv, groups = (a.pre.tiles + RT - 1) / RT;
-  const int tile0 = (int)(blockIdx.x / a.Hkv) % groups * RT, part = blockIdx.x / a.Hkv / groups;
-  const int G = a.H / a.Hkv, per = a.T * G;  // rows of a sequence
-  const int64_t total = (int64_t)a.B * per;
+  const unsigned G = (unsigned)a.H / (unsigned)a.Hkv, per = a.T * G, total = a.B * per;  // rows of a sequence, of all
+  const unsigned Hkv = a.Hkv, groups = ((unsigned)a.pre.tiles + RT - 1) / RT, id = blockIdx.x / Hkv;
+  const int hk = blockIdx.x % Hkv, tile0 = id % groups * RT, part = id / groups;
 
   // this lane's row of each tile, and the last key that it sees (below 0: none)
   int last[RT], lo = INT_MAX, hi = -1;
   bf16x8 q[RT][NP][N];
 #pragma unroll
   for (int x = 0; x < RT; ++x) {
-    const int64_t row = min((int64_t)(tile0 + x) * 16 + slot, total - 1);
-    const int b = (int)(row / per), r = (int)(row % per), t = r / G;
+    const unsigned row = min((unsigned)(tile0 + x) * 16 + slot, total - 1), b = row / per, r = row % per;
+    const int t = r / G;
     const int n = (int)min((int64_t)max(a.lengths[b], 0), (int64_t)a.width << a.lpage);
     last[x] = last_of(a, n - a.T + t);
     lo = min(lo, last[x]), hi = max(hi, last[x]);
@@ -98,8 +97,7 @@ __device__ __forceinline__ void prefix_part(const CachedArgs &a, WaveStats *red,
   }
   lo = __builtin_amdgcn_readfirstlane(lo), hi = __builtin_amdgcn_readfirstlane(hi);
   const int chunks = a.shared / CHUNK, seen = hi < 0 ? 0 : hi / CHUNK + 1;
-  const int c0 = (int)((int64_t)chunks * part / a.pre.parts);
-  const int c1 = min(seen, (int)((int64_t)chunks * (part + 1) / a.pre.parts));
+  const int c0 = share_of(chunks, part, a.pre.parts), c1 = min(seen, share_of(chunks, part + 1, a.pre.parts));
 
   const int codes = D / 2 << a.lpage;
   const int64_t block = (int64_t)codes + (D / 32 << a.lpage), stride = 2 * a.Hkv * block;
@@ -110,7 +108,9 @@ __device__ __forceinline__ void prefix_part(const CachedArgs &a, WaveStats *red,
 #pragma unroll
     for (int i = 0; i < TILES; ++i) entry[i] = entry_of(a.table, (min(c, c1 - 1) * CHUNK + 16 * i) >> a.lpage);
   };
+  Offsets<D> where(lane);
   auto load = [&](int c, Stage4<D, VALUES> &x) {
+    where.hold();
     x.ok = 0;
 #pragma unroll
     for (int i = 0; i < TILES; ++i) {
@@ -119,7 +119,7 @@ __device__ __forceinline__ void prefix_part(const CachedArgs &a, WaveStats *red,
       const bool ok = page >= 0 && page < a.pages;
       x.at[i] = key;
       x.ok |= ok << i;
-      load_tile<D, VALUES>(head + (ok ? page : 0) * stride, a.Hkv * block, key & ((1 << a.lpage) - 1), codes, lane, i, x);
+      load_tile<D, VALUES>(head + (ok ? page : 0) * stride, a.Hkv * block, key & ((1 << a.lpage) - 1), codes, where, i, x);
     }
   };
 
@@ -128,7 +128,7 @@ __device__ __forceinline__ void prefix_part(const CachedArgs &a, WaveStats *red,
   if constexpr (PASS == PASS_GRID) {
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
-      row_extrema(a, hk, min((int64_t)(tile0 + x) * 16 + slot, total - 1), kb, Mx[x], Mn[x]);
+      row_extrema(a, hk, min((unsigned)(tile0 + x) * 16 + slot, total - 1), kb, Mx[x], Mn[x]);
       rc[x] = row_const(Mx[x], Mn[x], a.K, CALIB, a.tau, a.scale);
     }
   }
@@ -145,7 +145,7 @@ __device__ __forceinline__ void prefix_part(const CachedArgs &a, WaveStats *red,
     load(c, cur);
     ask(c + NWAVE);
   }
-  for (; c < c1; c += NWAVE) {
+  auto step = [&](Stage4<D, VALUES> &cur, Stage4<D, VALUES> &nxt) __attribute__((always_inline)) {
     // (the last chunk again at the end: behind a branch, the wait for this chunk would be one for
     // what the branch may have asked for too)
     load(min(c + NWAVE, c1 - 1), nxt);
@@ -279,7 +279,17 @@ __device__ __forceinline__ void prefix_part(const CachedArgs &a, WaveStats *red,
           }
       }
     }
-    cur = nxt;
+  };
+  for (; c < c1; c += NWAVE) {
+    step(cur, nxt);
+    if constexpr (PASS == PASS_GRID) {
+      cur = nxt;
+    } else {
+      // (two chunks a turn, for no copies; the registers do not reach for the interval weights)
+      c += NWAVE;
+      if (c >= c1) break;
+      step(nxt, cur);
+    }
   }
 
   // the waves' parts, joined in their order
@@ -299,7 +309,7 @@ __device__ __forceinline__ void prefix_part(const CachedArgs &a, WaveStats *red,
     __syncthreads();
     if (tid < RT * 16) {
       const int x = tid / 16;
-      const int64_t row = (int64_t)(tile0 + x) * 16 + slot;
+      const unsigned row = (tile0 + x) * 16 + slot;
       if (row < total) {
         float mx = red[x][0][slot][0], mn = red[x][0][slot][1];
 #pragma unroll
@@ -323,7 +333,7 @@ __device__ __forceinline__ void prefix_part(const CachedArgs &a, WaveStats *red,
         for (int y = 0; y < NT; ++y) mine[(4 * kb + e) * NT + y] = o[x][y][e];
       __syncthreads();
       const int row16 = tid / 16, at = tid % 16;
-      const int64_t row = (int64_t)(tile0 + x) * 16 + row16;
+      const unsigned row = (tile0 + x) * 16 + row16;
       float top = 0.f, sum = 0.f, z[NT] = {};
       if constexpr (PASS == PASS_SOFTMAX) {
         top = red[x][0][row16][0];
