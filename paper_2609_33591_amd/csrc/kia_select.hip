@@ -16,7 +16,7 @@
 // to an eighth of that (three pieces: 768, to three eighths); magnitudes below 2^-96 count as
 // that, for what the matrix unit may flush.
 // Up to 500 pages of 32 sequences, 16 heads of 128 over 4 (17 MB of bounds), bf16: ranks 9.1 us,
-// the cut and the list 7.8, both mostly loads that wait for each other; with 64-bit sums for all
+// the cut and the list 7.3, both mostly loads that wait for each other; with 64-bit sums for all
 // 12.3 and 6.2. One token of 12 heads of 64 over 63 pages, one launch: 8.4.
 //
 // A workgroup selects for a token and key head. Where it can rank all of its pages soon
@@ -425,8 +425,9 @@ __device__ __forceinline__ bool refine(SelectLds<NT> &l, const SelectArgs &a, co
     int before = 0;  // those that come before this page
     if (open > need)
       for (int i = 0; i < open; ++i) {
-        const int v = __shfl(w, i);
-        const uint64_t o = (uint64_t)__shfl((unsigned long long)r, i);
+        const int v = __builtin_amdgcn_readlane(w, i);
+        const uint64_t o = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(r >> 32), i) << 32 |
+                           (uint32_t)__builtin_amdgcn_readlane((int)r, i);
         before += o > r || (o == r && v < w);
       }
     if (open <= 64 && w >= 0) rank[w] = before < need ? ALWAYS : 0;
@@ -483,14 +484,19 @@ template <typename TI, int D> __global__ __launch_bounds__(SCORE_NT) void score_
   if (threadIdx.x % 64 == 0) to.error[batch * NW + threadIdx.x / 64] = e;
 }
 
-template <typename TI, int D, int NT> __global__ __launch_bounds__(NT) void select_kernel(SelectArgs a) {
+// A selection from the ranks of a launch before; its own ones in LDS for up to RANKS pages (0: in the
+// workspace). 128 selections of up to 500 pages: 7.3 us, 8.4 from the workspace; four of 3125: 10.7 and
+// 11.4. (With 1024 threads and 256 for the other: 8.4, and 16.1.)
+template <typename TI, int D, int NT, int RANKS> __global__ __launch_bounds__(NT) void select_kernel(SelectArgs a) {
   extern __shared__ __attribute__((aligned(16))) float rows[];
   __shared__ SelectLds<NT> l;
+  __shared__ uint64_t rank[RANKS ? RANKS : 1];
   const Token k(a, blockIdx.x);
   const Space from(a, blockIdx.x);
   float e = 0.f;
   for (int i = threadIdx.x; i / (SCORE_NT / 64) * a.batch <= k.at; i += NT) e = larger(e, from.error[i]);
-  select<TI, D, NT>(l, a, k, blockIdx.x, from.key, e, rows, from.rank);
+  if constexpr (RANKS > 0) select<TI, D, NT>(l, a, k, blockIdx.x, from.key, e, rows, rank);
+  else select<TI, D, NT>(l, a, k, blockIdx.x, from.key, e, rows, from.rank);
 }
 
 // Both for pages that one workgroup ranks.
@@ -518,8 +524,10 @@ template <typename TI, int D> void run(const SelectArgs &a, hipStream_t s) {
     hipLaunchKernelGGL((score_kernel<TI, D>), dim3(batches * tokens), dim3(SCORE_NT), 0, s, a);
   });
   timed_call("kia_cache4_select", s, [&] {
-    if (a.width <= 1024) hipLaunchKernelGGL((select_kernel<TI, D, 256>), dim3(tokens), dim3(256), lds, s, a);
-    else hipLaunchKernelGGL((select_kernel<TI, D, 1024>), dim3(tokens), dim3(1024), lds, s, a);
+    const dim3 g(tokens);
+    if (a.width <= 1024) hipLaunchKernelGGL((select_kernel<TI, D, 256, 1024>), g, dim3(256), lds, s, a);
+    else if (a.width <= 4096) hipLaunchKernelGGL((select_kernel<TI, D, 1024, 4096>), g, dim3(1024), lds, s, a);
+    else hipLaunchKernelGGL((select_kernel<TI, D, 1024, 0>), g, dim3(1024), lds, s, a);
   });
 }
 

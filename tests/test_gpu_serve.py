@@ -62,6 +62,22 @@ def test_select_far_and_many():
             assert got[0].tolist() == want, (count, first, last)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("W", (1024, 1025, 4096, 4097))
+def test_select_of_the_most_heads(dtype, W):
+    """As many channels a key head as there may be, and tables to either side of what a
+    workgroup holds."""
+    page, d, H, n = 16, 128, 64, 16 * W - 5
+    table = torch.randperm(W, generator=torch.Generator().manual_seed(6)).int()[None].cuda()
+    cache = kia.Cache4(torch.zeros(W, 2, 1, page * (d // 2 + d // 32), dtype=torch.uint8, device="cuda"), d)
+    q, bounds = draw((1, H, 2, d), dtype, 7), draw((W, 1, 2, d), torch.bfloat16, 8)
+    bounds = torch.stack((bounds.amin(2), bounds.amax(2)), 2)
+    for count, first, last in ((64, 1, 2), (W - 3, 0, 1)):
+        got = kia.cache4_select(q, cache, bounds, table, ints(n), count, first, last)
+        want = select(q[0], by_table(bounds, table[0]), table[0].tolist(), n, page, W, count, first, last)
+        assert got[0].tolist() == want, (count, first, last)
+
+
 def test_select_what_is_not_finite():
     """A bound or query of NaN ranks as infinite, whatever else a page has; entries that name
     no page are not taken, first and last ones neither."""
