@@ -15,9 +15,9 @@
 // magnitudes: 2 D <= 256 products of bf16 queries, each rounded to 24 bits in the sum, add up
 // to an eighth of that (three pieces: 768, to three eighths); magnitudes below 2^-96 count as
 // that, for what the matrix unit may flush.
-// Up to 500 pages of 32 sequences, 16 heads of 128 over 4 (17 MB of bounds), bf16: ranks 9.1 us,
-// the cut and the list 7.3, both mostly loads that wait for each other; with 64-bit sums for all
-// 12.3 and 6.2. One token of 12 heads of 64 over 63 pages, one launch: 8.4.
+// Up to 500 pages of 32 sequences, 16 heads of 128 over 4 (17 MB of bounds), bf16: ranks 9.3 us,
+// the cut and the list 6.9, both mostly loads that wait for each other; with 64-bit sums for all
+// 12.3 and 6.2. One token of 12 heads of 64 over 63 pages, one launch: 8.5.
 //
 // A workgroup selects for a token and key head. Where it can rank all of its pages soon
 // enough, it does that itself; else a launch before ranks them in batches.
