@@ -560,6 +560,16 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
   }
 }
 
+// The power of two that a part's maximum m stands for, behind `top`: of a sequence's own keys m is a
+// score, of shared ones in log2 units already (`shared`), and so is `top` where there are shared ones.
+__device__ __forceinline__ float power_of(float m, float top, bool shared, float c2) {
+  if constexpr (MODE == BEHIND) return shared ? m - top : fmaf(m, c2, -top);
+  else return (m - top) * c2;
+}
+__device__ __forceinline__ float top_of(float m, bool shared, float c2) {
+  return MODE == BEHIND && !shared ? m * c2 : m;
+}
+
 // The parts of one row, joined in order: D / 4 threads a part, the parts in 1024 / D
 // groups whose sums are added in order of the groups.
 template <typename TI, int D> __global__ __launch_bounds__(256) void join_kernel(CachedArgs a) {
@@ -585,6 +595,7 @@ template <typename TI, int D> __global__ __launch_bounds__(256) void join_kernel
     shared = a.pre.parts;
     parts = a.parts + shared;
   }
+  const float c2 = a.scale * 1.44269504f;
   float m = -INFINITY, l = 0.f;
   if (tid < parts) {
     const float2 st = tid < shared ? reinterpret_cast<const float2 *>(a.pre.stat)[before + 16 * tid]
@@ -592,13 +603,13 @@ template <typename TI, int D> __global__ __launch_bounds__(256) void join_kernel
     l = st.y;
     if (l != 0.f) m = st.x;  // (a part that saw a key)
   }
-  float top = m;
+  float top = top_of(m, tid < shared, c2);
 #pragma unroll
   for (int i = 1; i < 64; i *= 2) top = fmaxf(top, __shfl_xor(top, i));
   if ((tid & 63) == 0) red[wave] = top;
   __syncthreads();
   top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  const float g = l == 0.f ? 0.f : __builtin_amdgcn_exp2f((m - top) * (a.scale * 1.44269504f));
+  const float g = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(power_of(m, top, tid < shared, c2));
   float sum = l * g;
 #pragma unroll
   for (int i = 1; i < 64; i *= 2) sum += __shfl_xor(sum, i);
@@ -655,11 +666,12 @@ template <typename TI, int D> __global__ __launch_bounds__(256) void join_few_ke
     return i < shared ? reinterpret_cast<const float2 *>(a.pre.stat)[before + 16 * i]
                       : reinterpret_cast<const float2 *>(a.stat)[first + 16 * (i - shared)];
   };
+  const float c2 = a.scale * 1.44269504f;
   float top = -INFINITY;
 #pragma unroll 4
   for (int i = 0; i < parts; ++i) {
     const float2 s = stat(i);
-    if (s.y != 0.f) top = fmaxf(top, s.x);  // (a part that saw a key)
+    if (s.y != 0.f) top = fmaxf(top, top_of(s.x, i < shared, c2));  // (a part that saw a key)
   }
   const f32x4 *p = reinterpret_cast<const f32x4 *>(a.part + first * D) + at;
   const f32x4 *y = reinterpret_cast<const f32x4 *>(a.pre.part + before * D) + at;
@@ -668,7 +680,7 @@ template <typename TI, int D> __global__ __launch_bounds__(256) void join_few_ke
 #pragma unroll 4
   for (int i = 0; i < parts; ++i) {
     const float2 s = stat(i);
-    const float g = s.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((s.x - top) * (a.scale * 1.44269504f));
+    const float g = s.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(power_of(s.x, top, i < shared, c2));
     sum = fmaf(s.y, g, sum);
     // (a NaN stays one, however small its part's weight)
     x += (i < shared ? y[(int64_t)i * 16 * W] : p[(int64_t)(i - shared) * 16 * W]) * g;

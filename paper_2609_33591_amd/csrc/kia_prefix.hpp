@@ -43,7 +43,11 @@ __device__ __forceinline__ void row_extrema(const CachedArgs &a, int hk, unsigne
 }
 
 // Weights of a row's scores of 32 keys against its running maximum m. That is moved, and the
-// sums scaled, only when passed by 2^8: where no lane sees that, no row does.
+// sums scaled, only when passed by 2^8: where no lane sees that, no row does. m is in log2 units,
+// rounded once where it is set: weights, rescaling and the joins all take that value, so that
+// its rounding (2^-16 of a weight at a score of 350 nats) is the same everywhere and divides out.
+// (Against m c2 rounded anew beside joins by the maximum itself, waves and parts were weighted
+// apart by that much.)
 template <int NT>
 __device__ __forceinline__ void softmax_weights(const float (&S)[TILES][4], float (&w)[TILES][4], float &m, float &sum,
                                                 f32x4 (&o)[NT], float c2) {
@@ -52,17 +56,17 @@ __device__ __forceinline__ void softmax_weights(const float (&S)[TILES][4], floa
   for (int i = 0; i < TILES; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) top = fmaxf(top, S[i][e]);
-  if (__any((top - m) * c2 > 8.f)) {
+  if (__any(fmaf(top, c2, -m) > 8.f)) {
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
-    const bool up = (top - m) * c2 > 8.f;
-    const float f = up ? __builtin_amdgcn_exp2f((m - top) * c2) : 1.f;
-    m = up ? top : m;
+    const bool up = fmaf(top, c2, -m) > 8.f;
+    const float to = top * c2, f = up ? __builtin_amdgcn_exp2f(m - to) : 1.f;
+    m = up ? to : m;
     sum *= f;
 #pragma unroll
     for (int y = 0; y < NT; ++y) o[y] *= f;
   }
-  const float mm = m == -INFINITY ? 0.f : m * c2;
+  const float mm = m == -INFINITY ? 0.f : m;
 #pragma unroll
   for (int i = 0; i < TILES; ++i)
 #pragma unroll
@@ -346,7 +350,7 @@ __device__ __forceinline__ void prefix_part(const CachedArgs &a, WaveStats *red,
       }
 #pragma unroll
       for (int i = 0; i < NWAVE; ++i) {
-        const float f = PASS == PASS_SOFTMAX ? __builtin_amdgcn_exp2f((red[x][i][row16][0] - top) * c2) : 1.f;
+        const float f = PASS == PASS_SOFTMAX ? __builtin_amdgcn_exp2f(red[x][i][row16][0] - top) : 1.f;
         sum = fmaf(red[x][i][row16][1], f, sum);
 #pragma unroll
         for (int e = 0; e < NT; ++e) z[e] = fmaf(rows[(i * 16 + row16) * (D + 4) + at * NT + e], f, z[e]);
@@ -356,7 +360,7 @@ __device__ __forceinline__ void prefix_part(const CachedArgs &a, WaveStats *red,
         float *y = a.pre.part + out * D + at * NT;
 #pragma unroll
         for (int e = 0; e < NT; ++e) y[e] = z[e];
-        if (at == 0) a.pre.stat[out * 2] = top, a.pre.stat[out * 2 + 1] = sum;
+        if (at == 0) a.pre.stat[out * 2] = top, a.pre.stat[out * 2 + 1] = sum;  // (log2 units)
       }
     }
   }

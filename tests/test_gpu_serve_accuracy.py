@@ -1,0 +1,43 @@
+"""Errors of the operators that serve from the 4-bit cache where single roundings would show:
+large scores, small ranks, far angles."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2609_33591_amd as kia  # noqa: E402
+from tests import around_reference as ref  # noqa: E402
+from tests.serve_reference import draw, ints, table_of  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("d", (32, 64, 128))
+@pytest.mark.parametrize("B,G", ((3, 4), (40, 16)))
+@pytest.mark.parametrize("score", (100, 700))
+def test_shared_weights_of_large_scores(d, B, G, score):
+    """Scores near `score` that fp32 holds exactly, one to a wave's keys and one to the sequence's
+    own: their weights agree however large the scores. All other keys weigh e^-score."""
+    page, shared = 16, 128
+    n, at = shared + 5, [5, 40, 70, 101, shared + 2]
+    table, pages = table_of((n,) * B, page, 3, shared)
+    cache = kia.new_cache4(pages, 1, page, d)
+    k, v = torch.zeros(B, 1, n, d, device="cuda"), draw((B, 1, n, d), torch.float32, 5)
+    v[:, :, :shared] = v[:1, :, :shared]
+    for i, j in enumerate(at):
+        k[:, 0, j, i] = 6.0
+    kia.cache4_write(k, v, cache, table, ints(*[0] * B))
+    q = torch.zeros(B, G, 1, d)
+    q[..., :5] = round(score * math.sqrt(d) / 6) + torch.randint(
+        0, 128, (B, G, 1, 5), generator=torch.Generator().manual_seed(7)) / 64
+    q, v = q.cuda(), ref.held(v)[:, :, at]
+    p = torch.softmax(6 * q.double()[..., :5] / math.sqrt(d), -1)
+    # In roundings of fp32, weights that are up to 3.1 powers of two apart: the factor of the scores
+    # (3) and the differences from maxima (3: weight, waves, parts) times 3.1 ln 2, three
+    # exponentials (2 each), products and sums (8): 27, and as many in the sum of the weights,
+    # whose reciprocal and product are 3 more
+    bound = 60 * ref.E * (p @ v.abs()) + 1e-30
+    for m in (0, shared):
+        o = kia.cache4_attention(q, cache, table, ints(*[n] * B), recon="softmax", shared=m)
+        ref.within(o, p @ v, bound, f"{m} shared")
