@@ -14,7 +14,9 @@
 // lies between is summed in 64 bits and chosen from. E is 2^-13 of the largest page's sum of
 // magnitudes: 2 D <= 256 products of bf16 queries, each rounded to 24 bits in the sum, add up
 // to an eighth of that (three pieces: 768, to three eighths); magnitudes below 2^-96 count as
-// that, for what the matrix unit may flush.
+// that, for factors that the matrix unit may flush, and E has 2^-116 beside, for the products and
+// sums that it may (768 times less than 2^-126): without it E itself is 0 for sums below 2^-136,
+// whose ranks are rounded to multiples of 2^-149.
 // Up to 500 pages of 32 sequences, 16 heads of 128 over 4 (17 MB of bounds), bf16: ranks 9.3 us,
 // the cut and the list 6.9, both mostly loads that wait for each other; with 64-bit sums for all
 // 12.3 and 6.2. One token of 12 heads of 64 over 63 pages, one launch: 8.5.
@@ -200,7 +202,7 @@ __device__ __forceinline__ float approximate(const SelectArgs &a, const Token &k
       }
     }
   }
-  return __uint_as_float(error) * 0x1p-13f;
+  return fmaf(__uint_as_float(error), 0x1p-13f, 0x1p-116f);
 }
 
 // The search for the place of a cut among the ranks K (32 or 64 bits) of a token's pages

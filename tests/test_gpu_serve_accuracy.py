@@ -8,7 +8,7 @@ torch = pytest.importorskip("torch")
 
 import paper_2609_33591_amd as kia  # noqa: E402
 from tests import around_reference as ref  # noqa: E402
-from tests.serve_reference import draw, ints, table_of  # noqa: E402
+from tests.serve_reference import draw, ints, select, table_of  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -41,3 +41,21 @@ def test_shared_weights_of_large_scores(d, B, G, score):
     for m in (0, shared):
         o = kia.cache4_attention(q, cache, table, ints(*[n] * B), recon="softmax", shared=m)
         ref.within(o, p @ v, bound, f"{m} shared")
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("W", (200, 1100))
+@pytest.mark.parametrize("scales", ((-40, -40), (-66, -66), (-70, -70), (-72, -72), (-75, -75), (-80, -80), (-20, -125),
+                                    (-125, -20), (-100, -120), (62, 62), (100, 24)))
+def test_select_of_any_magnitude(dtype, W, scales):
+    """Ranks whose fp32 sums would be rounded to few bits, to none, or pass fp32's range: the
+    selection is that of the sums in 64 bits, by one workgroup a token and by two launches."""
+    page, d, H, count = 16, 64, 4, 50
+    table = torch.randperm(W, generator=torch.Generator().manual_seed(6)).int()[None].cuda()
+    cache = kia.Cache4(torch.zeros(W, 2, 1, page * (d // 2 + d // 32), dtype=torch.uint8, device="cuda"), d)
+    q, x = ((draw(s, torch.float32, i).double() * 2.0 ** e).float()
+            for s, i, e in (((1, H, 2, d), 11, scales[0]), ((W, 1, 2, d), 12, scales[1])))
+    q, x, n = q.to(dtype), torch.stack((x.amin(2), x.amax(2)), 2).bfloat16(), 16 * W - 3
+    got = kia.cache4_select(q, cache, x, table, ints(n), count)
+    want = select(q[0], x[table[0].long()], table[0].tolist(), n, page, W, count, 1, 1)
+    assert got[0].tolist() == want
