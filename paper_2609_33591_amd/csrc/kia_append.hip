@@ -13,10 +13,11 @@
 // thirds of what the vector units can issue in that time. A token each of 32 sequences, 16 heads
 // of 128 over 4: 10 us, loads of the length, page, keys and earlier tokens one after another.
 //
-// A rotated key is rounded once, to its 4 bits. The rotation in 32 bits is off by up to
-// 2^-21 of the pair's magnitudes, which decides another code for about one value in 10^7: where
-// any of a group's codes or its scale could differ within 2^-20, the group is taken again in
-// 64 bits.
+// A rotated key is rounded once, to its 4 bits. The rotation in 32 bits is off by up to 7.4 roundings
+// (2^-24) of the pair's magnitudes: 4 of sine and cosine, 0.4 of the angle's rest in 32 bits, one each
+// of the factor, the product and the fma. That decides another code for about one value in
+// 10^7: where any of a group's codes or its scale could differ within 10 roundings, the group
+// is taken again in 64 bits.
 #include "kia_cache.hpp"
 
 namespace kia {
@@ -58,6 +59,18 @@ __device__ __forceinline__ void turn64(double x, double &s, double &c) {
   s = k & 1 ? w : u;
   c = k & 1 ? -u : w;
   if (k & 2) s = -s, c = -c;
+}
+
+// sin and cos of the same angle in 32 bits for that check: the rest behind the quarter turns is that
+// of the angle itself however far it is (2 / pi in two parts; rounded to 53 bits, their product is
+// off by more than the check allows for from 2^30 radians on, as rotated queries are there).
+__device__ __forceinline__ void turn_key(double x, float &s, float &c) {
+  constexpr double HI = 0.63661977236758134308, LO = -3.9357353350364972e-17;
+  const double q = rint(x * HI);
+  sincospif(0.5f * (float)fma(x, LO, fma(x, HI, -q)), &s, &c);
+  const int k = (int)(q - 4.0 * floor(q * 0.25));
+  if (k & 1) { const float y = s; s = c; c = -y; }
+  if (k & 2) { s = -s; c = -c; }
 }
 
 // The code and scale byte of a channel y from 64 bits: the other 31 of its group are the next
@@ -203,7 +216,7 @@ template <int MODE>
 __device__ __forceinline__ bool quantise_turned(const Chunk &k, const float2 *turn, int oct, int n, float factor,
                                                 uint32_t &w, uint32_t &s) {
   float z[8];
-  // what a turned channel may be off by
+  // what a turned channel may be off by: 10 roundings
   const float off = turned<MODE>(k, turn, oct, n, z) * fabsf(factor) * 0x1.4p-21f;
   uint32_t top = 0;  // (as bits: NaN above infinity above every finite value)
 #pragma unroll
@@ -386,7 +399,9 @@ __global__ __launch_bounds__(Threads<D>::N, 4) void append_kernel(AppendArgs a) 
       for (int e = tid; e < (s.hi - s.lo) * n; e += NT) {
         const int t = s.lo + e / n, m = e % n;
         float sn, cs;
-        turn_of((double)(s.base + t), a.freq[m], sn, cs);
+        const double p = (double)(s.base + t);
+        if (kind == 0) turn_key(p * a.freq[m], sn, cs);
+        else turn_of(p, a.freq[m], sn, cs);
         turns_of[(t - s.lo) * table.size() + table.at(m)] = make_float2(cs * a.factor, sn * a.factor);
       }
     }

@@ -59,3 +59,22 @@ def test_select_of_any_magnitude(dtype, W, scales):
     got = kia.cache4_select(q, cache, x, table, ints(n), count)
     want = select(q[0], x[table[0].long()], table[0].tolist(), n, page, W, count, 1, 1)
     assert got[0].tolist() == want
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("layout,rot", (("half", 128), ("interleaved", 128), ("half", 72)))
+@pytest.mark.parametrize("freq,start", ((1.0, 2 ** 31 - 2048), (1e4, 1_000_000), (1e6, 1_000_000), (1e6, 2 ** 31 - 2048)))
+def test_keys_at_far_angles(dtype, layout, rot, freq, start):
+    """Keys are held as the rounding of the exact rotation by the angle p f, a product in 64 bits,
+    however many turns that is."""
+    Hkv, T, d, page = 8, 512, 128, 256
+    W = (start + T) // page + 1
+    table = torch.full((1, W), -1, dtype=torch.int32)
+    table[0, start // page:] = torch.arange(W - start // page)
+    cache = kia.new_cache4(8, Hkv, page, d)
+    plan = kia.RotaryPlan(torch.linspace(freq / 2, freq, rot // 2, dtype=torch.float64, device="cuda"), layout)
+    k = draw((1, Hkv, T, d), dtype, 11, 2.0)
+    kia.cache4_append(k, k, k, cache, table.cuda(), ints(start), plan)
+    got = kia.cache4_read(cache, table.cuda(), ints(start), T, torch.float32)[0]
+    want = ref.rotary(k, plan.freq, layout, plan.factor, torch.arange(start, start + T, device="cuda")[None])[0]
+    assert torch.equal(got.double(), ref.held(want))
