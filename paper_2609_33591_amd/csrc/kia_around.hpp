@@ -18,6 +18,35 @@ template <typename TI> __device__ __forceinline__ TI *slice_of(const View &v, in
   return static_cast<TI *>(v.p) + b * v.sb + h * v.sh;
 }
 
+// A value of all 64 lanes, by rotations of 16 and then from lane to scalar.
+template <int CTRL> __device__ __forceinline__ uint32_t rotated(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xf, 0xf, true);
+}
+template <class F> __device__ __forceinline__ uint32_t over16(uint32_t x, F f) {
+  x = f(x, rotated<0x128>(x));  // row_ror 8, 4, 2, 1
+  x = f(x, rotated<0x124>(x));
+  x = f(x, rotated<0x122>(x));
+  return f(x, rotated<0x121>(x));
+}
+template <class F> __device__ __forceinline__ uint32_t over64(uint32_t x, F f) {
+  x = over16(x, f);
+  const uint32_t y[4] = {(uint32_t)__builtin_amdgcn_readlane((int)x, 0), (uint32_t)__builtin_amdgcn_readlane((int)x, 16),
+                         (uint32_t)__builtin_amdgcn_readlane((int)x, 32), (uint32_t)__builtin_amdgcn_readlane((int)x, 48)};
+  return f(f(y[0], y[1]), f(y[2], y[3]));
+}
+struct Sum { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return a + b; } };
+// The sum of the lanes before a lane, and its own.
+__device__ __forceinline__ uint32_t sum_to(uint32_t x) {
+  x += rotated<0x111>(x);  // row_shr 1, 2, 4, 8 (zeros come in)
+  x += rotated<0x112>(x);
+  x += rotated<0x114>(x);
+  x += rotated<0x118>(x);
+  const uint32_t a = __builtin_amdgcn_readlane((int)x, 15), b = __builtin_amdgcn_readlane((int)x, 31),
+                 c = __builtin_amdgcn_readlane((int)x, 47);
+  const int row = (threadIdx.x & 63) >> 4;
+  return x + (row > 0 ? a : 0) + (row > 1 ? b : 0) + (row > 2 ? c : 0);
+}
+
 // ---- rotary positions (kia_rotary.hip) ----------------------------------------
 struct RotSide {
   const void *x;
@@ -156,8 +185,11 @@ struct CachedArgs {
   float tau, scale;
   int tiles, shares;  // 16-row tiles of a key head's rows, parts of its keys (< 256)
   // Over listed pages, and over what lies behind shared tokens: `tiles` of a token's, or a
-  // sequence's, rows, `parts` for each, `shares` in all for a row tile.
-  int parts;
+  // sequence's, rows, `parts` for each, `shares` in all for a row tile. With `spread` (about
+  // so many in all) the sequences have parts by their lengths, up to `most`: `own` [tiles][B]
+  // says which, and `parts` is the usual number.
+  int parts, spread, most;
+  int2 *own;  // first part, and how many
   const int *list;  // [B][Hkv][T][count]
   int count;
   int shared;  // tokens
@@ -165,6 +197,9 @@ struct CachedArgs {
 };
 // Entries of a list that one part takes, at most.
 constexpr int LISTED_MOST = 1024;
+// A row's parts are joined by a workgroup, or, where up to FEW_PARTS are usual and there are many
+// rows, by D / 4 lanes.
+constexpr int FEW_PARTS = 8, MANY_ROWS = 2048;
 // Floats of the workspace: the parts' extrema, their maxima and sums, their rows.
 struct CachedLayout {
   size_t ext, stat, part, total;

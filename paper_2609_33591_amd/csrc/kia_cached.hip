@@ -82,12 +82,17 @@ struct Chunks {
   __device__ __forceinline__ int at(int n) const { return (n < sink ? n : low + n - sink) * CHUNK; }
 };
 
+// A sequence's keys.
+struct Length { int n; };
+__device__ __forceinline__ Length length_of(const CachedArgs &a, int b) {
+  return {(int)min((int64_t)max(a.lengths[b], 0), (int64_t)a.width << a.lpage)};
+}
 // The positions of the first and the last row of a row tile.
 struct Rows16 {
   int n, lo, hi;  // n: the sequence's keys
-  __device__ __forceinline__ Rows16(const CachedArgs &a, int b, int tile) {
+  __device__ __forceinline__ Rows16(const CachedArgs &a, int b, int tile) : Rows16(a, tile, length_of(a, b)) {}
+  __device__ __forceinline__ Rows16(const CachedArgs &a, int tile, Length x) : n(x.n) {
     const unsigned G = (unsigned)a.H / (unsigned)a.Hkv, total = a.T * G;
-    n = (int)min((int64_t)max(a.lengths[b], 0), (int64_t)a.width << a.lpage);
     lo = n - a.T + (int)(tile * 16u / G);
     hi = n - a.T + (int)(min(tile * 16u + 15, total - 1) / G);
   }
@@ -137,6 +142,53 @@ struct Share {
     }
   }
 };
+
+// The same of what lies behind shared tokens: about a.spread parts in all, one at least and a.most at
+// most for a sequence. (256 sequences at a time, whose lengths are asked for together, and sums
+// without LDS: short remainders have workgroups of a few us. As Share does it, 256 sequences of 200
+// tokens of their own took 8 us longer.)
+struct Spread {
+  int b = -1, first = 0, parts = 0;
+  Length length = {0};
+  __device__ __forceinline__ Spread(const CachedArgs &a, int tile, int w) {
+    constexpr int U = 4;
+    const int lane = threadIdx.x & 63, before = a.shared / CHUNK;
+    Length n[U];  // of sequences i + 64 u + lane
+    auto load = [&](int i) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) n[u] = length_of(a, min(i + 64 * u + lane, a.B - 1));
+    };
+    auto chunks = [&](int u) { return max(0, Rows16(a, tile, n[u]).chunks(a).count - before); };
+    double all = 0;
+    for (int i = 0; i < a.B; i += 64 * U) {
+      load(i);
+      uint32_t x = 0;  // (up to 2^28)
+#pragma unroll
+      for (int u = 0; u < U; ++u) x += i + 64 * u + lane < a.B ? chunks(u) : 0;
+      all += over64(x & 0xffff, Sum()) + 65536.0 * over64(x >> 16, Sum());
+    }
+    const int per = max(NWAVE, (int)ceil(all / a.spread));
+    int base = 0;
+    for (int i = 0; i < a.B; i += 64 * U) {
+      if (a.B > 64 * U) load(i);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int p = i + 64 * u + lane < a.B ? min(max(1, (chunks(u) + per - 1) / per), a.most) : 0;
+        const int to = (int)sum_to((uint32_t)p);
+        const uint64_t hit = __ballot(base + to > w);
+        if (hit) {
+          const int at = __builtin_ctzll(hit);
+          b = __builtin_amdgcn_readfirstlane(i + 64 * u + at);
+          length = {__builtin_amdgcn_readlane(n[u].n, at)};
+          parts = __builtin_amdgcn_readlane(p, at);
+          first = base + __builtin_amdgcn_readlane(to, at) - parts;
+          return;
+        }
+        base += __builtin_amdgcn_readlane(to, 63);
+      }
+    }
+  }
+};
 // Of part w of a key head's row tile: its place in the workspace, in rows.
 __device__ __forceinline__ int64_t slot_of(const CachedArgs &a, int hk, int tile, int w) {
   const int slots = MODE == SEQUENCE ? a.shares + a.B : a.shares;
@@ -150,17 +202,24 @@ struct Work {
   Chunks chunks;
   __device__ __forceinline__ Work(const CachedArgs &a, int tile, int w) {
     const int G = (unsigned)a.H / (unsigned)a.Hkv;
+    Length length;
     if constexpr (MODE == SEQUENCE) {
       const Share share(a, tile, w, false);
       b = share.b, first = share.first, parts = share.parts;
+      if (b < 0) return;
+      length = length_of(a, b);
+    } else if (MODE == BEHIND && a.spread) {
+      const Spread spread(a, tile, w);
+      b = spread.b, first = spread.first, parts = spread.parts, length = spread.length;
       if (b < 0) return;
     } else {
       // (as many parts for every sequence, or for every token of one)
       const unsigned id = (unsigned)w / (unsigned)a.parts;
       parts = a.parts, first = id * parts;
       b = MODE == LISTED ? id / (unsigned)a.T : id;
+      length = length_of(a, b);
     }
-    const Rows16 rows16(a, b, tile);
+    const Rows16 rows16(a, tile, length);
     n = rows16.n;
     if constexpr (MODE == LISTED) {
       t0 = first / parts - b * a.T, rows = G;
@@ -493,6 +552,10 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
   }
 
   const int64_t out = slot_of(a, hk, tile, w);
+  if constexpr (MODE == BEHIND && PASS != PASS_GRID) {
+    // (the first pass, for later launches)
+    if (a.spread && hk == 0 && w == work.first && tid == 0) a.own[tile * a.B + b] = make_int2(work.first, work.parts);
+  }
   if constexpr (PASS == PASS_EXTREMA) {
     m = across<FEW>(m, [](float x, float y) { return fmaxf(x, y); });
     low = across<FEW>(low, [](float x, float y) { return fminf(x, y); });
@@ -590,10 +653,11 @@ template <typename TI, int D> __global__ __launch_bounds__(256) void join_kernel
     first = slot_of(a, hk, r % G / 16, (b * a.T + r / G) * a.parts) + r % G % 16;
     parts = a.parts;
   } else {
-    first = slot_of(a, hk, r / 16, b * a.parts) + r % 16;
+    const int2 own = own_parts(a, r / 16, b);
+    first = slot_of(a, hk, r / 16, own.x) + r % 16;
     before = a.pre.slot(hk, b * a.T * G + r);
     shared = a.pre.parts;
-    parts = a.parts + shared;
+    parts = own.y + shared;
   }
   const float c2 = a.scale * 1.44269504f;
   float m = -INFINITY, l = 0.f;
@@ -644,7 +708,6 @@ template <typename TI, int D> __global__ __launch_bounds__(256) void join_kernel
 // The same for many rows of few parts: D / 4 lanes a row, which walk its parts in order, and
 // 1024 / D rows a workgroup. (4096 rows of five parts: 5.0 us, a workgroup each 8.3; 1024 rows of 13
 // parts 5.6 and 4.4.)
-constexpr int FEW_PARTS = 8, MANY_ROWS = 2048;
 template <typename TI, int D> __global__ __launch_bounds__(256) void join_few_kernel(CachedArgs a) {
   constexpr int W = D / 4, ROWS = 256 / W;
   const unsigned G = (unsigned)a.H / (unsigned)a.Hkv, per = a.T * G, id = blockIdx.x * ROWS + threadIdx.x / W;
@@ -653,15 +716,17 @@ template <typename TI, int D> __global__ __launch_bounds__(256) void join_few_ke
   // rows of a key head and sequence side by side
   const unsigned r = id % per, hk = id / per % (unsigned)a.Hkv, b = id / per / (unsigned)a.Hkv;
   int64_t first, before = 0;
-  int shared = 0;
+  int shared = 0, parts;
   if constexpr (MODE == LISTED) {
     first = slot_of(a, hk, r % G / 16, (b * a.T + r / G) * a.parts) + r % G % 16;
+    parts = a.parts;
   } else {
-    first = slot_of(a, hk, r / 16, b * a.parts) + r % 16;
+    const int2 own = own_parts(a, r / 16, b);
+    first = slot_of(a, hk, r / 16, own.x) + r % 16;
     before = a.pre.slot(hk, b * per + r);
     shared = a.pre.parts;
+    parts = own.y + shared;
   }
-  const int parts = a.parts + shared;
   auto stat = [&](int i) {
     return i < shared ? reinterpret_cast<const float2 *>(a.pre.stat)[before + 16 * i]
                       : reinterpret_cast<const float2 *>(a.stat)[first + 16 * (i - shared)];

@@ -23,6 +23,12 @@ __device__ __forceinline__ int last_of(const CachedArgs &a, int pos) { return mi
 // LDS of a workgroup: its waves' statistics and, tile by tile, their rows.
 typedef float WaveStats[NWAVE][16][2];
 
+// The parts of what lies behind the shared tokens, of row tile `tile` of sequence b: the first
+// one's number, and how many.
+__device__ __forceinline__ int2 own_parts(const CachedArgs &a, unsigned tile, unsigned b) {
+  return a.spread ? a.own[tile * a.B + b] : make_int2(b * a.parts, a.parts);
+}
+
 // A row's extrema (scaled) over the shared tokens and what lies behind them, from the first pass.
 __device__ __forceinline__ void row_extrema(const CachedArgs &a, int hk, unsigned row, int kb, float &Mx, float &Mn) {
   const unsigned per = a.T * ((unsigned)a.H / (unsigned)a.Hkv), b = row / per, r = row % per;
@@ -36,7 +42,8 @@ __device__ __forceinline__ void row_extrema(const CachedArgs &a, int hk, unsigne
     }
   };
   among(a.pre.ext, a.pre.slot(hk, row), a.pre.parts);
-  among(a.ext, (((int64_t)hk * a.tiles + r / 16) * a.shares + (int64_t)b * a.parts) * 16 + r % 16, a.parts);
+  const int2 own = own_parts(a, r / 16, b);
+  among(a.ext, (((int64_t)hk * a.tiles + r / 16) * a.shares + own.x) * 16 + r % 16, own.y);
   Mx = fmaxf(Mx, __shfl_xor(Mx, 16)), Mx = fmaxf(Mx, __shfl_xor(Mx, 32));
   Mn = fminf(Mn, __shfl_xor(Mn, 16)), Mn = fminf(Mn, __shfl_xor(Mn, 32));
   Mx *= a.scale, Mn *= a.scale;

@@ -60,36 +60,8 @@ template <int D> __device__ __forceinline__ double page_sum(double x) {
   if constexpr (D >= 128) x += moved<0x140>(x);  // row_mirror
   return x;
 }
-// A value of all 64 lanes, by rotations of 16 and then from lane to scalar.
-template <int CTRL> __device__ __forceinline__ uint32_t rotated(uint32_t x) {
-  return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xf, 0xf, true);
-}
-template <class F> __device__ __forceinline__ uint32_t over16(uint32_t x, F f) {
-  x = f(x, rotated<0x128>(x));  // row_ror 8, 4, 2, 1
-  x = f(x, rotated<0x124>(x));
-  x = f(x, rotated<0x122>(x));
-  return f(x, rotated<0x121>(x));
-}
-template <class F> __device__ __forceinline__ uint32_t over64(uint32_t x, F f) {
-  x = over16(x, f);
-  const uint32_t y[4] = {(uint32_t)__builtin_amdgcn_readlane((int)x, 0), (uint32_t)__builtin_amdgcn_readlane((int)x, 16),
-                         (uint32_t)__builtin_amdgcn_readlane((int)x, 32), (uint32_t)__builtin_amdgcn_readlane((int)x, 48)};
-  return f(f(y[0], y[1]), f(y[2], y[3]));
-}
 struct Most { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return max(a, b); } };
-struct Sum { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return a + b; } };
 struct Least { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return min(a, b); } };
-// The sum of the lanes before a lane, and its own.
-__device__ __forceinline__ uint32_t sum_to(uint32_t x) {
-  x += rotated<0x111>(x);  // row_shr 1, 2, 4, 8 (zeros come in)
-  x += rotated<0x112>(x);
-  x += rotated<0x114>(x);
-  x += rotated<0x118>(x);
-  const uint32_t a = __builtin_amdgcn_readlane((int)x, 15), b = __builtin_amdgcn_readlane((int)x, 31),
-                 c = __builtin_amdgcn_readlane((int)x, 47);
-  const int row = (threadIdx.x & 63) >> 4;
-  return x + (row > 0 ? a : 0) + (row > 1 ? b : 0) + (row > 2 ? c : 0);
-}
 // The larger magnitude, or NaN.
 __device__ __forceinline__ float larger(float a, float b) {
   return __uint_as_float(max(__float_as_uint(a) & 0x7fffffffu, __float_as_uint(b) & 0x7fffffffu));

@@ -191,7 +191,13 @@ size_t pages_lay(CachedArgs &a, int d, float *ws) {
 }
 
 // Shared tokens: the rows of all sequences over them in parts that fill the chip, and each
-// sequence's over what lies behind.
+// sequence's over what lies behind: as many parts for each, or, where the table has room for texts
+// that pass the shared tokens by more than SPREAD_FROM, about as many in all by the lengths (256
+// sequences behind 8192 tokens, 200 of their own and one 100 000: 60 us, with its own in one part 660,
+// without shared tokens 206; one 30 000: 55 and 214; one 4000: as many parts for each 51, by lengths 49).
+// Where all are short in such a table it costs a few us: 41 -> 47 for 256 of 200, 32 -> 35 for 64 of up
+// to 1000 (LERP), as each workgroup walks the lengths.
+constexpr int SPREAD_FROM = 4096;
 int shared_shape(CachedArgs &a, int page, int width, int B, int H, int Hkv, int T, int d, int shared, int dtype) {
   const int rc = check_sizes(a, page, width, B, H, Hkv, T, d);
   if (rc) return rc;
@@ -205,6 +211,9 @@ int shared_shape(CachedArgs &a, int page, int width, int B, int H, int Hkv, int 
   // (64 sequences behind 8192 tokens, 1000 of their own at most: with all of it 29.5 us, so 25).
   const int64_t groups = (int64_t)B * Hkv * a.tiles, own = keys - shared, cus = host_cus();
   a.parts = (int)std::max<int64_t>(1, std::min<int64_t>({2 * cus / groups, (own + 255) / 256, 64}));
+  // (a begun part a sequence is half of one)
+  if (own > SPREAD_FROM) a.spread = B * a.parts - B / 2;
+  a.shares = a.spread ? a.spread + B : B * a.parts;
   a.pre.tiles = (int)(((int64_t)B * T * G + 15) / 16);
   const int rt = prefix_tiles(a.pre.tiles, d, dtype);
   const int64_t blocks = (int64_t)Hkv * ((a.pre.tiles + rt - 1) / rt);
@@ -212,14 +221,17 @@ int shared_shape(CachedArgs &a, int page, int width, int B, int H, int Hkv, int 
   const int64_t slots = (int64_t)(2.0 * cus * std::max(0.5, work / (work + rest)));
   a.pre.parts = (int)std::max<int64_t>(
       1, std::min<int64_t>({(slots + blocks / 2) / blocks, ((int64_t)shared + 127) / 128, 128}));
-  if (too_many((double)groups * a.parts + (double)blocks * a.pre.parts)) return KIA_ERR_SHAPE;
+  if (too_many((double)a.shares * Hkv * a.tiles + (double)blocks * a.pre.parts)) return KIA_ERR_SHAPE;
   a.pre.blocks = (unsigned)(blocks * a.pre.parts);
-  a.shares = B * a.parts;
+  // (a join of up to 256 parts by a workgroup, or of not too many by a few lanes)
+  a.most = (int64_t)B * H * T >= MANY_ROWS && a.parts + a.pre.parts <= FEW_PARTS ? 24 : 127;
   return KIA_OK;
 }
 size_t shared_lay(CachedArgs &a, int d, float *ws) {
   const size_t at = lay(0, (size_t)a.shares * a.Hkv * a.tiles * 16, d, ws, a.ext, a.stat, a.part);
-  return lay(at, (size_t)a.Hkv * a.pre.tiles * 16 * a.pre.parts, d, ws, a.pre.ext, a.pre.stat, a.pre.part);
+  const size_t end = lay(at, (size_t)a.Hkv * a.pre.tiles * 16 * a.pre.parts, d, ws, a.pre.ext, a.pre.stat, a.pre.part);
+  if (ws) a.own = reinterpret_cast<int2 *>(ws + end);
+  return end + (a.spread ? 2 * (size_t)a.tiles * a.B : 0);
 }
 
 }  // namespace
