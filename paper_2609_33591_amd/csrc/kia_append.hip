@@ -8,10 +8,11 @@
 // multiples of their size, so that the tokens of a page are one workgroup's, and the bounds
 // need no atomics and no second pass: the held values of the page's tokens go to LDS, the
 // earlier ones read back from the page. 4 prompts of 2048 tokens, 16
-// heads of 128 for queries and keys, bf16, with bounds: 47 us for 152 MB, 3.3 TB/s of the 5.1
-// that a copy reaches; rotating, finding codes and bounds takes 19 million wave instructions, two
-// thirds of what the vector units can issue in that time. A token each of 32 sequences, 16 heads
-// of 128 over 4: 10 us, loads of the length, page, keys and earlier tokens one after another.
+// heads of 128 for queries and keys, bf16, with bounds: 47 us for 153 MB, 3.3 TB/s of the 5.1
+// that a copy reaches; rotating, finding codes and bounds keeps the vector units active for 56% of the
+// cycles. Neither is full: 128 registers leave two workgroups of eight waves a CU. A token each of 32
+// sequences, 16 heads of 128 over 4: 10 us, loads of the length, page, keys and earlier tokens one
+// after another, by 16 of a workgroup's 512 lanes.
 //
 // A rotated key is rounded once, to its 4 bits. The rotation in 32 bits is off by up to 7.4 roundings
 // (2^-24) of the pair's magnitudes: 4 of sine and cosine, 0.4 of the angle's rest in 32 bits, one each
@@ -569,9 +570,10 @@ template <int D> void append_d(const AppendArgs &a, dim3 grid, int dtype, hipStr
 }  // namespace
 
 // Workgroups: the spans of 64 positions (or a page), and of each span's heads as many shares
-// as make four workgroups a CU (the prompts above with three / four / six / eight / twelve: 49 /
-// 47 / 51 / 58 / 66 us, as more of them compute the same angles); keys, values and queries have
-// shares of their own.
+// as make four workgroups a CU, twice what the registers let run at once (the prompts above with three
+// / four / six / eight / twelve: 49 / 47 / 51 / 58 / 66 us: fewer leave the last round emptier, more
+// compute the same angles again); keys, values and queries have shares of their own, by their
+// heads and not by their work, of which keys have the most.
 void launch_append(AppendArgs a, int d, int dtype, int cus, hipStream_t s) {
   const unsigned spans = (unsigned)a.c.B * a.spans;
   const int want = (int)std::max(1u, (4u * cus + spans - 1) / spans), all = 2 * a.c.Hkv + a.H;

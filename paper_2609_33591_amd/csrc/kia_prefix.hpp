@@ -8,8 +8,8 @@
 // 100 vector operations, and a tile's weights, some 45, bound the kernel before the matrix unit
 // does; the keys come out of the L2 after the first tile. Key heads go round the workgroups, so
 // that an XCD's share of them are few and fit.
-// 1024 rows a key head over 16 384 tokens, four heads of 128, softmax, bf16: 56 us, 610 TFLOP/s (one
-// tile a wave: 80 us); 256 rows over 8192, LERP: 9 and 25 us (10 and 27). For a few row tiles it
+// 1024 rows a key head over 16 384 tokens, four heads of 128, softmax, bf16: 58 us, 600 TFLOP/s (one
+// tile a wave: 80 us); 256 rows over 8192, LERP: 9 to 10 and 25 us (10 and 27). For a few row tiles it
 // does not matter (six of fp32 heads of 64, two key heads: 4.7 and 8.7 us, 4.8 and 8.1).
 #pragma once
 

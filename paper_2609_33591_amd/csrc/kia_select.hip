@@ -18,8 +18,8 @@
 // sums that it may (768 times less than 2^-126): without it E itself is 0 for sums below 2^-136,
 // whose ranks are rounded to multiples of 2^-149.
 // Up to 500 pages of 32 sequences, 16 heads of 128 over 4 (17 MB of bounds), bf16: ranks 9.3 us,
-// the cut and the list 6.9, both mostly loads that wait for each other; with 64-bit sums for all
-// 12.3 and 6.2. One token of 12 heads of 64 over 63 pages, one launch: 8.5.
+// the cut and the list 7.1, both mostly loads that wait for each other; with 64-bit sums for all
+// the two took 1.5 us longer together. One token of 12 heads of 64 over 63 pages, one launch: 8.4.
 //
 // A workgroup selects for a token and key head. Where it can rank all of its pages soon
 // enough, it does that itself; else a launch before ranks them in batches.
@@ -243,7 +243,9 @@ __device__ __forceinline__ Cut<K> cut_of(SelectLds<NT> &l, const K *rank, int n,
   int bits = least == most ? 0 : sizeof(K) == 8 ? 64 - __builtin_clzll(least ^ most) : 32 - __builtin_clz((uint32_t)(least ^ most));
   r.mask = bits == BITS ? 0 : ALWAYS << bits;
   r.cut = most & r.mask;
-  // (of an approximate rank 16 bits: less than its error)
+  // (of an approximate rank 16 of the undecided bits. Where the ranks have their sign and five bits of
+  // the exponent in common, what is left is below 2^-13 of a rank and so within E; else it is up to
+  // 2^-7, and more pages are left open to the sums in 64 bits than need be: the selection is the same)
   for (int i = 0; bits > 0 && (sizeof(K) == 8 || i < 2); ++i) {
     const int shift = max(bits - 8, 0);
     const uint32_t digit = (1u << (bits - shift)) - 1;
@@ -459,8 +461,8 @@ template <typename TI, int D> __global__ __launch_bounds__(SCORE_NT) void score_
 }
 
 // A selection from the ranks of a launch before; its own ones in LDS for up to RANKS pages (0: in the
-// workspace). 128 selections of up to 500 pages: 7.3 us, 8.4 from the workspace; four of 3125: 10.7 and
-// 11.4. (With 1024 threads and 256 for the other: 8.4, and 16.1.)
+// workspace). 128 selections of up to 500 pages: 7.1 us, from the workspace one more; four of 3125: 10.8
+// and 0.7 more. (With 1024 threads the first took one more too, with 256 the other five.)
 template <typename TI, int D, int NT, int RANKS> __global__ __launch_bounds__(NT) void select_kernel(SelectArgs a) {
   extern __shared__ __attribute__((aligned(16))) float rows[];
   __shared__ SelectLds<NT> l;

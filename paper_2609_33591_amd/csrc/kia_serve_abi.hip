@@ -167,7 +167,9 @@ size_t lay(size_t at, size_t n, int d, float *ws, float *&ext, float *&stat, flo
   return at + (4 + (size_t)d) * n;
 }
 
-// Workgroups that the chip holds at once (see cached_shape of kia_around_abi.hip).
+// Workgroups that the chip holds at once, about (see cached_shape of kia_around_abi.hip): heads of 128
+// in their softmax and, with up to four heads a group, their weights; with more a group in bf16 some
+// weights' forms have two. Smaller heads and the extrema have up to eight.
 int64_t resident(int dtype) { return (int64_t)(dtype == KIA_F32 ? 2 : 3) * host_cus(); }
 
 // Selected pages: every token's list in as many parts as fill the chip, of 128 keys at least
@@ -206,7 +208,8 @@ int shared_shape(CachedArgs &a, int page, int width, int B, int H, int Hkv, int 
   a.shared = shared;
   const int G = H / Hkv;
   a.tiles = (T * G + 15) / 16;
-  // Two workgroups a CU run at once: those over the shared tokens get their part of the work's
+  // Two workgroups a CU run at once (of two row tiles in heads of 128; smaller heads and the extrema
+  // have two to eight): those over the shared tokens get their part of the work's
   // worth of that (a chunk of two row tiles costs 1.6 times one of one), half of it at least
   // (64 sequences behind 8192 tokens, 1000 of their own at most: with all of it 29.5 us, so 25).
   const int64_t groups = (int64_t)B * Hkv * a.tiles, own = keys - shared, cus = host_cus();
