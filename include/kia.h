@@ -669,7 +669,9 @@ int kia_cache4_attn(const kia_view *q, const kia_view *o, const void *cache,
  * ---- Many and long texts from the cache ------------------------------------
  *
  * Timed as "kia_cache4_append", "kia_cache4_bounds", "kia_cache4_score" and
- * "kia_cache4_select"; the attention as above.
+ * "kia_cache4_select"; the attention as above, and, of more than 64 sequences
+ * behind shared tokens in a table with room for more than 4096 others,
+ * "kia_cache4_plan".
  *
  * The bounds of a page's keys: bounds[pages][Hkv][2][d], bf16, 16-byte aligned,
  * of each channel the least (0) and the largest (1) of what the cache stands for

@@ -186,10 +186,12 @@ struct CachedArgs {
   int tiles, shares;  // 16-row tiles of a key head's rows, parts of its keys (< 256)
   // Over listed pages, and over what lies behind shared tokens: `tiles` of a token's, or a
   // sequence's, rows, `parts` for each, `shares` in all for a row tile. With `spread` (about
-  // so many in all) the sequences have parts by their lengths, up to `most`: `own` [tiles][B]
-  // says which, and `parts` is the usual number.
+  // so many in all) the sequences have parts by their lengths, up to `most`, and `parts` is the
+  // usual number. Which, is found by every workgroup, or of more than PLANNED_FROM sequences by a
+  // launch before the others:
   int parts, spread, most;
-  int2 *own;  // first part, and how many
+  int4 *plan;  // [tiles][shares]: a part's sequence (-1: none), that one's first part, parts and keys
+  int2 *own;   // [tiles][B]: a sequence's first part, and parts
   const int *list;  // [B][Hkv][T][count]
   int count;
   int shared;  // tokens
@@ -200,6 +202,10 @@ constexpr int LISTED_MOST = 1024;
 // A row's parts are joined by a workgroup, or, where up to FEW_PARTS are usual and there are many
 // rows, by D / 4 lanes.
 constexpr int FEW_PARTS = 8, MANY_ROWS = 2048;
+// (A launch takes 3 to 4 us and a walk over 64 sequences' lengths 1 to 2, but of all workgroups: 16
+// sequences behind 2048 tokens, up to 4000 of their own, 21 us planned and 18 by each; 256 behind 2048, 200
+// of their own, LERP, 45 and 49; 1024, softmax, 88 and 150.)
+constexpr int PLANNED_FROM = 64;
 // Floats of the workspace: the parts' extrema, their maxima and sums, their rows.
 struct CachedLayout {
   size_t ext, stat, part, total;

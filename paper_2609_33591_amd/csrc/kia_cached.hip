@@ -145,8 +145,7 @@ struct Share {
 
 // The same of what lies behind shared tokens: about a.spread parts in all, one at least and a.most at
 // most for a sequence. (256 sequences at a time, whose lengths are asked for together, and sums
-// without LDS: short remainders have workgroups of a few us. As Share does it, 256 sequences of 200
-// tokens of their own took 8 us longer.)
+// without LDS.)
 struct Spread {
   int b = -1, first = 0, parts = 0;
   Length length = {0};
@@ -208,9 +207,14 @@ struct Work {
       b = share.b, first = share.first, parts = share.parts;
       if (b < 0) return;
       length = length_of(a, b);
+    } else if (MODE == BEHIND && a.plan) {
+      const int4 x = a.plan[(int64_t)tile * a.shares + w];
+      b = __builtin_amdgcn_readfirstlane(x.x), first = __builtin_amdgcn_readfirstlane(x.y);
+      parts = __builtin_amdgcn_readfirstlane(x.z), length = {__builtin_amdgcn_readfirstlane(x.w)};
+      if (b < 0) return;
     } else if (MODE == BEHIND && a.spread) {
-      const Spread spread(a, tile, w);
-      b = spread.b, first = spread.first, parts = spread.parts, length = spread.length;
+      const Spread x(a, tile, w);
+      b = x.b, first = x.first, parts = x.parts, length = x.length;
       if (b < 0) return;
     } else {
       // (as many parts for every sequence, or for every token of one)
@@ -554,7 +558,8 @@ __global__ __launch_bounds__(64 * NWAVE, 2) void cached_kernel(CachedArgs a) {
   const int64_t out = slot_of(a, hk, tile, w);
   if constexpr (MODE == BEHIND && PASS != PASS_GRID) {
     // (the first pass, for later launches)
-    if (a.spread && hk == 0 && w == work.first && tid == 0) a.own[tile * a.B + b] = make_int2(work.first, work.parts);
+    if (a.spread && !a.plan && hk == 0 && w == work.first && tid == 0)
+      a.own[(int64_t)tile * a.B + b] = make_int2(work.first, work.parts);
   }
   if constexpr (PASS == PASS_EXTREMA) {
     m = across<FEW>(m, [](float x, float y) { return fmaxf(x, y); });
@@ -756,6 +761,17 @@ template <typename TI, int D> __global__ __launch_bounds__(256) void join_few_ke
   else *reinterpret_cast<u32x2 *>(out) = u32x2{cvt_bf16x2(x[0], x[1]), cvt_bf16x2(x[2], x[3])};
 }
 
+// The parts by lengths of what lies behind shared tokens, a wave each.
+__global__ __launch_bounds__(64 * NWAVE) void plan_kernel(CachedArgs a) {
+  const int id = __builtin_amdgcn_readfirstlane(blockIdx.x * NWAVE + (threadIdx.x >> 6));
+  if (id >= a.shares * a.tiles) return;
+  const int tile = (unsigned)id / (unsigned)a.shares, w = (unsigned)id % (unsigned)a.shares;
+  const Spread x(a, tile, w);
+  if ((threadIdx.x & 63) != 0) return;
+  a.plan[id] = make_int4(x.b, x.first, x.parts, x.length.n);
+  if (x.b >= 0 && w == x.first) a.own[(int64_t)tile * a.B + x.b] = make_int2(x.first, x.parts);
+}
+
 // The passes' launches (g: workgroups, join: whether a row has several parts).
 template <typename TI, int D, bool FEW, int CALIB, int RT>
 void grid_passes(const CachedArgs &a, dim3 g, hipStream_t s) {
@@ -780,6 +796,12 @@ template <typename TI, int D, int CALIB, int RT> void grid_rows(const CachedArgs
 template <typename TI, int D, int RT> void run(const CachedArgs &a, bool join, hipStream_t s) {
   const int parts = MODE == SEQUENCE ? a.shares + a.B : a.shares;
   const dim3 g((RT ? a.pre.blocks : 0) + (unsigned)parts * a.Hkv * a.tiles);
+  if constexpr (RT > 0) {
+    if (a.plan)
+      timed_call("kia_cache4_plan", s, [&] {
+        hipLaunchKernelGGL(plan_kernel, dim3(((unsigned)a.shares * a.tiles + NWAVE - 1) / NWAVE), dim3(64 * NWAVE), 0, s, a);
+      });
+  }
   if (a.recon == REC_SOFTMAX) {
     timed_call("kia_cache4_attn", s, [&] {
       hipLaunchKernelGGL((cached_kernel<TI, D, PASS_SOFTMAX, CAL_FWM, REC_SOFTMAX, false, RT>), g,

@@ -26,7 +26,7 @@ typedef float WaveStats[NWAVE][16][2];
 // The parts of what lies behind the shared tokens, of row tile `tile` of sequence b: the first
 // one's number, and how many.
 __device__ __forceinline__ int2 own_parts(const CachedArgs &a, unsigned tile, unsigned b) {
-  return a.spread ? a.own[tile * a.B + b] : make_int2(b * a.parts, a.parts);
+  return a.spread ? a.own[(int64_t)tile * a.B + b] : make_int2(b * a.parts, a.parts);
 }
 
 // A row's extrema (scaled) over the shared tokens and what lies behind them, from the first pass.

@@ -195,10 +195,10 @@ size_t pages_lay(CachedArgs &a, int d, float *ws) {
 // Shared tokens: the rows of all sequences over them in parts that fill the chip, and each
 // sequence's over what lies behind: as many parts for each, or, where the table has room for texts
 // that pass the shared tokens by more than SPREAD_FROM, about as many in all by the lengths (256
-// sequences behind 8192 tokens, 200 of their own and one 100 000: 60 us, with its own in one part 660,
-// without shared tokens 206; one 30 000: 55 and 214; one 4000: as many parts for each 51, by lengths 49).
-// Where all are short in such a table it costs a few us: 41 -> 47 for 256 of 200, 32 -> 35 for 64 of up
-// to 1000 (LERP), as each workgroup walks the lengths.
+// sequences behind 8192 tokens, 200 of their own and one 100 000, softmax: 63 us, with its own in one part
+// 657, without shared tokens 214; one 30 000: 54 and 214; one 4000: as many parts for each 52, by lengths
+// 49). Where all are short in such a table finding the parts costs 0 to 6 us: 41 -> 45 for those 256, 21 ->
+// 25 for 64 of up to 1000; of thousands a tenth (2048 behind 2048: 154 -> 171).
 constexpr int SPREAD_FROM = 4096;
 int shared_shape(CachedArgs &a, int page, int width, int B, int H, int Hkv, int T, int d, int shared, int dtype) {
   const int rc = check_sizes(a, page, width, B, H, Hkv, T, d);
@@ -214,8 +214,9 @@ int shared_shape(CachedArgs &a, int page, int width, int B, int H, int Hkv, int 
   // (64 sequences behind 8192 tokens, 1000 of their own at most: with all of it 29.5 us, so 25).
   const int64_t groups = (int64_t)B * Hkv * a.tiles, own = keys - shared, cus = host_cus();
   a.parts = (int)std::max<int64_t>(1, std::min<int64_t>({2 * cus / groups, (own + 255) / 256, 64}));
-  // (a begun part a sequence is half of one)
-  if (own > SPREAD_FROM) a.spread = B * a.parts - B / 2;
+  // (a begun part a sequence is half of one; of many sequences no more than run at once beside theirs)
+  if (own > SPREAD_FROM)
+    a.spread = (int)std::max<int64_t>(1, std::min<int64_t>(B * a.parts - B / 2, 2 * cus / ((int64_t)Hkv * a.tiles)));
   a.shares = a.spread ? a.spread + B : B * a.parts;
   a.pre.tiles = (int)(((int64_t)B * T * G + 15) / 16);
   const int rt = prefix_tiles(a.pre.tiles, d, dtype);
@@ -233,8 +234,11 @@ int shared_shape(CachedArgs &a, int page, int width, int B, int H, int Hkv, int 
 size_t shared_lay(CachedArgs &a, int d, float *ws) {
   const size_t at = lay(0, (size_t)a.shares * a.Hkv * a.tiles * 16, d, ws, a.ext, a.stat, a.part);
   const size_t end = lay(at, (size_t)a.Hkv * a.pre.tiles * 16 * a.pre.parts, d, ws, a.pre.ext, a.pre.stat, a.pre.part);
-  if (ws) a.own = reinterpret_cast<int2 *>(ws + end);
-  return end + (a.spread ? 2 * (size_t)a.tiles * a.B : 0);
+  if (!a.spread) return end;
+  const size_t entries = a.B > PLANNED_FROM ? (size_t)a.tiles * a.shares : 0;
+  if (ws && entries) a.plan = reinterpret_cast<int4 *>(ws + end);
+  if (ws) a.own = reinterpret_cast<int2 *>(ws + end + 4 * entries);
+  return end + 4 * entries + 2 * (size_t)a.tiles * a.B;
 }
 
 }  // namespace

@@ -70,6 +70,23 @@ def test_shared_and_many_sequences(op, B, H):
         assert torch.equal(y, call())
 
 
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("op", OPS, ids=lambda op: "-".join(str(x) for x in op.values()))
+@pytest.mark.parametrize("B,H,Hkv,T,d", ((64, 12, 2, 3, 32), (65, 12, 2, 3, 32), (90, 20, 1, 5, 64)))
+def test_long_remainders_of_many_row_tiles(dtype, op, B, H, Hkv, T, d):
+    """Sequences of several row tiles, as many as find their parts in each workgroup and more, queries
+    before the text and texts that end within the shared tokens among them."""
+    page, shared = 32, 64
+    lengths = [(shared + b, shared, 1 + b % 70, 0)[b % 4] for b in range(B)]
+    lengths[0], lengths[B - 1] = 4700, 5300
+    cache, table, _, k, v = filled(tuple(lengths), Hkv, d, page, dtype, 200, 0.7, shared)
+    q = draw((B, H, T, d), dtype, 204)
+    o = kia.cache4_attention(q, cache, table, ints(*lengths), shared=shared, **op)
+    for b, m in enumerate(lengths):
+        want = ref.cached(q[b], k[b, :, :m], v[b, :, :m], m, **{**dict(K=4, calib="fwm", tau=8.0), **op})
+        ref.within(o[b], *want, f"sequence {b}")
+
+
 def shortest(call, runs=20):
     times = []
     for _ in range(runs):
